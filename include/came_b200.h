@@ -185,6 +185,15 @@ came_status came_create(came_ctx** out, const came_tensor* t, int32_t n, int32_t
 came_status came_step(came_ctx* ctx, const came_hparams* hp, const void* const* grads,
                       void* cuda_stream);
 
+/* came_step with a further gradient pre-scale that lives on the device: the step uses
+ * g_t = grad_scale * (*device_scale) * (gradient buffer).  `device_scale` (DEVICE fp32 [1],
+ * 4-byte aligned, NULL = none) is read by the step's kernels on `cuda_stream`, so an earlier
+ * kernel of that stream may have just written it: with results + 1 of came_clip_norm the step
+ * takes clipped gradients without any pass that writes them, and without the host ever seeing the
+ * norm.  Everything else as came_step; device_scale == NULL is exactly came_step. */
+came_status came_step_scaled(came_ctx* ctx, const came_hparams* hp, const void* const* grads,
+                             const float* device_scale, void* cuda_stream);
+
 /* Same step, fed from and drained to HOST memory: for every tensor i copies
  * host_grads[i] (HOST, grad_dtype [rows*cols], ideally pinned) into the tensor's
  * device gradient buffer, runs the step, then, where host_params_out is not NULL
@@ -316,6 +325,56 @@ came_status came_factor_update_static_plan(const void* grad, int32_t grad_dtype,
                                            int64_t cols, const float* r, const float* c,
                                            double beta2, double eps1, int32_t device,
                                            int32_t* out_vec, int64_t* out_scratch_bytes);
+
+/* ---- Global gradient norm and clipping ----------------------------------------------------
+ *
+ * For a list of gradient tensors g_i and a host pre-scale s:
+ *   n_i  = s sqrt(sum_j g_ij^2)            N = sqrt(sum_i n_i^2)
+ *   coef = 1                               if N + eps <= max_norm
+ *        = max_norm / (N + eps)            otherwise
+ *   out_ij = g_ij * (s * coef)             rounded once, to nearest even (came_clip_grads only)
+ * Squares are added in fp32 within a thread (a few hundred terms) and in double from there on, in
+ * a fixed order: results are bit-reproducible.  A finite N is found even where squares overflow
+ * fp32; gradients below 1e-19 in magnitude may count as zero.  Inf or NaN in a gradient gives
+ * N = inf or NaN and coef = 0 or NaN, as the formulas do; nothing is skipped.
+ *
+ * A gradient may have any length (0 included) and any element-aligned address; it is contiguous.
+ * Outputs (optional, for all tensors or for none) may be the gradient buffers themselves, of the
+ * same dtype, else they share memory with no other buffer of the list (CAME_ERR_OVERLAP). */
+typedef struct came_clip_ctx came_clip_ctx;   /* opaque */
+
+typedef struct {
+    const void* grad;         /* DEVICE grad_dtype [numel]; may be NULL when numel == 0 */
+    void*       out;          /* DEVICE out_dtype [numel] or NULL                        */
+    int64_t     numel;        /* >= 0                                                    */
+    int32_t     grad_dtype;   /* came_dtype                                              */
+    int32_t     out_dtype;    /* came_dtype (ignored without an output)                  */
+} came_clip_tensor;
+
+typedef struct {
+    double max_norm;          /* > 0; infinity = never clip       */
+    double eps;               /* >= 0, finite                     */
+    double grad_scale;        /* s > 0, as in came_hparams; 0 = 1 */
+} came_clip_params;
+
+/* Plans the tiles and allocates the context's tables and workspace; `t`: HOST array of n
+ * descriptors; `device` must be current.  Synchronises the device once.  Errors of these
+ * functions are reported through came_last_error(NULL) on the calling thread. */
+came_status came_clip_create(came_clip_ctx** out, const came_clip_tensor* t, int32_t n, int32_t device);
+
+/* One launch: `results` (DEVICE fp32 [2 + n], 4-byte aligned) receives N, coef, n_0 .. n_{n-1}.
+ * `grads`: HOST array of n DEVICE pointers that replace the gradients given before (the outputs of
+ * tensors clipped in place move with them), or NULL.  Asynchronous on `cuda_stream`; allocates
+ * nothing.  One context serves one stream at a time. */
+came_status came_clip_norm(came_clip_ctx* ctx, const came_clip_params* p, const void* const* grads,
+                           float* results, void* cuda_stream);
+
+/* came_clip_norm and then the outputs (a second launch).  CAME_ERR_UNSUPPORTED without outputs. */
+came_status came_clip_grads(came_clip_ctx* ctx, const came_clip_params* p, const void* const* grads,
+                            float* results, void* cuda_stream);
+
+/* Frees the context; the caller has synchronised the streams it used. */
+came_status came_clip_destroy(came_clip_ctx* ctx);
 
 /* Process-wide tuning knobs, read by later came_create calls (each knob is an atomic, so any
  * thread may set one; a context takes the values in force while it is being created, so set

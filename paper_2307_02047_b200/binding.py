@@ -16,6 +16,9 @@ from typing import List, Optional, Sequence
 from . import build as _build
 
 CAME_OK = 0
+(CAME_ERR_NULL, CAME_ERR_SHAPE, CAME_ERR_DTYPE, CAME_ERR_ALIGN, CAME_ERR_HPARAM, CAME_ERR_STEP_ORDER,
+ CAME_ERR_DEVICE, CAME_ERR_OOM, CAME_ERR_CUDA, CAME_ERR_INTERNAL, CAME_ERR_UNSUPPORTED,
+ CAME_ERR_OVERLAP) = range(1, 13)
 CAME_F32, CAME_BF16 = 0, 1
 CAME_T_NO_WEIGHT_DECAY = 1
 CAME_T_VEC_NO_CONFIDENCE = 2
@@ -45,7 +48,8 @@ EXPORTED = ["came_create", "came_step", "came_step_host", "came_destroy", "came_
             "came_phase_name", "came_plan_tensor", "came_tune", "came_factor_update_static",
             "came_factor_update_static_plan", "came_required_grad_alignment",
             "came_device_status", "came_lr_warmup", "came_clear_device_error",
-            "came_selftest_wait_timeout", "came_debug_bounds"]
+            "came_selftest_wait_timeout", "came_debug_bounds", "came_step_scaled",
+            "came_clip_create", "came_clip_norm", "came_clip_grads", "came_clip_destroy"]
 
 
 class CameError(RuntimeError):
@@ -68,6 +72,16 @@ class came_hparams(ctypes.Structure):
                 ("beta3", ctypes.c_double), ("eps1", ctypes.c_double), ("eps2", ctypes.c_double),
                 ("clip_d", ctypes.c_double), ("weight_decay", ctypes.c_double),
                 ("step", ctypes.c_int64), ("grad_scale", ctypes.c_double)]
+
+
+class came_clip_tensor(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("grad_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
+class came_clip_params(ctypes.Structure):
+    _fields_ = [("max_norm", ctypes.c_double), ("eps", ctypes.c_double),
+                ("grad_scale", ctypes.c_double)]
 
 
 _lib = None
@@ -157,6 +171,16 @@ def _bind(L):
     L.came_selftest_wait_timeout.restype = i32
     L.came_debug_bounds.argtypes = [i32, ctypes.POINTER(ctypes.c_uint32)]
     L.came_debug_bounds.restype = i32
+    L.came_step_scaled.argtypes = [vp, ctypes.POINTER(came_hparams), ctypes.POINTER(vp), vp, vp]
+    L.came_step_scaled.restype = i32
+    L.came_clip_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(came_clip_tensor), i32, i32]
+    L.came_clip_create.restype = i32
+    L.came_clip_norm.argtypes = [vp, ctypes.POINTER(came_clip_params), ctypes.POINTER(vp), vp, vp]
+    L.came_clip_norm.restype = i32
+    L.came_clip_grads.argtypes = L.came_clip_norm.argtypes
+    L.came_clip_grads.restype = i32
+    L.came_clip_destroy.argtypes = [vp]
+    L.came_clip_destroy.restype = i32
     return L
 
 
@@ -183,6 +207,17 @@ def came_step(ctx, hp: came_hparams, grads: Optional[Sequence[int]] = None, stre
     if grads is not None:
         garr = (ctypes.c_void_p * len(grads))(*grads)
     _check(L.came_step(ctx, ctypes.byref(hp), garr, ctypes.c_void_p(stream)), ctx)
+
+
+def came_step_scaled(ctx, hp: came_hparams, grads: Optional[Sequence[int]], device_scale: int,
+                     stream: int = 0) -> None:
+    """came_step with a further gradient pre-scale read from device memory (address of one fp32)."""
+    L = load()
+    garr = None
+    if grads is not None:
+        garr = (ctypes.c_void_p * len(grads))(*grads)
+    _check(L.came_step_scaled(ctx, ctypes.byref(hp), garr, ctypes.c_void_p(device_scale),
+                              ctypes.c_void_p(stream)), ctx)
 
 
 def came_step_host(ctx, hp: came_hparams, host_grads: Sequence[int],
@@ -299,11 +334,136 @@ def came_debug_bounds(device: int = 0) -> dict:
     return dict(zip(("code", "rb", "cb", "rows", "cols", "threads"), (int(x) for x in out)))
 
 
+def came_clip_create(tensors: Sequence[came_clip_tensor], device: int = 0) -> ctypes.c_void_p:
+    ctx = ctypes.c_void_p()
+    arr = (came_clip_tensor * len(tensors))(*tensors)
+    _check(load().came_clip_create(ctypes.byref(ctx), arr, len(tensors), device))
+    return ctx
+
+
+def came_clip_norm(ctx, params: came_clip_params, results: int, grads: Optional[Sequence[int]] = None,
+                   stream: int = 0) -> None:
+    garr = None if grads is None else (ctypes.c_void_p * len(grads))(*grads)
+    _check(load().came_clip_norm(ctx, params, garr, results, stream))
+
+
+def came_clip_grads(ctx, params: came_clip_params, results: int, grads: Optional[Sequence[int]] = None,
+                    stream: int = 0) -> None:
+    garr = None if grads is None else (ctypes.c_void_p * len(grads))(*grads)
+    _check(load().came_clip_grads(ctx, params, garr, results, stream))
+
+
+def came_clip_destroy(ctx) -> None:
+    _check(load().came_clip_destroy(ctx))
+
+
 def make_hparams(step: int, **kw) -> came_hparams:
     return came_hparams(float(kw["lr"]), float(kw["beta1"]), float(kw["beta2"]), float(kw["beta3"]),
                         float(kw["eps1"]), float(kw["eps2"]), float(kw["clip_d"]),
                         float(kw.get("weight_decay", 0.0)), int(step),
                         float(kw.get("grad_scale", 1.0)))
+
+
+# --- gradient norm and clipping ------------------------------------------------------------
+
+def _cuda_tensor(x, name, dtype=None, device=None) -> None:
+    if not x.is_cuda or (device is not None and x.device != device):
+        raise CameError(CAME_ERR_DEVICE, f"{name} must be a CUDA tensor on {device or 'a GPU'}")
+    if dtype is not None and x.dtype != dtype:
+        raise CameError(CAME_ERR_DTYPE, f"{name} must be {dtype}, got {x.dtype}")
+
+
+def _dtype_code(x, name) -> int:
+    import torch
+    code = {torch.float32: CAME_F32, torch.bfloat16: CAME_BF16}.get(x.dtype)
+    if code is None:
+        raise CameError(CAME_ERR_DTYPE, f"{name} must be fp32 or bf16, got {x.dtype}")
+    return code
+
+
+class GradClip:
+    """The global norm of a list of gradients, and clipping by it.
+
+    ``grads``: contiguous fp32 or bf16 CUDA tensors of any shape, read by every call (their
+    storage may be refilled).  ``outs``: where ``clip`` writes, tensors of the same sizes (``grads``
+    itself clips in place), fp32 or bf16; None: norm only.  After a call ``total_norm``, ``coef``
+    (CUDA scalars) and ``tensor_norms`` (one per tensor) hold its results, until the next call.
+    """
+
+    def __init__(self, grads, outs=None):
+        import torch
+        self.ctx = None
+        self.grads = list(grads)
+        self.outs = None if outs is None else list(outs)
+        if not self.grads:
+            raise CameError(CAME_ERR_SHAPE, "need at least one tensor")
+        if self.outs is not None and len(self.outs) != len(self.grads):
+            raise CameError(CAME_ERR_SHAPE, "outs must be as many as grads")
+        self.device = self.grads[0].device
+        descs = []
+        for i, g in enumerate(self.grads):
+            o = None if self.outs is None else self.outs[i]
+            self._check_tensor(g, f"grads[{i}]")
+            if o is not None:
+                self._check_tensor(o, f"outs[{i}]")
+                if o.numel() != g.numel():
+                    raise CameError(CAME_ERR_SHAPE, f"outs[{i}] has another size than grads[{i}]")
+            descs.append(came_clip_tensor(g.data_ptr(), None if o is None else o.data_ptr(), g.numel(),
+                                          _dtype_code(g, f"grads[{i}]"),
+                                          0 if o is None else _dtype_code(o, f"outs[{i}]")))
+        self._codes = [d.grad_dtype for d in descs]
+        self.results = torch.zeros(2 + len(descs), dtype=torch.float32, device=self.device)
+        self.total_norm, self.coef, self.tensor_norms = self.results[0], self.results[1], self.results[2:]
+        self._results_at = self.results.data_ptr()
+        self._stream = torch.cuda.current_stream
+        self._params = came_clip_params()
+        with torch.cuda.device(self.device):
+            self.ctx = came_clip_create(descs, self.device.index)
+
+    def _check_tensor(self, x, name):
+        _cuda_tensor(x, name, None, self.device)
+        if not x.is_contiguous():
+            raise CameError(CAME_ERR_UNSUPPORTED, f"{name} must be contiguous")
+
+    def _run(self, call, max_norm, eps, grad_scale, grads):
+        at = None
+        if grads is not None:
+            grads = list(grads)
+            if len(grads) != len(self.grads):
+                raise CameError(CAME_ERR_SHAPE, "grads must be as many as at creation")
+            for i, (g, old) in enumerate(zip(grads, self.grads)):
+                self._check_tensor(g, f"grads[{i}]")
+                if g.numel() != old.numel() or _dtype_code(g, f"grads[{i}]") != self._codes[i]:
+                    raise CameError(CAME_ERR_SHAPE, f"grads[{i}] must keep its size and dtype")
+            at = [g.data_ptr() for g in grads]
+        p = self._params
+        p.max_norm, p.eps, p.grad_scale = max_norm, eps, grad_scale
+        call(self.ctx, p, self._results_at, at, self._stream(self.device).cuda_stream)
+        if grads is not None:
+            self.grads = grads
+        return self.total_norm, self.coef, self.tensor_norms
+
+    def norm(self, max_norm: float = float("inf"), eps: float = 1e-6, grad_scale: float = 1.0,
+             grads=None):
+        """``(total_norm, coef, tensor_norms)``; ``grads`` replaces the tensors of earlier calls."""
+        return self._run(came_clip_norm, max_norm, eps, grad_scale, grads)
+
+    def clip(self, max_norm: float, eps: float = 1e-6, grad_scale: float = 1.0, grads=None):
+        """``norm``, and ``outs = grads * (grad_scale * coef)``."""
+        return self._run(came_clip_grads, max_norm, eps, grad_scale, grads)
+
+    def close(self) -> None:
+        if self.ctx is not None:
+            import torch
+            torch.cuda.synchronize(self.device)
+            came_clip_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 # --- convenience wrapper -------------------------------------------------------------------
@@ -350,10 +510,17 @@ class CameOptimizer:
         self.ctx = came_create(descs, device=device, flags=create_flags)
         self.step_count = 0
 
-    def step(self, **hp) -> None:
+    def step(self, device_scale=None, **hp) -> None:
+        """``device_scale``: an fp32 CUDA scalar that multiplies every gradient (``GradClip.coef``:
+        the step then takes clipped gradients that nothing has to write)."""
+        if device_scale is not None:
+            _cuda_tensor(device_scale, "device_scale", self.torch.float32, self.params[0].device)
+            if device_scale.numel() != 1:
+                raise CameError(CAME_ERR_SHAPE, "device_scale must hold one value")
         self.step_count += 1
         stream = self.torch.cuda.current_stream().cuda_stream
-        came_step(self.ctx, make_hparams(self.step_count, **hp), None, stream)
+        came_step_scaled(self.ctx, make_hparams(self.step_count, **hp), None,
+                         0 if device_scale is None else device_scale.data_ptr(), stream)
 
     def query(self, what: int) -> int:
         return came_query(self.ctx, what)

@@ -5,6 +5,7 @@
 #include "came_kernels.cuh"
 #include "came_pipelined.cuh"
 #include "came_stream.cuh"
+#include "ops/came_ops.cuh"
 
 #include <algorithm>
 #include <atomic>
@@ -293,7 +294,7 @@ StepConsts make_consts(const came_hparams& h)
     const double gs = h.grad_scale == 0.0 ? 1.0 : h.grad_scale;
     c.gscale = static_cast<float>(gs);
     c.gscale2 = static_cast<float>(gs * gs);
-    c.pad_ = 0.f;
+    c.dscale = nullptr;
     c.clip_d = h.clip_d;
     return c;
 }
@@ -425,9 +426,11 @@ int launch_range(const came_ctx* ctx, const StepConsts& hc, cudaStream_t stream,
     return iv;
 }
 
-came_status launch_step(came_ctx* ctx, const came_hparams* hp, cudaStream_t stream)
+came_status launch_step(came_ctx* ctx, const came_hparams* hp, const float* device_scale,
+                        cudaStream_t stream)
 {
-    const StepConsts hc = make_consts(*hp);
+    StepConsts hc = make_consts(*hp);
+    hc.dscale = device_scale;
     if (ctx->pipelined) {
         const bool prof = ctx->profiling && !ctx->prof_ev.empty();
         cudaEvent_t* ev = prof ? &ctx->prof_ev[(ctx->prof_count % kProfSlots) * (kMaxPhases + 1)] : nullptr;
@@ -541,6 +544,30 @@ came_status check_current_device(came_ctx* ctx)
 }
 
 }  // namespace
+
+// Error reporting shared with the operators in csrc/ops (contexts of their own, or none): the
+// text goes where came_last_error(NULL) finds it.
+namespace came_ops {
+
+came_status report(came_status s, const char* msg) { return fail(nullptr, s, msg); }
+
+came_status report_cuda(cudaError_t e, const char* what) { return cuda_fail(nullptr, e, what); }
+
+came_status require_current_device(int32_t device)
+{
+    int cur = -1;
+    const cudaError_t e = cudaGetDevice(&cur);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(nullptr, CAME_ERR_DEVICE, "no usable CUDA device");
+    }
+    if (came_device_status(device, cur) == CAME_OK) return CAME_OK;
+    char buf[120];
+    std::snprintf(buf, sizeof buf, "the tensors live on device %d but device %d is current", device, cur);
+    return fail(nullptr, CAME_ERR_DEVICE, buf);
+}
+
+}  // namespace came_ops
 
 extern "C" {
 
@@ -906,8 +933,15 @@ came_status came_create(came_ctx** out, const came_tensor* t, int32_t n, int32_t
 came_status came_step(came_ctx* ctx, const came_hparams* hp, const void* const* grads,
                       void* cuda_stream)
 {
+    return came_step_scaled(ctx, hp, grads, nullptr, cuda_stream);
+}
+
+came_status came_step_scaled(came_ctx* ctx, const came_hparams* hp, const void* const* grads,
+                             const float* device_scale, void* cuda_stream)
+{
     if (!ctx) return CAME_ERR_NULL;
     if (!hp) return fail(ctx, CAME_ERR_NULL, "hparams is NULL");
+    if (!aligned(device_scale, 4)) return fail(ctx, CAME_ERR_ALIGN, "device_scale not 4-byte aligned");
     std::string msg;
     came_status s = validate_hparams(*hp, ctx->last_step, msg);
     if (s != CAME_OK) return fail(ctx, s, msg);
@@ -934,7 +968,7 @@ came_status came_step(came_ctx* ctx, const came_hparams* hp, const void* const* 
             if (s != CAME_OK) return s;
         }
     }
-    return launch_step(ctx, hp, stream);
+    return launch_step(ctx, hp, device_scale, stream);
 }
 
 came_status came_step_host(came_ctx* ctx, const came_hparams* hp, const void* const* host_grads,

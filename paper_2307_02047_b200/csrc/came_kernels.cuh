@@ -122,7 +122,8 @@ struct StepConsts {
     float eps1, eps2;
     float lr, wd;
     float gscale, gscale2;   // gradient pre-scale s and s^2 (g_t = s * gradient buffer)
-    float pad_;
+    const float* dscale;     // device memory: a further factor of s, read by every kernel of the
+                             // step (NULL = none)
     double clip_d;
 };
 
@@ -1133,6 +1134,17 @@ __device__ __forceinline__ Tile fetch_tile(const Tile* tiles, int ntiles, int re
 __device__ __forceinline__ void pdl_release_dependents() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait_for_previous_grid() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// The pre-scale that lives in device memory (a clipping coefficient computed by an earlier kernel
+// of the stream): call after the wait, before the constants are used.
+__device__ __forceinline__ void apply_device_scale(StepConsts& hc)
+{
+    if (hc.dscale) {
+        const float s = __ldcg(hc.dscale);
+        hc.gscale *= s;
+        hc.gscale2 = hc.gscale * hc.gscale;
+    }
+}
+
 __global__ void __launch_bounds__(kThreads, CAME_P1_MINB)
 k_p1_reduce_g2(const TensorDev* __restrict__ T, const Tile* __restrict__ tiles, int ntiles,
                int reverse, StepConsts hc)
@@ -1142,6 +1154,7 @@ k_p1_reduce_g2(const TensorDev* __restrict__ T, const Tile* __restrict__ tiles, 
     const Tile t = fetch_tile(tiles, ntiles, reverse);
     const TensorDev d = T[t.tensor];       // by value: descriptor fields live in registers
     pdl_wait_for_previous_grid();
+    apply_device_scale(hc);
     if (d.ndim == 1) { vec_second_moment_chunk(d, t.rb, hc, sm); return; }
     CAME_DISPATCH(p1_tile, d, t.rb, t.cb, hc, sm)
 }
@@ -1155,6 +1168,7 @@ k_p2_sum_u2(const TensorDev* __restrict__ T, const Tile* __restrict__ tiles, int
     const Tile t = fetch_tile(tiles, ntiles, reverse);
     const TensorDev d = T[t.tensor];
     pdl_wait_for_previous_grid();
+    apply_device_scale(hc);
     if (d.ndim == 1) return;               // vectors have no second reduction pass
     CAME_DISPATCH(p2_tile, d, t.rb, t.cb, hc, sm)
 }
@@ -1168,6 +1182,7 @@ k_p3_momentum_instability(const TensorDev* __restrict__ T, const Tile* __restric
     const Tile t = fetch_tile(tiles, ntiles, reverse);
     const TensorDev d = T[t.tensor];
     pdl_wait_for_previous_grid();
+    apply_device_scale(hc);
     if (d.ndim == 1) { vec_apply_chunk(d, t.rb, hc); return; }
     CAME_DISPATCH(p3_tile, d, t.rb, t.cb, hc, sm)
 }
@@ -1192,6 +1207,7 @@ k_p34_adafactor_apply(const TensorDev* __restrict__ T, const Tile* __restrict__ 
     const Tile t = fetch_tile(tiles, ntiles, reverse);
     const TensorDev d = T[t.tensor];
     pdl_wait_for_previous_grid();
+    apply_device_scale(hc);
     if (d.ndim == 1) { vec_apply_chunk(d, t.rb, hc); return; }
     CAME_DISPATCH(p34_adafactor_tile, d, t.rb, t.cb, hc)
 }

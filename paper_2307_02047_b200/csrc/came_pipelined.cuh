@@ -91,6 +91,7 @@ k_step_pipelined(const TensorDev* __restrict__ T, const Item* __restrict__ items
     // a grid that starts with the error word set hands out no ticket and changes nothing
     if (s_ctl[0] != 0u) return;
     const unsigned epoch = s_ctl[1];
+    apply_device_scale(hc);
 
     if (tid >= kThreads) {
         // ---------------- helper warp ----------------

@@ -217,6 +217,7 @@ k_p1_stream(const TensorDev* __restrict__ T, const StreamTile* __restrict__ st, 
     if (has_cur) cur = load_stream_tile(st + t);
     if (has_nxt) nxt = load_stream_tile(st + t + G);
     pdl_wait_for_previous_grid();
+    apply_device_scale(hc);
     unsigned issued = 0u, consumed = 0u;
     int iq = 0, ib = 0;                         // where the next copy batch comes from: tile (0 cur, 1 nxt), batch
     while (has_cur) {
