@@ -376,6 +376,49 @@ came_status came_clip_grads(came_clip_ctx* ctx, const came_clip_params* p, const
 /* Frees the context; the caller has synchronised the streams it used. */
 came_status came_clip_destroy(came_clip_ctx* ctx);
 
+/* ---- Embedding lookup and its gradient -------------------------------------------------------
+ *
+ * Forward:   out[t, :] = rn(scale * W[id_t, :]) for 0 <= id_t < rows, and 0 for any other id
+ *            (masked or padding tokens are often -1).
+ * Backward:  dW[v, :] = rn(scale * sum over the tokens t with id_t = v of dY[t, :]), every row
+ *            written (rows without tokens with 0); with CAME_EMBED_ACCUMULATE
+ *            dW[v, :] = rn(dW[v, :] + scale * sum ...), rows without tokens untouched.
+ * The sums are fp32, a row's tokens are added in an order fixed by the ids alone, and each result
+ * is rounded once: results are bit-reproducible.  Lengths from zero tokens and one column up; rows
+ * may have any stride >= cols and any element-aligned address (aligned ones are faster).  The
+ * output shares no memory with an input (CAME_ERR_OVERLAP). */
+typedef enum { CAME_I32 = 0, CAME_I64 = 1 } came_id_dtype;
+
+enum {
+    CAME_EMBED_ACCUMULATE  = 1u << 0,   /* backward: add to dW instead of overwriting it     */
+    CAME_EMBED_PADDING_ROW = 1u << 1    /* backward: tokens of row padding_row add nothing   */
+};
+
+typedef struct {
+    void*       table;        /* DEVICE table_dtype [rows][table_ld]: W (read) or dW (written) */
+    void*       data;         /* DEVICE data_dtype [tokens][data_ld]: out (written) or dY (read) */
+    const void* ids;          /* DEVICE id_dtype [tokens]                                    */
+    int64_t     rows, cols;   /* >= 1                                                        */
+    int64_t     tokens;       /* >= 0 (data and ids may then be NULL)                        */
+    int64_t     table_ld, data_ld;      /* elements from row to row, >= cols                 */
+    int64_t     padding_row;  /* used with CAME_EMBED_PADDING_ROW                            */
+    double      scale;        /* finite                                                      */
+    int32_t     table_dtype, data_dtype;   /* came_dtype                                     */
+    int32_t     id_dtype;     /* came_id_dtype                                               */
+    uint32_t    flags;        /* CAME_EMBED_*; forward: 0                                    */
+    uint32_t    reserved;     /* must be 0                                                   */
+} came_embed;
+
+/* Asynchronous on `cuda_stream`; allocate nothing; `device` must be current and hold every
+ * buffer.  Errors through came_last_error(NULL).  The backward pass needs `workspace` (DEVICE,
+ * 16-byte aligned, at least the bytes that came_embed_workspace answers for the same descriptor; no
+ * CUDA call there); its contents need not be kept between calls, and calls that may run at the
+ * same time need one each. */
+came_status came_embed_forward(const came_embed* e, int32_t device, void* cuda_stream);
+came_status came_embed_workspace(const came_embed* e, int64_t* out_bytes);
+came_status came_embed_backward(const came_embed* e, void* workspace, int64_t workspace_bytes,
+                                int32_t device, void* cuda_stream);
+
 /* Process-wide tuning knobs, read by later came_create calls (each knob is an atomic, so any
  * thread may set one; a context takes the values in force while it is being created, so set
  * them before the contexts they are meant for).  CAME_TUNE_TILE_ELEMS:

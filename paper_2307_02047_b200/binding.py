@@ -20,6 +20,8 @@ CAME_OK = 0
  CAME_ERR_DEVICE, CAME_ERR_OOM, CAME_ERR_CUDA, CAME_ERR_INTERNAL, CAME_ERR_UNSUPPORTED,
  CAME_ERR_OVERLAP) = range(1, 13)
 CAME_F32, CAME_BF16 = 0, 1
+CAME_I32, CAME_I64 = 0, 1
+CAME_EMBED_ACCUMULATE, CAME_EMBED_PADDING_ROW = 1, 2
 CAME_T_NO_WEIGHT_DECAY = 1
 CAME_T_VEC_NO_CONFIDENCE = 2
 CAME_CREATE_KEEP_STATE = 1
@@ -49,7 +51,8 @@ EXPORTED = ["came_create", "came_step", "came_step_host", "came_destroy", "came_
             "came_factor_update_static_plan", "came_required_grad_alignment",
             "came_device_status", "came_lr_warmup", "came_clear_device_error",
             "came_selftest_wait_timeout", "came_debug_bounds", "came_step_scaled",
-            "came_clip_create", "came_clip_norm", "came_clip_grads", "came_clip_destroy"]
+            "came_clip_create", "came_clip_norm", "came_clip_grads", "came_clip_destroy",
+            "came_embed_forward", "came_embed_workspace", "came_embed_backward"]
 
 
 class CameError(RuntimeError):
@@ -82,6 +85,15 @@ class came_clip_tensor(ctypes.Structure):
 class came_clip_params(ctypes.Structure):
     _fields_ = [("max_norm", ctypes.c_double), ("eps", ctypes.c_double),
                 ("grad_scale", ctypes.c_double)]
+
+
+class came_embed(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("data", ctypes.c_void_p), ("ids", ctypes.c_void_p),
+                ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("table_ld", ctypes.c_int64), ("data_ld", ctypes.c_int64),
+                ("padding_row", ctypes.c_int64), ("scale", ctypes.c_double),
+                ("table_dtype", ctypes.c_int32), ("data_dtype", ctypes.c_int32),
+                ("id_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 _lib = None
@@ -181,6 +193,12 @@ def _bind(L):
     L.came_clip_grads.restype = i32
     L.came_clip_destroy.argtypes = [vp]
     L.came_clip_destroy.restype = i32
+    L.came_embed_forward.argtypes = [ctypes.POINTER(came_embed), i32, vp]
+    L.came_embed_forward.restype = i32
+    L.came_embed_workspace.argtypes = [ctypes.POINTER(came_embed), ctypes.POINTER(i64)]
+    L.came_embed_workspace.restype = i32
+    L.came_embed_backward.argtypes = [ctypes.POINTER(came_embed), vp, i64, i32, vp]
+    L.came_embed_backward.restype = i32
     return L
 
 
@@ -357,6 +375,21 @@ def came_clip_destroy(ctx) -> None:
     _check(load().came_clip_destroy(ctx))
 
 
+def came_embed_forward(e: came_embed, device: int = 0, stream: int = 0) -> None:
+    _check(load().came_embed_forward(e, device, stream))
+
+
+def came_embed_workspace(e: came_embed) -> int:
+    out = ctypes.c_int64()
+    _check(load().came_embed_workspace(e, out))
+    return out.value
+
+
+def came_embed_backward(e: came_embed, workspace: int, workspace_bytes: int, device: int = 0,
+                        stream: int = 0) -> None:
+    _check(load().came_embed_backward(e, workspace, workspace_bytes, device, stream))
+
+
 def make_hparams(step: int, **kw) -> came_hparams:
     return came_hparams(float(kw["lr"]), float(kw["beta1"]), float(kw["beta2"]), float(kw["beta3"]),
                         float(kw["eps1"]), float(kw["eps2"]), float(kw["clip_d"]),
@@ -464,6 +497,80 @@ class GradClip:
             self.close()
         except Exception:
             pass
+
+
+# --- embedding lookup and its gradient -------------------------------------------------------
+
+def _matrix(x, name, device):
+    """(rows, row stride) of a CUDA matrix whose rows are contiguous."""
+    _cuda_tensor(x, name, None, device)
+    rows, cols = x.shape
+    ld, one = x.stride()
+    if one != 1 and cols > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must be contiguous")
+    return rows, max(ld, cols) if rows <= 1 else ld
+
+
+def _embed_args(table, table_name, data, data_name, ids, scale):
+    import torch
+    if table.dim() != 2:
+        raise CameError(CAME_ERR_SHAPE, f"{table_name} must be a matrix")
+    rows, table_ld = _matrix(table, table_name, table.device)
+    cols = table.shape[1]
+    _cuda_tensor(ids, "ids", None, table.device)
+    code = {torch.int32: CAME_I32, torch.int64: CAME_I64}.get(ids.dtype)
+    if code is None:
+        raise CameError(CAME_ERR_DTYPE, f"ids must be int32 or int64, got {ids.dtype}")
+    if not ids.is_contiguous():
+        raise CameError(CAME_ERR_UNSUPPORTED, "ids must be contiguous")
+    if data.shape != (*ids.shape, cols):
+        raise CameError(CAME_ERR_SHAPE, f"{data_name} must have the shape of ids and the columns of {table_name}")
+    flat = data if data.dim() == 2 else data.view(-1, cols)
+    tokens, data_ld = _matrix(flat, data_name, table.device)
+    return came_embed(table.data_ptr(), flat.data_ptr(), ids.data_ptr(), rows, cols, tokens, table_ld,
+                      data_ld, 0, scale, _dtype_code(table, table_name), _dtype_code(data, data_name),
+                      code, 0, 0)
+
+
+def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
+    """``out[t] = scale * table[ids[t]]``, zero where an id is not a row of the table.
+
+    ``table``: fp32 or bf16 CUDA matrix with contiguous rows; ``ids``: contiguous int32 or int64
+    CUDA tensor of any shape; ``out``: tensor of shape ``(*ids.shape, cols)``, fp32 or bf16, made
+    here when it is None (of type ``out_dtype``, the table's when that is None too)."""
+    import torch
+    if out is None:
+        if table.dim() != 2:
+            raise CameError(CAME_ERR_SHAPE, "table must be a matrix")
+        out = torch.empty((*ids.shape, table.shape[1]), dtype=out_dtype or table.dtype, device=table.device)
+    elif out_dtype is not None and out.dtype != out_dtype:
+        raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
+    e = _embed_args(table, "table", out, "out", ids, scale)
+    with torch.cuda.device(table.device):
+        came_embed_forward(e, table.device.index, torch.cuda.current_stream().cuda_stream)
+    return out
+
+
+def embed_backward(grad_out, ids, grad, scale: float = 1.0, padding_row: Optional[int] = None,
+                   accumulate: bool = False):
+    """``grad[v] = scale * (sum of grad_out[t] over the tokens with ids[t] == v)``; with
+    ``accumulate`` the sums are added to ``grad`` (a table tied to the output head).
+
+    ``grad_out``: fp32 or bf16, shape ``(*ids.shape, cols)``; ``grad``: fp32 or bf16 matrix, every
+    row of it written unless ``accumulate``; tokens of ``padding_row`` add nothing.  Returns
+    ``grad``.  Bit-reproducible: a row's tokens are added in an order fixed by the ids."""
+    import torch
+    e = _embed_args(grad, "grad", grad_out, "grad_out", ids, scale)
+    if accumulate:
+        e.flags |= CAME_EMBED_ACCUMULATE
+    if padding_row is not None:
+        e.flags |= CAME_EMBED_PADDING_ROW
+        e.padding_row = padding_row
+    with torch.cuda.device(grad.device):
+        ws = torch.empty(came_embed_workspace(e), dtype=torch.uint8, device=grad.device)
+        came_embed_backward(e, ws.data_ptr(), ws.numel(), grad.device.index,
+                            torch.cuda.current_stream().cuda_stream)
+    return grad
 
 
 # --- convenience wrapper -------------------------------------------------------------------

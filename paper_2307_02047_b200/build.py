@@ -5,7 +5,7 @@ import os
 import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(_HERE, "csrc", s) for s in ("came_api.cu", "ops/came_clip.cu")]
+SRCS = [os.path.join(_HERE, "csrc", s) for s in ("came_api.cu", "ops/came_clip.cu", "ops/came_embed.cu")]
 DEPS = SRCS + [os.path.join(_HERE, "csrc", h) for h in
                ("came_kernels.cuh", "came_pipelined.cuh", "came_stream.cuh", "ops/came_ops.cuh")] + \
        [os.path.join(os.path.dirname(_HERE), "include", "came_b200.h")]

@@ -47,3 +47,47 @@ def test_operators_without_gpu_report_device_error():
         with pytest.raises(binding.CameError) as e:
             binding.came_clip_create(descs)
         assert e.value.status == 7      # CAME_ERR_DEVICE: no silent CPU fallback
+
+
+def _embed(**over):
+    d = dict(table=0x10000, data=0x20000, ids=0x30000, rows=10, cols=8, tokens=4, table_ld=8, data_ld=8, padding_row=0,
+             scale=1.0, table_dtype=0, data_dtype=0, id_dtype=1, flags=0, reserved=0)
+    d.update(over)
+    return binding.came_embed(**d)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(rows=0), 2), (dict(cols=0), 2), (dict(tokens=-1), 2), (dict(rows=(1 << 31) - 1), 2), (dict(tokens=1 << 31), 2),
+    (dict(table_ld=7), 2), (dict(data_ld=7), 2), (dict(table_ld=1 << 40), 2), (dict(table_dtype=2), 3), (dict(data_dtype=-1), 3),
+    (dict(id_dtype=2), 3), (dict(flags=8), 11), (dict(reserved=1), 2), (dict(scale=float("nan")), 5), (dict(table=None), 1),
+    (dict(data=None), 1), (dict(ids=None), 1), (dict(table=0x10002), 4), (dict(data=0x20001), 4), (dict(ids=0x30004), 4),
+    (dict(data=0x10010), 12),
+])
+def test_embed_refuses_before_any_cuda_call(over, status):
+    for call in (binding.came_embed_workspace, lambda e: binding.came_embed_forward(e), lambda e: binding.came_embed_backward(e, 0x40000, 1 << 20)):
+        with pytest.raises(binding.CameError) as e:
+            call(_embed(**over))
+        assert e.value.status == status and binding.came_last_error(None) != ""
+
+
+def test_embed_workspace_and_flags():
+    L = binding.load()
+    assert L.came_embed_workspace(_embed(), None) == 1 and L.came_embed_forward(None, 0, None) == 1
+    small, large = binding.came_embed_workspace(_embed(tokens=0, data=None, ids=None)), binding.came_embed_workspace(_embed(tokens=1000, data=0x100000))
+    assert 0 < small < large
+    with pytest.raises(binding.CameError) as e:
+        binding.came_embed_forward(_embed(flags=1))          # the flags belong to the gradient
+    assert e.value.status == 11
+    with pytest.raises(binding.CameError) as e:
+        binding.came_embed_forward(_embed(data=0x2FFF0))     # the output runs into the ids
+    assert e.value.status == 12
+
+
+def test_embed_without_gpu_reports_device_error():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    for call in (lambda e: binding.came_embed_forward(e), lambda e: binding.came_embed_backward(e, 0x40000, 1 << 20)):
+        with pytest.raises(binding.CameError) as e:
+            call(_embed())
+        assert e.value.status == 7
