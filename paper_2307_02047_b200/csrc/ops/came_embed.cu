@@ -22,43 +22,38 @@ using namespace came_ops;
 
 constexpr int kSlice = 256;              // columns one warp works on: 8 per lane
 
-// EV consecutive elements as fp32, one access of EV * sizeof(T) bytes.
+// EV consecutive elements as they are stored: one access of EV * sizeof(T) bytes.
 template <int EV, typename T>
-__device__ __forceinline__ void load_ev(const T* p, float* x)
-{
-    constexpr int B = EV * static_cast<int>(sizeof(T));
-    if constexpr (B == 32) {
-        uint32_t w[8];
-        asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]),
-                       "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(w[j]);
-    } else if constexpr (B >= 4) {
-        constexpr int W = B / 4;
-        uint32_t w[W];
-        if constexpr (W == 4) {
+struct Raw {
+    static constexpr int B = EV * static_cast<int>(sizeof(T));
+    static constexpr int W = B < 4 ? 1 : B / 4;
+    uint32_t w[W];
+
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (B == 32) {
+            asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]),
+                           "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+        } else if constexpr (B == 16) {
             const uint4 v = *reinterpret_cast<const uint4*>(p);
             w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-        } else if constexpr (W == 2) {
+        } else if constexpr (B == 8) {
             const uint2 v = *reinterpret_cast<const uint2*>(p);
             w[0] = v.x; w[1] = v.y;
-        } else {
+        } else if constexpr (B == 4) {
             w[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            w[0] = *reinterpret_cast<const uint16_t*>(p);
         }
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            if constexpr (sizeof(T) == 4) {
-                x[j] = __uint_as_float(w[j]);
-            } else {
-                x[2 * j] = __uint_as_float(w[j] << 16);
-                x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-            }
-        }
-    } else {
-        x[0] = to_float(*p);
     }
-}
+
+    __device__ __forceinline__ float value(int k) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[k]);
+        else return __uint_as_float(k & 1 ? w[k >> 1] & 0xffff0000u : w[k >> 1] << 16);
+    }
+};
 
 template <int EV, typename T>
 __device__ __forceinline__ void store_ev(T* p, const float* x)
@@ -110,13 +105,13 @@ k_embed_forward(const T* __restrict__ table, long long rows, long long cols, lon
     const bool hit = id >= 0 && id < rows;
     const T* const src = table + (hit ? id : 0) * table_ld;
     O* const dst = out + t * out_ld;
-    float x[kFwdSlices][8];
+    Raw<EV, T> x[kFwdSlices][8 / EV];
 #pragma unroll
     for (int s = 0; s < kFwdSlices; ++s)
 #pragma unroll
         for (int g = 0; g < 8 / EV; ++g) {
             const long long c = column<EV>(s0 + s, g, lane);
-            if (hit && c < cols) load_ev<EV, T>(src + c, x[s] + g * EV);
+            if (hit && c < cols) x[s][g].load(src + c);
         }
 #pragma unroll
     for (int s = 0; s < kFwdSlices; ++s)
@@ -126,7 +121,7 @@ k_embed_forward(const T* __restrict__ table, long long rows, long long cols, lon
             if (c < cols) {
                 float y[EV];
 #pragma unroll
-                for (int k = 0; k < EV; ++k) y[k] = hit ? x[s][g * EV + k] * scale : 0.f;
+                for (int k = 0; k < EV; ++k) y[k] = hit ? x[s][g].value(k) * scale : 0.f;
                 store_ev<EV, O>(dst + c, y);
             }
         }
@@ -148,9 +143,11 @@ constexpr size_t kSortSmem = sizeof(unsigned) * kSortWarps * kMaxBins;
 struct SortArgs {
     unsigned* key[2];        // ping-pong buffers [tokens]
     unsigned* token[2];
-    unsigned* row_start;     // [rows] first and last + 1 sorted position of a row's tokens
+    unsigned* row_start;     // [rows] first and last + 1 sorted position of a row's tokens; set
+                             // for rows that have some
     unsigned* row_end;
-    long long tokens;
+    unsigned* arrived;       // [n_arrived] counters of the sums' grid, cleared here
+    long long tokens, n_arrived;
     unsigned  rows, padding; // padding: its own row, or rows when there is none
     int       digit_bits, passes;
 };
@@ -182,6 +179,10 @@ k_embed_sort(const I* __restrict__ ids, SortArgs a)
     const int blocks = static_cast<int>(cluster.num_blocks()), me = static_cast<int>(cluster.block_rank());
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int bins = 1 << a.digit_bits;
+    release_dependents();
+    for (long long k = static_cast<long long>(me) * kSortThreads + tid; k < a.n_arrived;
+         k += static_cast<long long>(blocks) * kSortThreads)
+        a.arrived[k] = 0u;
     const long long runs = static_cast<long long>(blocks) * kSortWarps;
     const long long per = ((a.tokens + runs - 1) / runs + 31) / 32 * 32;
     const long long begin = min(a.tokens, (static_cast<long long>(me) * kSortWarps + warp) * per);
@@ -254,54 +255,226 @@ k_embed_sort(const I* __restrict__ ids, SortArgs a)
     }
 }
 
-// ---- backward: the rows' sums ------------------------------------------------------------------
+// ---- backward: rows without tokens ---------------------------------------------------------------
+// Runs beside the sort (it needs the ids only): block c owns the rows r = c mod gridDim.x (a
+// power of two, so that frequent ids, which are neighbours in most vocabularies, spread over the
+// blocks), marks those that have tokens in a bit map of its own and writes zeros to the others.
+constexpr int kZeroThreads = 512;
+constexpr int kZeroWords = 4096;         // bits of rows per round: 131072
 
-template <typename T, typename O, int EV>
-__global__ void __launch_bounds__(256)
-k_embed_rows(const T* __restrict__ dy, long long dy_ld, const unsigned* __restrict__ token,
-             const unsigned* __restrict__ row_start, const unsigned* __restrict__ row_end,
-             long long rows, long long cols, float scale, O* __restrict__ grad, long long grad_ld,
-             int slices, int accumulate)
+template <typename I, typename O, int EV>
+__global__ void __launch_bounds__(kZeroThreads)
+k_embed_zero(const I* __restrict__ ids, long long tokens, unsigned rows, unsigned padding, long long cols,
+             O* __restrict__ grad, long long grad_ld, int log2_blocks)
 {
-    constexpr int U = 4;
-    const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const long long v = item / slices;
-    if (v >= rows) return;
-    const long long slice = item - v * slices;
-    const int lane = threadIdx.x & 31;
-    const unsigned begin = row_start[v], end = row_end[v];
-    if (accumulate && begin == end) return;
-    float acc[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    for (unsigned k = begin; k < end; k += U) {
-        float x[U][8];
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int g = 0; g < 8 / EV; ++g) {
-                const long long c = column<EV>(slice, g, lane);
-                if (k + u < end && c < cols)
-                    load_ev<EV, T>(dy + static_cast<long long>(token[k + u]) * dy_ld + c, x[u] + g * EV);
-            }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (k + u < end)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += x[u][j];
+    __shared__ unsigned seen[kZeroWords];
+    release_dependents();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned own = blockIdx.x, mask = (1u << log2_blocks) - 1u;
+    const unsigned owned = own < rows ? ((rows - 1u - own) >> log2_blocks) + 1u : 0u;      // rows of this block
+    const float zeros[EV] = {};
+    for (unsigned first = 0; first < owned; first += kZeroWords * 32u) {
+        const unsigned count = min(owned - first, kZeroWords * 32u);
+        for (unsigned k = tid; k < (count + 31u) / 32u; k += kZeroThreads) seen[k] = 0u;
+        __syncthreads();
+#pragma unroll 4
+        for (long long t = tid; t < tokens; t += kZeroThreads) {
+            const long long id = static_cast<long long>(ids[t]);
+            if (id < 0 || id >= rows || (static_cast<unsigned>(id) & mask) != own || id == padding) continue;
+            const unsigned bit = (static_cast<unsigned>(id) >> log2_blocks) - first;
+            if (bit < count && !(seen[bit >> 5] >> (bit & 31u) & 1u)) atomicOr(&seen[bit >> 5], 1u << (bit & 31u));
+        }
+        __syncthreads();
+        for (unsigned k = warp; k < count; k += kZeroThreads / 32) {
+            if (seen[k >> 5] >> (k & 31u) & 1u) continue;
+            O* const dst = grad + (static_cast<long long>(first + k) * (mask + 1u) + own) * grad_ld;
+            for (long long c = static_cast<long long>(lane) * EV; c < cols; c += 32 * EV) store_ev<EV, O>(dst + c, zeros);
+        }
+        __syncthreads();
     }
-    O* const dst = grad + v * grad_ld;
+    // the sums' grid waits for this one; by waiting for the sort here it waits for both
+    wait_for_previous_grid();
+}
+
+// ---- backward: the sums ----------------------------------------------------------------------------
+// A block takes 8 * per_warp consecutive sorted tokens and one slice of the columns, a warp
+// per_warp of them: however many tokens a row has, the work is even.  A run of equal keys that
+// begins and ends within a warp is stored at once.  A part of a run that crosses warps goes
+// through shared memory to the warp in which the run ends; one that crosses blocks goes to
+// the workspace, and the block that arrives last for that run adds the parts in order.
+constexpr int kSumWarps = 8;
+enum : int { kLinkHead = 1, kLinkTail = 2, kLinkThrough = 4 };
+
+struct SumArgs {
+    const unsigned* key;       // sorted [tokens]
+    const unsigned* token;
+    const unsigned* row_start;
+    const unsigned* row_end;
+    float*    part;            // [blocks of tokens][2][slices][kSlice]: 0 = run from before, 1 = run that goes on
+    unsigned* arrived;         // [blocks of tokens][slices]
+    long long tokens, cols, dy_ld, grad_ld;
+    unsigned  rows;
+    int       slices, per_warp, accumulate;
+    float     scale;
+};
+
+template <typename O, int EV>
+__device__ __forceinline__ void store_row(const SumArgs& a, O* grad, unsigned row, int slice, int lane, const float (&sum)[8])
+{
+    O* const dst = grad + static_cast<long long>(row) * a.grad_ld;
 #pragma unroll
     for (int g = 0; g < 8 / EV; ++g) {
         const long long c = column<EV>(slice, g, lane);
-        if (c >= cols) continue;
+        if (c >= a.cols) continue;
         float y[EV];
+        if (a.accumulate) {
+            Raw<EV, O> old;
+            old.load(dst + c);
 #pragma unroll
-        for (int k = 0; k < EV; ++k) y[k] = 0.f;
-        if (accumulate) load_ev<EV, O>(dst + c, y);
+            for (int k = 0; k < EV; ++k) y[k] = fmaf(a.scale, sum[g * EV + k], old.value(k));
+        } else {
 #pragma unroll
-        for (int k = 0; k < EV; ++k) y[k] = fmaf(scale, acc[g * EV + k], y[k]);
+            for (int k = 0; k < EV; ++k) y[k] = a.scale * sum[g * EV + k];
+        }
         store_ev<EV, O>(dst + c, y);
+    }
+}
+
+// One block's part of a run that crosses blocks.  The last of the run's blocks to arrive adds
+// all parts in the order of the tokens and stores the row.
+template <typename O, int EV>
+__device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned row, unsigned block, int slot, int slice,
+                                            int lane, const float (&sum)[8])
+{
+    const unsigned size = static_cast<unsigned>(kSumWarps * a.per_warp);
+    const unsigned first = __ldcg(a.row_start + row) / size, last = (__ldcg(a.row_end + row) - 1u) / size;
+    auto at = [&](unsigned b, int s) {
+        return a.part + ((static_cast<long long>(b) * 2 + s) * a.slices + slice) * kSlice + lane; };
+    float* const mine = at(block, slot);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) __stcg(mine + j * 32, sum[j]);
+    __threadfence();
+    __syncwarp();
+    unsigned final = 0;
+    if (lane == 0)
+        final = atomicAdd(&a.arrived[static_cast<long long>(first) * a.slices + slice], 1u) == last - first;
+    if (!__shfl_sync(0xffffffffu, final, 0)) return;
+    __threadfence();
+    float total[8];
+    {
+        const float* const p = at(first, 1);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) total[j] = __ldcg(p + j * 32);
+    }
+    for (unsigned b = first + 1; b <= last; b += 4) {
+        float x[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float* const p = at(b + u, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[u][j] = b + u <= last ? __ldcg(p + j * 32) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) total[j] += x[u][j];
+    }
+    store_row<O, EV>(a, grad, row, slice, lane, total);
+}
+
+template <typename T, typename O, int EV>
+__global__ void __launch_bounds__(kSumWarps * 32)
+k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
+{
+    constexpr int U = sizeof(T) == 2 ? 8 : 4;            // rows in flight: 8 * 16 or 4 * 32 bytes per lane
+    __shared__ float part[kSumWarps][2][8][32];          // [warp][head, tail][element][lane]
+    __shared__ int link[kSumWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const unsigned block = blockIdx.x / static_cast<unsigned>(a.slices);
+    const int slice = static_cast<int>(blockIdx.x - block * static_cast<unsigned>(a.slices));
+    const int K = a.per_warp;
+    const long long p0 = (static_cast<long long>(block) * kSumWarps + warp) * K;
+    wait_for_previous_grid();
+
+    const long long p = p0 + lane;
+    const bool in = lane < K && p < a.tokens;
+    const unsigned key = in ? __ldcg(a.key + p) : a.rows;
+    const unsigned token = in ? __ldcg(a.token + p) : 0u;
+    const int n = __popc(__ballot_sync(0xffffffffu, key < a.rows));          // keys that are rows come first
+    const unsigned key_first = __shfl_sync(0xffffffffu, key, 0);
+    const unsigned key_last = __shfl_sync(0xffffffffu, key, K - 1);
+    const bool head = n > 0 && p0 > 0 && __ldcg(a.key + p0 - 1) == key_first;
+    const bool tail = n == K && p0 + K < a.tokens && __ldcg(a.key + p0 + K) == key_last;
+    const bool through = head && tail && key_first == key_last;
+    if (lane == 0) link[warp] = (head ? kLinkHead : 0) | (tail ? kLinkTail : 0) | (through ? kLinkThrough : 0);
+
+    float acc[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+    auto keep = [&](int which) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) part[warp][which][j][lane] = acc[j];
+    };
+    unsigned current = key_first;
+    bool open_head = head;                               // the run being added began in an earlier warp
+    for (int k = 0; k < n; k += U) {
+        Raw<EV, T> x[U][8 / EV];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const unsigned t = __shfl_sync(0xffffffffu, token, (k + u) & 31);
+#pragma unroll
+            for (int g = 0; g < 8 / EV; ++g) {
+                const long long c = column<EV>(slice, g, lane);
+                if (k + u < n && c < a.cols) x[u][g].load(dy + static_cast<long long>(t) * a.dy_ld + c);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const unsigned v = __shfl_sync(0xffffffffu, key, (k + u) & 31);
+            if (k + u < n) {
+                if (v != current) {
+                    if (open_head) keep(0);
+                    else store_row<O, EV>(a, grad, current, slice, lane, acc);
+                    open_head = false;
+                    current = v;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += x[u][j / EV].value(j % EV);
+            }
+        }
+    }
+    if (n > 0) {
+        if (open_head) keep(0);                          // ends here, or goes through
+        else if (tail) keep(1);
+        else store_row<O, EV>(a, grad, current, slice, lane, acc);
+    }
+    __syncthreads();
+
+    // parts of runs that cross warps: added by the warp in which the run ends, or by the last one
+    auto gather = [&](int which_end) -> int {            // acc = the run's parts up to this warp; its first warp or -1
+        int w = warp - 1;
+        if (which_end == 1) {
+            w = warp;                                    // the run begins in this warp
+        } else {
+            while (w >= 0 && (link[w] & kLinkThrough)) --w;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j] = w >= 0 ? part[w][1][j][lane] : 0.f;
+        if (which_end == 0)
+            for (int q = max(w + 1, 0); q <= warp; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[j] += part[q][0][j][lane];
+        return w;
+    };
+    if (head && !through) {
+        if (gather(0) >= 0) store_row<O, EV>(a, grad, key_first, slice, lane, acc);
+        else join_blocks<O, EV>(a, grad, key_first, block, 0, slice, lane, acc);
+    }
+    if (warp == kSumWarps - 1 && tail) {
+        const int w = gather(through ? 0 : 1);
+        join_blocks<O, EV>(a, grad, key_last, block, w >= 0 ? 1 : 0, slice, lane, acc);
     }
 }
 
@@ -309,8 +482,18 @@ k_embed_rows(const T* __restrict__ dy, long long dy_ld, const unsigned* __restri
 
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
+// Sorted tokens per warp of the sums' grid: enough to cover the latency of a row's load, few
+// enough that there are several thousand warps.  Fixed by the sizes alone, as the order of the sums is.
+int tokens_per_warp(const came_embed& e)
+{
+    const long long work = e.tokens * ceil_div(e.cols, kSlice);
+    return work >= 32 * 8192 ? 32 : work >= 16 * 8192 ? 16 : 8;
+}
+
 struct Layout {
-    size_t key[2], token[2], row_start, row_end, bytes;
+    size_t key[2], token[2], row_start, row_end, part, arrived, bytes;
+    long long blocks, slices;            // of the sums' grid
+    int per_warp;
 };
 
 Layout layout(const came_embed& e)
@@ -318,10 +501,15 @@ Layout layout(const came_embed& e)
     Layout l;
     size_t at = 0;
     auto take = [&](size_t b) { const size_t p = at; at += (b + 255) / 256 * 256; return p; };
+    l.per_warp = tokens_per_warp(e);
+    l.blocks = ceil_div(e.tokens, kSumWarps * l.per_warp);
+    l.slices = ceil_div(e.cols, kSlice);
     for (int k = 0; k < 2; ++k) l.key[k] = take(sizeof(unsigned) * e.tokens);
     for (int k = 0; k < 2; ++k) l.token[k] = take(sizeof(unsigned) * e.tokens);
     l.row_start = take(sizeof(unsigned) * e.rows);
     l.row_end = take(sizeof(unsigned) * e.rows);
+    l.part = take(sizeof(float) * 2 * kSlice * l.blocks * l.slices);
+    l.arrived = take(sizeof(unsigned) * l.blocks * l.slices);
     l.bytes = at;
     return l;
 }
@@ -405,26 +593,21 @@ void launch_forward_types(const came_embed& e, cudaStream_t stream)
     }
 }
 
-template <typename T, typename O, int EV>
-void launch_rows(const came_embed& e, const SortArgs& a, cudaStream_t stream)
+// Launched with programmatic stream serialisation: the kernel waits for the grid before it itself.
+// (early = false: an ordinary launch.)
+template <typename K, typename... A>
+cudaError_t launch_dependent(K kernel, bool early, long long blocks, int threads, cudaStream_t stream, A... args)
 {
-    const int slices = static_cast<int>(ceil_div(e.cols, kSlice));
-    const long long items = e.rows * slices;
-    k_embed_rows<T, O, EV><<<static_cast<unsigned>(ceil_div(items, 8)), 256, 0, stream>>>(
-        static_cast<const T*>(e.data), e.data_ld, a.token[(a.passes + 1) & 1], a.row_start, a.row_end, e.rows, e.cols,
-        static_cast<float>(e.scale), static_cast<O*>(e.table), e.table_ld, slices,
-        (e.flags & CAME_EMBED_ACCUMULATE) ? 1 : 0);
-}
-
-template <typename T, typename O>
-void launch_rows_ev(const came_embed& e, const SortArgs& a, cudaStream_t stream)
-{
-    switch (elements_per_access(e)) {
-        case 8:  launch_rows<T, O, 8>(e, a, stream); break;
-        case 4:  launch_rows<T, O, 4>(e, a, stream); break;
-        case 2:  launch_rows<T, O, 2>(e, a, stream); break;
-        default: launch_rows<T, O, 1>(e, a, stream); break;
-    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 template <typename I>
@@ -447,6 +630,42 @@ cudaError_t launch_sort(const came_embed& e, const SortArgs& a, cudaStream_t str
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, k_embed_sort<I>, static_cast<const I*>(e.ids), a);
+}
+
+template <typename I, typename O, int EV>
+cudaError_t launch_zero(const came_embed& e, unsigned padding, cudaStream_t stream)
+{
+    int lg = 0;
+    while (lg < 8 && (2ll << lg) <= e.rows) ++lg;        // at most 256 blocks, two per SM
+    // it may start while the sort runs, but only behind a sort: the sort has waited for everything
+    // before it, and only then may rows be written
+    return launch_dependent(k_embed_zero<I, O, EV>, e.tokens > 0, 1ll << lg, kZeroThreads, stream, static_cast<const I*>(e.ids),
+                            static_cast<long long>(e.tokens), static_cast<unsigned>(e.rows), padding,
+                            static_cast<long long>(e.cols), static_cast<O*>(e.table),
+                            static_cast<long long>(e.table_ld), lg);
+}
+
+template <typename T, typename O, int EV>
+cudaError_t launch_sums(const came_embed& e, const SumArgs& s, unsigned padding, long long blocks, cudaStream_t stream)
+{
+    cudaError_t err = cudaSuccess;
+    if (!s.accumulate)
+        err = e.id_dtype == CAME_I64 ? launch_zero<long long, O, EV>(e, padding, stream) : launch_zero<int, O, EV>(e, padding, stream);
+    if (err == cudaSuccess && blocks > 0)
+        err = launch_dependent(k_embed_sum<T, O, EV>, true, blocks, kSumWarps * 32, stream, static_cast<const T*>(e.data),
+                               static_cast<O*>(e.table), s);
+    return err;
+}
+
+template <typename T, typename O>
+cudaError_t launch_sums_ev(const came_embed& e, const SumArgs& s, unsigned padding, long long blocks, cudaStream_t stream)
+{
+    switch (elements_per_access(e)) {
+        case 8:  return launch_sums<T, O, 8>(e, s, padding, blocks, stream);
+        case 4:  return launch_sums<T, O, 4>(e, s, padding, blocks, stream);
+        case 2:  return launch_sums<T, O, 2>(e, s, padding, blocks, stream);
+        default: return launch_sums<T, O, 1>(e, s, padding, blocks, stream);
+    }
 }
 
 }  // namespace
@@ -493,16 +712,18 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
         return report(CAME_ERR_SHAPE, "workspace smaller than came_embed_workspace says");
     if ((s = require_current_device(device)) != CAME_OK) return s;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (e->rows * ceil_div(e->cols, kSlice) > (1ll << 33))
-        return report(CAME_ERR_SHAPE, "too many rows times columns for one launch");
+    if (l.blocks * l.slices >= (1ll << 31)) return report(CAME_ERR_SHAPE, "too many tokens times columns for one launch");
     char* const w = static_cast<char*>(workspace);
+    auto at = [&](size_t offset) { return reinterpret_cast<unsigned*>(w + offset); };
     SortArgs a = {};
     for (int k = 0; k < 2; ++k) {
-        a.key[k] = reinterpret_cast<unsigned*>(w + l.key[k]);
-        a.token[k] = reinterpret_cast<unsigned*>(w + l.token[k]);
+        a.key[k] = at(l.key[k]);
+        a.token[k] = at(l.token[k]);
     }
-    a.row_start = reinterpret_cast<unsigned*>(w + l.row_start);
-    a.row_end = reinterpret_cast<unsigned*>(w + l.row_end);
+    a.row_start = at(l.row_start);
+    a.row_end = at(l.row_end);
+    a.arrived = at(l.arrived);
+    a.n_arrived = l.blocks * l.slices;
     a.tokens = e->tokens;
     a.rows = static_cast<unsigned>(e->rows);
     a.padding = padding ? static_cast<unsigned>(e->padding_row) : a.rows;
@@ -510,21 +731,35 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     while ((e->rows >> bits) != 0) ++bits;                // the keys are 0 .. rows
     a.passes = static_cast<int>(ceil_div(bits, kMaxDigitBits));
     a.digit_bits = static_cast<int>(ceil_div(bits, a.passes));
-    cudaError_t err = cudaMemsetAsync(a.row_start, 0, l.bytes - l.row_start, stream);
-    if (err != cudaSuccess) return report_cuda(err, "cudaMemsetAsync(row table)");
-    if (e->tokens > 0) {
+    SumArgs t = {};
+    t.key = a.key[(a.passes + 1) & 1];
+    t.token = a.token[(a.passes + 1) & 1];
+    t.row_start = a.row_start;
+    t.row_end = a.row_end;
+    t.part = reinterpret_cast<float*>(w + l.part);
+    t.arrived = a.arrived;
+    t.tokens = e->tokens;
+    t.cols = e->cols;
+    t.dy_ld = e->data_ld;
+    t.grad_ld = e->table_ld;
+    t.rows = a.rows;
+    t.slices = static_cast<int>(l.slices);
+    t.per_warp = l.per_warp;
+    t.accumulate = (e->flags & CAME_EMBED_ACCUMULATE) ? 1 : 0;
+    t.scale = static_cast<float>(e->scale);
+    cudaError_t err = cudaSuccess;
+    if (e->tokens > 0)
         err = e->id_dtype == CAME_I64 ? launch_sort<long long>(*e, a, stream) : launch_sort<int>(*e, a, stream);
-        if (err != cudaSuccess) return report_cuda(err, "kernel launch(sort)");
-    }
+    if (err != cudaSuccess) return report_cuda(err, "kernel launch(sort)");
     using bf16 = __nv_bfloat16;
-    if (e->data_dtype == CAME_BF16) {
-        if (e->table_dtype == CAME_BF16) launch_rows_ev<bf16, bf16>(*e, a, stream);
-        else                             launch_rows_ev<bf16, float>(*e, a, stream);
-    } else {
-        if (e->table_dtype == CAME_BF16) launch_rows_ev<float, bf16>(*e, a, stream);
-        else                             launch_rows_ev<float, float>(*e, a, stream);
-    }
-    err = cudaGetLastError();
+    const long long blocks = l.blocks * l.slices;
+    if (e->data_dtype == CAME_BF16)
+        err = e->table_dtype == CAME_BF16 ? launch_sums_ev<bf16, bf16>(*e, t, a.padding, blocks, stream)
+                                          : launch_sums_ev<bf16, float>(*e, t, a.padding, blocks, stream);
+    else
+        err = e->table_dtype == CAME_BF16 ? launch_sums_ev<float, bf16>(*e, t, a.padding, blocks, stream)
+                                          : launch_sums_ev<float, float>(*e, t, a.padding, blocks, stream);
+    if (err == cudaSuccess) err = cudaGetLastError();
     return err == cudaSuccess ? CAME_OK : report_cuda(err, "kernel launch");
 }
 
