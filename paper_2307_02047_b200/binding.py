@@ -397,6 +397,39 @@ def make_hparams(step: int, **kw) -> came_hparams:
                         float(kw.get("grad_scale", 1.0)))
 
 
+# --- what the operators' wrappers share ------------------------------------------------------
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
+class _on:
+    """``with _on(device) as stream:`` makes ``device`` current for the block (nothing to do when it
+    is already) and gives the address of its current stream."""
+    __slots__ = ("index", "before")
+
+    def __init__(self, device):
+        self.index = device.index
+
+    def __enter__(self):
+        cuda = _torch().cuda
+        self.before = cuda.current_device()
+        if self.before != self.index:
+            cuda.set_device(self.index)
+        return cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            _torch().cuda.set_device(self.before)
+
+
 # --- gradient norm and clipping ------------------------------------------------------------
 
 def _cuda_tensor(x, name, dtype=None, device=None) -> None:
@@ -406,9 +439,13 @@ def _cuda_tensor(x, name, dtype=None, device=None) -> None:
         raise CameError(CAME_ERR_DTYPE, f"{name} must be {dtype}, got {x.dtype}")
 
 
+_DTYPE_CODES = {}       # torch dtype -> came_dtype
+
+
 def _dtype_code(x, name) -> int:
-    import torch
-    code = {torch.float32: CAME_F32, torch.bfloat16: CAME_BF16}.get(x.dtype)
+    if not _DTYPE_CODES:
+        _DTYPE_CODES.update({_torch().float32: CAME_F32, _torch().bfloat16: CAME_BF16})
+    code = _DTYPE_CODES.get(x.dtype)
     if code is None:
         raise CameError(CAME_ERR_DTYPE, f"{name} must be fp32 or bf16, got {x.dtype}")
     return code
@@ -448,9 +485,8 @@ class GradClip:
         self.results = torch.zeros(2 + len(descs), dtype=torch.float32, device=self.device)
         self.total_norm, self.coef, self.tensor_norms = self.results[0], self.results[1], self.results[2:]
         self._results_at = self.results.data_ptr()
-        self._stream = torch.cuda.current_stream
         self._params = came_clip_params()
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             self.ctx = came_clip_create(descs, self.device.index)
 
     def _check_tensor(self, x, name):
@@ -471,7 +507,8 @@ class GradClip:
             at = [g.data_ptr() for g in grads]
         p = self._params
         p.max_norm, p.eps, p.grad_scale = max_norm, eps, grad_scale
-        call(self.ctx, p, self._results_at, at, self._stream(self.device).cuda_stream)
+        with _on(self.device) as stream:
+            call(self.ctx, p, self._results_at, at, stream)
         if grads is not None:
             self.grads = grads
         return self.total_norm, self.coef, self.tensor_norms
@@ -501,35 +538,43 @@ class GradClip:
 
 # --- embedding lookup and its gradient -------------------------------------------------------
 
-def _matrix(x, name, device):
-    """(rows, row stride) of a CUDA matrix whose rows are contiguous."""
-    _cuda_tensor(x, name, None, device)
-    rows, cols = x.shape
-    ld, one = x.stride()
-    if one != 1 and cols > 1:
-        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must be contiguous")
-    return rows, max(ld, cols) if rows <= 1 else ld
+_ID_CODES = {}          # torch dtype -> came_id_dtype, filled on first use (torch is imported late)
 
 
 def _embed_args(table, table_name, data, data_name, ids, scale):
-    import torch
+    """The descriptor of a call, and the device; every refusal that needs the tensors is here."""
     if table.dim() != 2:
         raise CameError(CAME_ERR_SHAPE, f"{table_name} must be a matrix")
-    rows, table_ld = _matrix(table, table_name, table.device)
-    cols = table.shape[1]
-    _cuda_tensor(ids, "ids", None, table.device)
-    code = {torch.int32: CAME_I32, torch.int64: CAME_I64}.get(ids.dtype)
+    rows, cols = table.shape
+    table_ld, one = table.stride()
+    if one != 1 and cols > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {table_name} must be contiguous")
+    device = table.device
+    _cuda_tensor(table, table_name)
+    _cuda_tensor(ids, "ids", None, device)
+    _cuda_tensor(data, data_name, None, device)
+    if not _ID_CODES:
+        _ID_CODES.update({_torch().int32: CAME_I32, _torch().int64: CAME_I64})
+    code = _ID_CODES.get(ids.dtype)
     if code is None:
         raise CameError(CAME_ERR_DTYPE, f"ids must be int32 or int64, got {ids.dtype}")
     if not ids.is_contiguous():
         raise CameError(CAME_ERR_UNSUPPORTED, "ids must be contiguous")
     if data.shape != (*ids.shape, cols):
         raise CameError(CAME_ERR_SHAPE, f"{data_name} must have the shape of ids and the columns of {table_name}")
-    flat = data if data.dim() == 2 else data.view(-1, cols)
-    tokens, data_ld = _matrix(flat, data_name, table.device)
-    return came_embed(table.data_ptr(), flat.data_ptr(), ids.data_ptr(), rows, cols, tokens, table_ld,
+    if data.dim() != 2:
+        data = data.view(-1, cols)
+    data_ld, one = data.stride()
+    if one != 1 and cols > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {data_name} must be contiguous")
+    tokens = data.shape[0]
+    if rows == 1:                       # the stride of a single row says nothing
+        table_ld = cols
+    if tokens <= 1:
+        data_ld = cols
+    return came_embed(table.data_ptr(), data.data_ptr(), ids.data_ptr(), rows, cols, tokens, table_ld,
                       data_ld, 0, scale, _dtype_code(table, table_name), _dtype_code(data, data_name),
-                      code, 0, 0)
+                      code, 0, 0), device
 
 
 def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
@@ -538,16 +583,15 @@ def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
     ``table``: fp32 or bf16 CUDA matrix with contiguous rows; ``ids``: contiguous int32 or int64
     CUDA tensor of any shape; ``out``: tensor of shape ``(*ids.shape, cols)``, fp32 or bf16, made
     here when it is None (of type ``out_dtype``, the table's when that is None too)."""
-    import torch
     if out is None:
         if table.dim() != 2:
             raise CameError(CAME_ERR_SHAPE, "table must be a matrix")
-        out = torch.empty((*ids.shape, table.shape[1]), dtype=out_dtype or table.dtype, device=table.device)
+        out = table.new_empty((*ids.shape, table.shape[1]), dtype=out_dtype)
     elif out_dtype is not None and out.dtype != out_dtype:
         raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
-    e = _embed_args(table, "table", out, "out", ids, scale)
-    with torch.cuda.device(table.device):
-        came_embed_forward(e, table.device.index, torch.cuda.current_stream().cuda_stream)
+    e, device = _embed_args(table, "table", out, "out", ids, scale)
+    with _on(device) as stream:
+        came_embed_forward(e, device.index, stream)
     return out
 
 
@@ -559,17 +603,17 @@ def embed_backward(grad_out, ids, grad, scale: float = 1.0, padding_row: Optiona
     ``grad_out``: fp32 or bf16, shape ``(*ids.shape, cols)``; ``grad``: fp32 or bf16 matrix, every
     row of it written unless ``accumulate``; tokens of ``padding_row`` add nothing.  Returns
     ``grad``.  Bit-reproducible: a row's tokens are added in an order fixed by the ids."""
-    import torch
-    e = _embed_args(grad, "grad", grad_out, "grad_out", ids, scale)
+    e, device = _embed_args(grad, "grad", grad_out, "grad_out", ids, scale)
     if accumulate:
         e.flags |= CAME_EMBED_ACCUMULATE
     if padding_row is not None:
         e.flags |= CAME_EMBED_PADDING_ROW
         e.padding_row = padding_row
-    with torch.cuda.device(grad.device):
-        ws = torch.empty(came_embed_workspace(e), dtype=torch.uint8, device=grad.device)
-        came_embed_backward(e, ws.data_ptr(), ws.numel(), grad.device.index,
-                            torch.cuda.current_stream().cuda_stream)
+    with _on(device) as stream:
+        size = came_embed_workspace(e)
+        # from torch's allocator, on the stream of the call: kept from reuse until the call is done
+        ws = grad_out.new_empty(-(-size // 4), dtype=_torch().float32)
+        came_embed_backward(e, ws.data_ptr(), size, device.index, stream)
     return grad
 
 

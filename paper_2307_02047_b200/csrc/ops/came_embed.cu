@@ -8,13 +8,9 @@
 // bit-reproducible.
 #include "came_ops.cuh"
 
-#include <cooperative_groups.h>
-
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
-
-namespace cg = cooperative_groups;
 
 namespace {
 
@@ -128,172 +124,285 @@ k_embed_forward(const T* __restrict__ table, long long rows, long long cols, lon
 }
 
 // ---- backward: stable sort of the tokens by row ----------------------------------------------
-// One cluster of blocks, least significant digit first.  A warp owns a contiguous run of the
-// input; per digit it knows how many equal digits come before its run (in its block: a count per
-// warp and digit; in the cluster: the blocks' totals, read through distributed shared memory;
-// over all digits: a scan), so every element's place is known and nothing is added by atomics
-// whose order matters.  Ids that are not rows (and the padding row) get the key `rows` and end
-// up behind all others.
+// Least significant digit first.  A warp owns a contiguous run of the input; per digit it knows how
+// many equal digits come before its run (in its block: a count per warp and digit; in the grid:
+// the blocks' counts; over all digits: a scan), so every element's place is known and nothing
+// depends on the order in which atomics arrive.  Ids that are not rows (and the padding row) get the
+// key `rows` and end up behind all others.
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMaxDigitBits = 9;
 constexpr int kMaxBins = 1 << kMaxDigitBits;
-constexpr size_t kSortSmem = sizeof(unsigned) * kSortWarps * kMaxBins;
+constexpr int kMaxPasses = 4;            // keys below 2^31 in digits of 8 bits
+constexpr int kFewTokens = 512;          // up to here every token counts the tokens before it
+constexpr unsigned kFewRows = 1u << 22;  // (key and position then fit one word)
+constexpr int kOneTokens = 4096;         // up to here one block sorts in its shared memory
+constexpr int kSortBlocks = 148;         // beyond that one block per SM at most
+constexpr size_t kHistBytes = sizeof(unsigned) * kSortWarps * kMaxBins;
+constexpr size_t kOneBytes = kHistBytes + sizeof(uint2) * kOneTokens;
 
 struct SortArgs {
-    unsigned* key[2];        // ping-pong buffers [tokens]
-    unsigned* token[2];
-    unsigned* row_start;     // [rows] first and last + 1 sorted position of a row's tokens; set
-                             // for rows that have some
-    unsigned* row_end;
+    uint2*    pair[2];       // (key, token) ping-pong buffers [tokens]; the result is in the first
+    unsigned* count[kMaxPasses];     // [blocks][bins] digits of each pass in each block's part of its input
     unsigned* arrived;       // [n_arrived] counters of the sums' grid, cleared here
     long long tokens, n_arrived;
     unsigned  rows, padding; // padding: its own row, or rows when there is none
-    int       digit_bits, passes;
+    unsigned  tile;          // tokens per block of the counting and moving grids
+    int       digit_bits, passes, blocks;
 };
 
-__device__ __forceinline__ unsigned block_exclusive_scan(unsigned v, unsigned* warp_totals)
+// Exclusive sum over the block's threads (kSortThreads of them); `totals` has room for a warp.
+__device__ __forceinline__ unsigned block_exclusive_scan(unsigned v, unsigned* totals)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned s = v;
+    auto warp_scan = [&](unsigned x) {
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const unsigned u = __shfl_up_sync(0xffffffffu, s, o);
-        if (lane >= o) s += u;
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned u = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += u;
+        }
+        return x;
+    };
+    const unsigned s = warp_scan(v);
+    if (lane == 31) totals[warp] = s;
+    __syncthreads();
+    const unsigned t = totals[lane], upto = warp_scan(t);
+    return __shfl_sync(0xffffffffu, upto - t, warp) + s - v;
+}
+
+template <typename I>
+__device__ __forceinline__ unsigned key_of(I id, const SortArgs& a)
+{
+    const long long v = static_cast<long long>(id);
+    return (v >= 0 && v < a.rows && v != a.padding) ? static_cast<unsigned>(v) : a.rows;
+}
+
+// The lanes of `in` whose digit equals this lane's: one vote per bit of the digit.  (The match
+// instruction takes its time for every distinct value; votes take the same for all data.)
+__device__ __forceinline__ unsigned lanes_with(unsigned digit, unsigned in, int bits)
+{
+    unsigned m = in;
+#pragma unroll
+    for (int b = 0; b < kMaxDigitBits; ++b) {
+        if (b >= bits) break;
+        const bool one = digit >> b & 1u;
+        const unsigned v = __ballot_sync(0xffffffffu, one);
+        m &= one ? v : ~v;
     }
-    if (lane == 31) warp_totals[warp] = s;
+    return m;
+}
+
+// Number of equal digits before this lane's element in the warp's run, which `counts` holds for
+// the elements before these 32; adds these 32 to it.  The whole warp calls.
+__device__ __forceinline__ unsigned rank_and_count(unsigned digit, bool in, int bits, unsigned* counts)
+{
+    const unsigned peers = lanes_with(digit, __ballot_sync(0xffffffffu, in), bits);
+    const unsigned before = __popc(peers & ((1u << (threadIdx.x & 31)) - 1u));
+    const unsigned sum = in ? counts[digit] : 0u;
+    __syncwarp();
+    if (in && before == 0) counts[digit] = sum + __popc(peers);
+    __syncwarp();
+    return sum + before;
+}
+
+// hist[warp][digit] becomes the count in the warps before; returns the block's count of digit tid.
+__device__ __forceinline__ unsigned sum_over_warps(unsigned* hist, int bins)
+{
+    unsigned s = 0;
+    if (static_cast<int>(threadIdx.x) < bins) {
+        unsigned v[kSortWarps];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) v[w] = hist[w * kMaxBins + threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            hist[w * kMaxBins + threadIdx.x] = s;
+            s += v[w];
+        }
+    }
+    return s;
+}
+
+// Up to kFewTokens tokens: the place of a token is the number of tokens that sort before it.
+template <typename I>
+__global__ void __launch_bounds__(kFewTokens)
+k_embed_sort_few(const I* __restrict__ ids, SortArgs a)
+{
+    __shared__ __align__(16) unsigned word[kFewTokens];
+    release_dependents();
+    const unsigned t = threadIdx.x, n = static_cast<unsigned>(a.tokens);
+    for (long long k = t; k < a.n_arrived; k += kFewTokens) a.arrived[k] = 0u;
+    const unsigned mine = t < n ? key_of(ids[t], a) << 9 | t : 0xffffffffu;
+    word[t] = mine;
     __syncthreads();
+    if (t >= n) return;
     unsigned before = 0;
-    for (int w = 0; w < warp; ++w) before += warp_totals[w];
+    for (unsigned j = 0; j < n; j += 4) {                // words behind the last token are all ones
+        const uint4 w = *reinterpret_cast<const uint4*>(word + j);
+        before += (w.x < mine) + (w.y < mine) + (w.z < mine) + (w.w < mine);
+    }
+    a.pair[0][before] = make_uint2(mine >> 9, t);
+}
+
+// Up to kOneTokens tokens: one block, the elements stay in registers and shared memory.
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads)
+k_embed_sort_one(const I* __restrict__ ids, SortArgs a)
+{
+    constexpr int kRounds = kOneTokens / kSortThreads;
+    extern __shared__ __align__(16) unsigned hist[];     // [warp][digit], then the elements
+    uint2* const s_pair = reinterpret_cast<uint2*>(hist + kSortWarps * kMaxBins);
+    __shared__ unsigned base[kMaxBins], scan_totals[32];
+    release_dependents();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int n = static_cast<int>(a.tokens), bins = 1 << a.digit_bits;
+    for (long long k = tid; k < a.n_arrived; k += kSortThreads) a.arrived[k] = 0u;
+    const int per = (n + kSortThreads - 1) / kSortThreads * 32;
+    const int begin = min(n, warp * per), end = min(n, begin + per);
+    unsigned* const mine = hist + warp * kMaxBins;
+    uint2 pair[kRounds];
+    unsigned rank[kRounds];
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+        const int k = begin + r * 32 + lane;
+        pair[r] = make_uint2(k < end ? key_of(ids[k], a) : 0u, static_cast<unsigned>(k));
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * a.digit_bits;
+        if (pass > 0) {
+#pragma unroll
+            for (int r = 0; r < kRounds; ++r) {
+                const int k = begin + r * 32 + lane;
+                if (k < end) pair[r] = s_pair[k];
+            }
+        }
+        for (int k = lane; k < bins; k += 32) mine[k] = 0u;
+        __syncwarp();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (begin + r * 32 >= end) break;
+            rank[r] = rank_and_count(pair[r].x >> shift & (bins - 1), begin + r * 32 + lane < end, a.digit_bits, mine);
+        }
+        __syncthreads();
+        const unsigned first = block_exclusive_scan(sum_over_warps(hist, bins), scan_totals);
+        if (tid < bins) base[tid] = first;
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (begin + r * 32 + lane >= end) break;
+            const unsigned digit = pair[r].x >> shift & (bins - 1);
+            s_pair[base[digit] + mine[digit] + rank[r]] = pair[r];
+        }
+        __syncthreads();
+    }
+    for (int k = tid; k < n; k += kSortThreads) a.pair[0][k] = s_pair[k];
+}
+
+// More tokens: a counting grid, then one moving grid per digit.  Block b has the tokens (in the
+// order of the pass's input) from b * tile on.
+template <typename I>
+__global__ void __launch_bounds__(kSortThreads)
+k_embed_count(const I* __restrict__ ids, SortArgs a)
+{
+    __shared__ unsigned count[kMaxBins];
+    release_dependents();
+    const int tid = threadIdx.x, bins = 1 << a.digit_bits;
+    const long long at = static_cast<long long>(blockIdx.x) * kSortThreads + tid;
+    const long long all = static_cast<long long>(a.blocks) * kSortThreads;
+    for (long long k = at; k < a.n_arrived; k += all) a.arrived[k] = 0u;
+    // the moving grids count the digits of the pass after theirs
+    for (int pass = 1; pass < a.passes; ++pass)
+        for (int k = tid; k < bins; k += kSortThreads) a.count[pass][static_cast<long long>(blockIdx.x) * bins + k] = 0u;
+    if (tid < bins) count[tid] = 0u;
     __syncthreads();
-    return before + s - v;
+    const long long begin = static_cast<long long>(blockIdx.x) * a.tile, end = min(a.tokens, begin + a.tile);
+#pragma unroll 4
+    for (long long k = begin + tid; k < end; k += kSortThreads) atomicAdd(&count[key_of(ids[k], a) & (bins - 1)], 1u);
+    __syncthreads();
+    if (tid < bins) a.count[0][static_cast<long long>(blockIdx.x) * bins + tid] = count[tid];
 }
 
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads)
-k_embed_sort(const I* __restrict__ ids, SortArgs a)
+k_embed_move(const I* __restrict__ ids, SortArgs a, int pass)
 {
-    extern __shared__ unsigned hist[];                   // [warp][digit]
-    __shared__ unsigned total[kMaxBins], base[kMaxBins], warp_totals[kSortWarps];
-    cg::cluster_group cluster = cg::this_cluster();
-    const int blocks = static_cast<int>(cluster.num_blocks()), me = static_cast<int>(cluster.block_rank());
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int bins = 1 << a.digit_bits;
+    constexpr int kRounds = 4;                           // elements per lane that are loaded at once
+    extern __shared__ __align__(16) unsigned hist[];     // [warp][digit]
+    __shared__ unsigned sum_before[kSortThreads], sum_all[kSortThreads], base[kMaxBins], scan_totals[32];
     release_dependents();
-    for (long long k = static_cast<long long>(me) * kSortThreads + tid; k < a.n_arrived;
-         k += static_cast<long long>(blocks) * kSortThreads)
-        a.arrived[k] = 0u;
-    const long long runs = static_cast<long long>(blocks) * kSortWarps;
-    const long long per = ((a.tokens + runs - 1) / runs + 31) / 32 * 32;
-    const long long begin = min(a.tokens, (static_cast<long long>(me) * kSortWarps + warp) * per);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int bins = 1 << a.digit_bits, shift = pass * a.digit_bits, me = static_cast<int>(blockIdx.x);
+    const int to_buffer = (a.passes - 1 - pass) & 1;
+    const uint2* const src = a.pair[to_buffer ^ 1];
+    uint2* const dst = a.pair[to_buffer];
+    const long long per = a.tile / kSortWarps;
+    const long long begin = min(a.tokens, static_cast<long long>(me) * a.tile + warp * per);
     const long long end = min(a.tokens, begin + per);
     unsigned* const mine = hist + warp * kMaxBins;
-
-    for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * a.digit_bits;
-        const unsigned* const src_key = a.key[(pass + 1) & 1];
-        const unsigned* const src_token = a.token[(pass + 1) & 1];
-        unsigned* const dst_key = a.key[pass & 1];
-        unsigned* const dst_token = a.token[pass & 1];
-        auto key_at = [&](long long k) -> unsigned {
-            if (pass > 0) return __ldcg(src_key + k);
-            const long long id = static_cast<long long>(ids[k]);
-            return (id >= 0 && id < a.rows && id != a.padding) ? static_cast<unsigned>(id) : a.rows;
-        };
-        for (int k = lane; k < bins; k += 32) mine[k] = 0u;
-        __syncwarp();
-        for (long long k = begin + lane; k < end; k += 32)
-            atomicAdd(&mine[(key_at(k) >> shift) & (bins - 1)], 1u);
-        __syncthreads();
-        if (tid < bins) {
-            unsigned s = 0;
-            for (int w = 0; w < kSortWarps; ++w) {
-                const unsigned v = hist[w * kMaxBins + tid];
-                hist[w * kMaxBins + tid] = s;
-                s += v;
-            }
-            total[tid] = s;
-        }
-        cluster.sync();
-        unsigned before = 0, all = 0;
-        if (tid < bins)
-            for (int b = 0; b < blocks; ++b) {
-                const unsigned v = *cluster.map_shared_rank(&total[tid], b);
-                if (b < me) before += v;
-                all += v;
-            }
-        const unsigned first = block_exclusive_scan(all, warp_totals);
-        if (tid < bins) base[tid] = first + before;
-        __syncthreads();
-        for (long long k0 = begin; k0 < end; k0 += 32) {
-            const long long k = k0 + lane;
-            const bool in = k < end;
-            const unsigned active = __ballot_sync(0xffffffffu, in);
-            if (in) {
-                const unsigned key = key_at(k);
-                const unsigned token = pass > 0 ? __ldcg(src_token + k) : static_cast<unsigned>(k);
-                const unsigned digit = (key >> shift) & (bins - 1);
-                const unsigned peers = __match_any_sync(active, digit);
-                const unsigned rank = __popc(peers & ((1u << lane) - 1u));
-                const unsigned at = base[digit] + mine[digit] + rank;
-                __syncwarp(active);
-                if (rank == 0) mine[digit] += __popc(peers);
-                __syncwarp(active);
-                dst_key[at] = key;
-                dst_token[at] = token;
-            }
-        }
-        __threadfence();
-        cluster.sync();
-    }
-    const unsigned* const key = a.key[(a.passes + 1) & 1];
-    for (long long k = begin + lane; k < end; k += 32) {
-        const unsigned v = __ldcg(key + k);
-        if (v >= a.rows) continue;
-        if (k == 0 || __ldcg(key + k - 1) != v) a.row_start[v] = static_cast<unsigned>(k);
-        if (k + 1 == a.tokens || __ldcg(key + k + 1) != v) a.row_end[v] = static_cast<unsigned>(k + 1);
-    }
-}
-
-// ---- backward: rows without tokens ---------------------------------------------------------------
-// Runs beside the sort (it needs the ids only): block c owns the rows r = c mod gridDim.x (a
-// power of two, so that frequent ids, which are neighbours in most vocabularies, spread over the
-// blocks), marks those that have tokens in a bit map of its own and writes zeros to the others.
-constexpr int kZeroThreads = 512;
-constexpr int kZeroWords = 4096;         // bits of rows per round: 131072
-
-template <typename I, typename O, int EV>
-__global__ void __launch_bounds__(kZeroThreads)
-k_embed_zero(const I* __restrict__ ids, long long tokens, unsigned rows, unsigned padding, long long cols,
-             O* __restrict__ grad, long long grad_ld, int log2_blocks)
-{
-    __shared__ unsigned seen[kZeroWords];
-    release_dependents();
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned own = blockIdx.x, mask = (1u << log2_blocks) - 1u;
-    const unsigned owned = own < rows ? ((rows - 1u - own) >> log2_blocks) + 1u : 0u;      // rows of this block
-    const float zeros[EV] = {};
-    for (unsigned first = 0; first < owned; first += kZeroWords * 32u) {
-        const unsigned count = min(owned - first, kZeroWords * 32u);
-        for (unsigned k = tid; k < (count + 31u) / 32u; k += kZeroThreads) seen[k] = 0u;
-        __syncthreads();
-#pragma unroll 4
-        for (long long t = tid; t < tokens; t += kZeroThreads) {
-            const long long id = static_cast<long long>(ids[t]);
-            if (id < 0 || id >= rows || (static_cast<unsigned>(id) & mask) != own || id == padding) continue;
-            const unsigned bit = (static_cast<unsigned>(id) >> log2_blocks) - first;
-            if (bit < count && !(seen[bit >> 5] >> (bit & 31u) & 1u)) atomicOr(&seen[bit >> 5], 1u << (bit & 31u));
-        }
-        __syncthreads();
-        for (unsigned k = warp; k < count; k += kZeroThreads / 32) {
-            if (seen[k >> 5] >> (k & 31u) & 1u) continue;
-            O* const dst = grad + (static_cast<long long>(first + k) * (mask + 1u) + own) * grad_ld;
-            for (long long c = static_cast<long long>(lane) * EV; c < cols; c += 32 * EV) store_ev<EV, O>(dst + c, zeros);
-        }
-        __syncthreads();
-    }
-    // the sums' grid waits for this one; by waiting for the sort here it waits for both
+    for (int k = lane; k < bins; k += 32) mine[k] = 0u;
     wait_for_previous_grid();
+    // digit tid % bins: all of it, and what the blocks before this one have (bins divides the threads)
+    {
+        const unsigned* const count = a.count[pass];
+        const int digit = tid & (bins - 1), step = kSortThreads >> a.digit_bits;
+        unsigned before = 0, all = 0;
+#pragma unroll 8
+        for (int b = tid >> a.digit_bits; b < a.blocks; b += step) {
+            const unsigned v = __ldcg(count + static_cast<long long>(b) * bins + digit);
+            all += v;
+            if (b < me) before += v;
+        }
+        sum_before[tid] = before;
+        sum_all[tid] = all;
+    }
+    uint2 pair[kRounds];
+    unsigned rank[kRounds];
+    auto load = [&](long long at) {
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            const long long k = at + r * 32 + lane;
+            if (k < end) pair[r] = pass > 0 ? __ldcg(src + k) : make_uint2(key_of(ids[k], a), static_cast<unsigned>(k));
+            else pair[r] = make_uint2(0u, 0u);
+        }
+    };
+    auto count_ranks = [&](long long at) {
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (at + r * 32 >= end) break;
+            rank[r] = rank_and_count(pair[r].x >> shift & (bins - 1), at + r * 32 + lane < end, a.digit_bits, mine);
+        }
+    };
+    const bool kept = per <= 32 * kRounds;               // a warp's run fits its registers
+    __syncwarp();
+    for (long long at = begin; at < end; at += 32 * kRounds) {
+        load(at);
+        count_ranks(at);
+    }
+    __syncthreads();
+    sum_over_warps(hist, bins);
+    unsigned before = 0, all = 0;
+    if (tid < bins)
+        for (int k = tid; k < kSortThreads; k += bins) {
+            before += sum_before[k];
+            all += sum_all[k];
+        }
+    const unsigned first = block_exclusive_scan(all, scan_totals);
+    if (tid < bins) base[tid] = first + before;
+    __syncthreads();
+    for (long long at = begin; at < end; at += 32 * kRounds) {
+        if (!kept) {                                     // counts go on from what the warps before have
+            load(at);
+            count_ranks(at);
+        }
+#pragma unroll
+        for (int r = 0; r < kRounds; ++r) {
+            if (at + r * 32 + lane >= end) break;
+            const unsigned digit = pair[r].x >> shift & (bins - 1);
+            const unsigned to = base[digit] + rank[r] + (kept ? mine[digit] : 0u);
+            dst[to] = pair[r];
+            if (pass + 1 < a.passes)
+                atomicAdd(&a.count[pass + 1][static_cast<long long>(to / a.tile) * bins + (pair[r].x >> (shift + a.digit_bits) & (bins - 1))], 1u);
+        }
+    }
 }
 
 // ---- backward: the sums ----------------------------------------------------------------------------
@@ -302,19 +411,23 @@ k_embed_zero(const I* __restrict__ ids, long long tokens, unsigned rows, unsigne
 // begins and ends within a warp is stored at once.  A part of a run that crosses warps goes
 // through shared memory to the warp in which the run ends; one that crosses blocks goes to
 // the workspace, and the block that arrives last for that run adds the parts in order.
+//
+// The first zero_blocks blocks write the rows without tokens instead.  They need the ids only, so
+// they do not wait for the sort: the zeros are written while it runs.
 constexpr int kSumWarps = 8;
+constexpr int kZeroBlocks = 256;
+constexpr int kZeroWords = 4096;         // bits of rows per round: 131072
 enum : int { kLinkHead = 1, kLinkTail = 2, kLinkThrough = 4 };
 
 struct SumArgs {
-    const unsigned* key;       // sorted [tokens]
-    const unsigned* token;
-    const unsigned* row_start;
-    const unsigned* row_end;
+    const uint2* pair;         // sorted (key, token) [tokens]
     float*    part;            // [blocks of tokens][2][slices][kSlice]: 0 = run from before, 1 = run that goes on
     unsigned* arrived;         // [blocks of tokens][slices]
+    const void* ids;
     long long tokens, cols, dy_ld, grad_ld;
-    unsigned  rows;
-    int       slices, per_warp, accumulate;
+    unsigned  rows, padding;
+    int       slices, per_warp, accumulate, id64;
+    int       zero_blocks;     // 0 or a power of two
     float     scale;
 };
 
@@ -341,23 +454,39 @@ __device__ __forceinline__ void store_row(const SumArgs& a, O* grad, unsigned ro
 }
 
 // One block's part of a run that crosses blocks.  The last of the run's blocks to arrive adds
-// all parts in the order of the tokens and stores the row.
+// all parts in the order of the tokens and stores the row.  begins / ends: the run does so here.
 template <typename O, int EV>
-__device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned row, unsigned block, int slot, int slice,
-                                            int lane, const float (&sum)[8])
+__device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned row, int block, bool begins, bool ends,
+                                            int slice, int lane, const float (&sum)[8])
 {
-    const unsigned size = static_cast<unsigned>(kSumWarps * a.per_warp);
-    const unsigned first = __ldcg(a.row_start + row) / size, last = (__ldcg(a.row_end + row) - 1u) / size;
-    auto at = [&](unsigned b, int s) {
+    const int size = kSumWarps * a.per_warp;
+    auto at = [&](int b, int s) {
         return a.part + ((static_cast<long long>(b) * 2 + s) * a.slices + slice) * kSlice + lane; };
-    float* const mine = at(block, slot);
+    float* const mine = at(block, begins ? 1 : 0);
 #pragma unroll
     for (int j = 0; j < 8; ++j) __stcg(mine + j * 32, sum[j]);
+    // the run's first and last block: 32 blocks' borders are looked at at once
+    int first = block, last = block;
+    while (!begins) {
+        const int b = first - 1 - lane;                  // the run reaches back into block first - 1
+        const bool here = b <= 0 || __ldcg(&a.pair[static_cast<long long>(b) * size - 1].x) != row;
+        const unsigned found = __ballot_sync(0xffffffffu, here);
+        first -= found ? __ffs(found) : 32;
+        begins = found != 0;
+    }
+    while (!ends) {
+        const int b = last + 1 + lane;
+        const long long next = (static_cast<long long>(b) + 1) * size;
+        const bool here = next >= a.tokens || __ldcg(&a.pair[next].x) != row;
+        const unsigned found = __ballot_sync(0xffffffffu, here);
+        last += found ? __ffs(found) : 32;
+        ends = found != 0;
+    }
     __threadfence();
     __syncwarp();
     unsigned final = 0;
     if (lane == 0)
-        final = atomicAdd(&a.arrived[static_cast<long long>(first) * a.slices + slice], 1u) == last - first;
+        final = atomicAdd(&a.arrived[static_cast<long long>(first) * a.slices + slice], 1u) == static_cast<unsigned>(last - first);
     if (!__shfl_sync(0xffffffffu, final, 0)) return;
     __threadfence();
     float total[8];
@@ -366,7 +495,7 @@ __device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned 
 #pragma unroll
         for (int j = 0; j < 8; ++j) total[j] = __ldcg(p + j * 32);
     }
-    for (unsigned b = first + 1; b <= last; b += 4) {
+    for (int b = first + 1; b <= last; b += 4) {
         float x[4][8];
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
@@ -382,29 +511,92 @@ __device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned 
     store_row<O, EV>(a, grad, row, slice, lane, total);
 }
 
+// Block `own` of zero_blocks: the rows r = own mod zero_blocks (frequent ids are neighbours in
+// most vocabularies: this spreads them), marked in a bit map when a token has them, else zeroed.
+template <typename I, typename O, int EV>
+__device__ __forceinline__ void zero_rows(const I* __restrict__ ids, O* __restrict__ grad, const SumArgs& a, unsigned* seen)
+{
+    constexpr int kPer = 16 / static_cast<int>(sizeof(I)), kBatch = 8;       // 16-byte loads, eight at a time
+    constexpr int kThreads = kSumWarps * 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned own = blockIdx.x, mask = static_cast<unsigned>(a.zero_blocks) - 1u;
+    const int shift = __popc(mask);
+    const unsigned owned = own < a.rows ? ((a.rows - 1u - own) >> shift) + 1u : 0u;
+    // the ids from the first 16-byte boundary on go in whole loads, the others one by one
+    const long long lead = min(a.tokens, static_cast<long long>((16 - reinterpret_cast<uintptr_t>(ids) % 16) % 16 / sizeof(I)));
+    const long long whole = (a.tokens - lead) / kPer;
+    const float zeros[EV] = {};
+    for (unsigned first = 0; first < owned; first += kZeroWords * 32u) {
+        const unsigned count = min(owned - first, kZeroWords * 32u);
+        for (unsigned k = tid; k < (count + 31u) / 32u; k += kThreads) seen[k] = 0u;
+        __syncthreads();
+        auto mark = [&](I raw) {
+            const long long id = static_cast<long long>(raw);
+            if (id < 0 || id >= a.rows || (static_cast<unsigned>(id) & mask) != own || id == a.padding) return;
+            const unsigned bit = (static_cast<unsigned>(id) >> shift) - first;
+            if (bit < count && !(seen[bit >> 5] >> (bit & 31u) & 1u)) atomicOr(&seen[bit >> 5], 1u << (bit & 31u));
+        };
+        for (long long k = tid; k < whole; k += kBatch * kThreads) {
+            uint4 w[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u)
+                w[u] = k + u * kThreads < whole ? reinterpret_cast<const uint4*>(ids + lead)[k + u * kThreads]
+                                                : make_uint4(~0u, ~0u, ~0u, ~0u);        // -1: no row
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                if constexpr (sizeof(I) == 4) {
+                    mark(static_cast<I>(w[u].x)); mark(static_cast<I>(w[u].y));
+                    mark(static_cast<I>(w[u].z)); mark(static_cast<I>(w[u].w));
+                } else {
+                    mark(static_cast<I>(static_cast<unsigned long long>(w[u].y) << 32 | w[u].x));
+                    mark(static_cast<I>(static_cast<unsigned long long>(w[u].w) << 32 | w[u].z));
+                }
+            }
+        }
+        if (tid < lead) mark(ids[tid]);
+        const long long rest = lead + whole * kPer + tid;
+        if (rest < a.tokens) mark(ids[rest]);
+        __syncthreads();
+        for (unsigned k = warp; k < count; k += kSumWarps) {
+            if (seen[k >> 5] >> (k & 31u) & 1u) continue;
+            O* const dst = grad + (static_cast<long long>(first + k) * (mask + 1u) + own) * a.grad_ld;
+            for (long long c = static_cast<long long>(lane) * EV; c < a.cols; c += 32 * EV) store_ev<EV, O>(dst + c, zeros);
+        }
+        __syncthreads();
+    }
+}
+
 template <typename T, typename O, int EV>
 __global__ void __launch_bounds__(kSumWarps * 32)
 k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
 {
     constexpr int U = sizeof(T) == 2 ? 8 : 4;            // rows in flight: 8 * 16 or 4 * 32 bytes per lane
     __shared__ float part[kSumWarps][2][8][32];          // [warp][head, tail][element][lane]
+    static_assert(sizeof(part) >= sizeof(unsigned) * kZeroWords, "the bit map takes the parts' place");
     __shared__ int link[kSumWarps];
+    if (blockIdx.x < static_cast<unsigned>(a.zero_blocks)) {
+        unsigned* const seen = reinterpret_cast<unsigned*>(part);
+        if (a.id64) zero_rows<long long, O, EV>(static_cast<const long long*>(a.ids), grad, a, seen);
+        else        zero_rows<int, O, EV>(static_cast<const int*>(a.ids), grad, a, seen);
+        return;
+    }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const unsigned block = blockIdx.x / static_cast<unsigned>(a.slices);
-    const int slice = static_cast<int>(blockIdx.x - block * static_cast<unsigned>(a.slices));
+    const unsigned at = blockIdx.x - static_cast<unsigned>(a.zero_blocks);
+    const unsigned block = at / static_cast<unsigned>(a.slices);
+    const int slice = static_cast<int>(at - block * static_cast<unsigned>(a.slices));
     const int K = a.per_warp;
     const long long p0 = (static_cast<long long>(block) * kSumWarps + warp) * K;
     wait_for_previous_grid();
 
     const long long p = p0 + lane;
     const bool in = lane < K && p < a.tokens;
-    const unsigned key = in ? __ldcg(a.key + p) : a.rows;
-    const unsigned token = in ? __ldcg(a.token + p) : 0u;
+    const uint2 pair = in ? __ldcg(a.pair + p) : make_uint2(a.rows, 0u);
+    const unsigned key = pair.x, token = pair.y;
     const int n = __popc(__ballot_sync(0xffffffffu, key < a.rows));          // keys that are rows come first
     const unsigned key_first = __shfl_sync(0xffffffffu, key, 0);
     const unsigned key_last = __shfl_sync(0xffffffffu, key, K - 1);
-    const bool head = n > 0 && p0 > 0 && __ldcg(a.key + p0 - 1) == key_first;
-    const bool tail = n == K && p0 + K < a.tokens && __ldcg(a.key + p0 + K) == key_last;
+    const bool head = n > 0 && p0 > 0 && __ldcg(&a.pair[p0 - 1].x) == key_first;
+    const bool tail = n == K && p0 + K < a.tokens && __ldcg(&a.pair[p0 + K].x) == key_last;
     const bool through = head && tail && key_first == key_last;
     if (lane == 0) link[warp] = (head ? kLinkHead : 0) | (tail ? kLinkTail : 0) | (through ? kLinkThrough : 0);
 
@@ -470,11 +662,11 @@ k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
     };
     if (head && !through) {
         if (gather(0) >= 0) store_row<O, EV>(a, grad, key_first, slice, lane, acc);
-        else join_blocks<O, EV>(a, grad, key_first, block, 0, slice, lane, acc);
+        else join_blocks<O, EV>(a, grad, key_first, static_cast<int>(block), false, true, slice, lane, acc);
     }
     if (warp == kSumWarps - 1 && tail) {
         const int w = gather(through ? 0 : 1);
-        join_blocks<O, EV>(a, grad, key_last, block, w >= 0 ? 1 : 0, slice, lane, acc);
+        join_blocks<O, EV>(a, grad, key_last, static_cast<int>(block), w >= 0, false, slice, lane, acc);
     }
 }
 
@@ -491,7 +683,9 @@ int tokens_per_warp(const came_embed& e)
 }
 
 struct Layout {
-    size_t key[2], token[2], row_start, row_end, part, arrived, bytes;
+    size_t pair[2], count[kMaxPasses], part, arrived, bytes;
+    int digit_bits, passes, sort_blocks; // of the sort
+    unsigned tile;
     long long blocks, slices;            // of the sums' grid
     int per_warp;
 };
@@ -504,13 +698,18 @@ Layout layout(const came_embed& e)
     l.per_warp = tokens_per_warp(e);
     l.blocks = ceil_div(e.tokens, kSumWarps * l.per_warp);
     l.slices = ceil_div(e.cols, kSlice);
-    for (int k = 0; k < 2; ++k) l.key[k] = take(sizeof(unsigned) * e.tokens);
-    for (int k = 0; k < 2; ++k) l.token[k] = take(sizeof(unsigned) * e.tokens);
-    l.row_start = take(sizeof(unsigned) * e.rows);
-    l.row_end = take(sizeof(unsigned) * e.rows);
+    int bits = 1;
+    while ((e.rows >> bits) != 0) ++bits;                 // the keys are 0 .. rows
+    l.passes = static_cast<int>(ceil_div(bits, kMaxDigitBits));
+    l.digit_bits = static_cast<int>(ceil_div(bits, l.passes));
+    l.tile = static_cast<unsigned>(ceil_div(std::max<long long>(e.tokens, 1), kSortThreads * kSortBlocks) * kSortThreads);
+    l.sort_blocks = static_cast<int>(ceil_div(e.tokens, l.tile));
+    for (int k = 0; k < 2; ++k) l.pair[k] = take(sizeof(uint2) * e.tokens);
+    for (int k = 0; k < l.passes; ++k)
+        l.count[k] = take(sizeof(unsigned) * (static_cast<size_t>(l.sort_blocks) << l.digit_bits));
     l.part = take(sizeof(float) * 2 * kSlice * l.blocks * l.slices);
     l.arrived = take(sizeof(unsigned) * l.blocks * l.slices);
-    l.bytes = at;
+    l.bytes = std::max<size_t>(at, 256);
     return l;
 }
 
@@ -596,11 +795,12 @@ void launch_forward_types(const came_embed& e, cudaStream_t stream)
 // Launched with programmatic stream serialisation: the kernel waits for the grid before it itself.
 // (early = false: an ordinary launch.)
 template <typename K, typename... A>
-cudaError_t launch_dependent(K kernel, bool early, long long blocks, int threads, cudaStream_t stream, A... args)
+cudaError_t launch_dependent(K kernel, bool early, long long blocks, int threads, size_t smem, cudaStream_t stream, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -613,58 +813,44 @@ cudaError_t launch_dependent(K kernel, bool early, long long blocks, int threads
 template <typename I>
 cudaError_t launch_sort(const came_embed& e, const SortArgs& a, cudaStream_t stream)
 {
-    cudaError_t err = cudaFuncSetAttribute(k_embed_sort<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           static_cast<int>(kSortSmem));
+    const I* const ids = static_cast<const I*>(e.ids);
+    if (e.tokens <= kFewTokens && a.rows < kFewRows) {
+        k_embed_sort_few<I><<<1, kFewTokens, 0, stream>>>(ids, a);
+        return cudaGetLastError();
+    }
+    if (e.tokens <= kOneTokens) {
+        const cudaError_t err = cudaFuncSetAttribute(k_embed_sort_one<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                     static_cast<int>(kOneBytes));
+        if (err != cudaSuccess) return err;
+        k_embed_sort_one<I><<<1, kSortThreads, kOneBytes, stream>>>(ids, a);
+        return cudaGetLastError();
+    }
+    cudaError_t err = cudaFuncSetAttribute(k_embed_move<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           static_cast<int>(kHistBytes));
     if (err != cudaSuccess) return err;
-    cudaLaunchConfig_t cfg = {};
-    const unsigned blocks = e.tokens <= 4096 ? 1 : 8;
-    cfg.gridDim = dim3(blocks);
-    cfg.blockDim = dim3(kSortThreads);
-    cfg.dynamicSmemBytes = kSortSmem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = blocks;
-    attr[0].val.clusterDim.y = 1;
-    attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_embed_sort<I>, static_cast<const I*>(e.ids), a);
-}
-
-template <typename I, typename O, int EV>
-cudaError_t launch_zero(const came_embed& e, unsigned padding, cudaStream_t stream)
-{
-    int lg = 0;
-    while (lg < 8 && (2ll << lg) <= e.rows) ++lg;        // at most 256 blocks, two per SM
-    // it may start while the sort runs, but only behind a sort: the sort has waited for everything
-    // before it, and only then may rows be written
-    return launch_dependent(k_embed_zero<I, O, EV>, e.tokens > 0, 1ll << lg, kZeroThreads, stream, static_cast<const I*>(e.ids),
-                            static_cast<long long>(e.tokens), static_cast<unsigned>(e.rows), padding,
-                            static_cast<long long>(e.cols), static_cast<O*>(e.table),
-                            static_cast<long long>(e.table_ld), lg);
-}
-
-template <typename T, typename O, int EV>
-cudaError_t launch_sums(const came_embed& e, const SumArgs& s, unsigned padding, long long blocks, cudaStream_t stream)
-{
-    cudaError_t err = cudaSuccess;
-    if (!s.accumulate)
-        err = e.id_dtype == CAME_I64 ? launch_zero<long long, O, EV>(e, padding, stream) : launch_zero<int, O, EV>(e, padding, stream);
-    if (err == cudaSuccess && blocks > 0)
-        err = launch_dependent(k_embed_sum<T, O, EV>, true, blocks, kSumWarps * 32, stream, static_cast<const T*>(e.data),
-                               static_cast<O*>(e.table), s);
+    k_embed_count<I><<<a.blocks, kSortThreads, 0, stream>>>(ids, a);
+    for (int pass = 0; pass < a.passes && err == cudaSuccess; ++pass)
+        err = launch_dependent(k_embed_move<I>, true, a.blocks, kSortThreads, kHistBytes, stream, ids, a, pass);
     return err;
 }
 
+template <typename T, typename O, int EV>
+cudaError_t launch_sums(const came_embed& e, const SumArgs& s, long long blocks, cudaStream_t stream)
+{
+    // the rows without tokens may be written while the sort runs, but only behind a sort: it has
+    // waited for everything that came before
+    return launch_dependent(k_embed_sum<T, O, EV>, e.tokens > 0, s.zero_blocks + blocks, kSumWarps * 32, 0, stream,
+                            static_cast<const T*>(e.data), static_cast<O*>(e.table), s);
+}
+
 template <typename T, typename O>
-cudaError_t launch_sums_ev(const came_embed& e, const SumArgs& s, unsigned padding, long long blocks, cudaStream_t stream)
+cudaError_t launch_sums_ev(const came_embed& e, const SumArgs& s, long long blocks, cudaStream_t stream)
 {
     switch (elements_per_access(e)) {
-        case 8:  return launch_sums<T, O, 8>(e, s, padding, blocks, stream);
-        case 4:  return launch_sums<T, O, 4>(e, s, padding, blocks, stream);
-        case 2:  return launch_sums<T, O, 2>(e, s, padding, blocks, stream);
-        default: return launch_sums<T, O, 1>(e, s, padding, blocks, stream);
+        case 8:  return launch_sums<T, O, 8>(e, s, blocks, stream);
+        case 4:  return launch_sums<T, O, 4>(e, s, blocks, stream);
+        case 2:  return launch_sums<T, O, 2>(e, s, blocks, stream);
+        default: return launch_sums<T, O, 1>(e, s, blocks, stream);
     }
 }
 
@@ -712,30 +898,23 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
         return report(CAME_ERR_SHAPE, "workspace smaller than came_embed_workspace says");
     if ((s = require_current_device(device)) != CAME_OK) return s;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (l.blocks * l.slices >= (1ll << 31)) return report(CAME_ERR_SHAPE, "too many tokens times columns for one launch");
+    if (l.blocks * l.slices + kZeroBlocks >= (1ll << 31)) return report(CAME_ERR_SHAPE, "too many tokens times columns for one launch");
     char* const w = static_cast<char*>(workspace);
     auto at = [&](size_t offset) { return reinterpret_cast<unsigned*>(w + offset); };
     SortArgs a = {};
-    for (int k = 0; k < 2; ++k) {
-        a.key[k] = at(l.key[k]);
-        a.token[k] = at(l.token[k]);
-    }
-    a.row_start = at(l.row_start);
-    a.row_end = at(l.row_end);
+    for (int k = 0; k < 2; ++k) a.pair[k] = reinterpret_cast<uint2*>(w + l.pair[k]);
+    for (int k = 0; k < l.passes; ++k) a.count[k] = at(l.count[k]);
     a.arrived = at(l.arrived);
     a.n_arrived = l.blocks * l.slices;
     a.tokens = e->tokens;
     a.rows = static_cast<unsigned>(e->rows);
     a.padding = padding ? static_cast<unsigned>(e->padding_row) : a.rows;
-    int bits = 1;
-    while ((e->rows >> bits) != 0) ++bits;                // the keys are 0 .. rows
-    a.passes = static_cast<int>(ceil_div(bits, kMaxDigitBits));
-    a.digit_bits = static_cast<int>(ceil_div(bits, a.passes));
+    a.passes = l.passes;
+    a.digit_bits = l.digit_bits;
+    a.tile = l.tile;
+    a.blocks = l.sort_blocks;
     SumArgs t = {};
-    t.key = a.key[(a.passes + 1) & 1];
-    t.token = a.token[(a.passes + 1) & 1];
-    t.row_start = a.row_start;
-    t.row_end = a.row_end;
+    t.pair = a.pair[0];
     t.part = reinterpret_cast<float*>(w + l.part);
     t.arrived = a.arrived;
     t.tokens = e->tokens;
@@ -747,6 +926,14 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     t.per_warp = l.per_warp;
     t.accumulate = (e->flags & CAME_EMBED_ACCUMULATE) ? 1 : 0;
     t.scale = static_cast<float>(e->scale);
+    t.ids = e->ids;
+    t.id64 = e->id_dtype == CAME_I64;
+    t.padding = a.padding;
+    if (!t.accumulate) {
+        t.zero_blocks = 1;
+        while (t.zero_blocks < kZeroBlocks && 2ll * t.zero_blocks <= e->rows) t.zero_blocks *= 2;
+    }
+    if (e->tokens == 0 && t.accumulate) return CAME_OK;
     cudaError_t err = cudaSuccess;
     if (e->tokens > 0)
         err = e->id_dtype == CAME_I64 ? launch_sort<long long>(*e, a, stream) : launch_sort<int>(*e, a, stream);
@@ -754,11 +941,11 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     using bf16 = __nv_bfloat16;
     const long long blocks = l.blocks * l.slices;
     if (e->data_dtype == CAME_BF16)
-        err = e->table_dtype == CAME_BF16 ? launch_sums_ev<bf16, bf16>(*e, t, a.padding, blocks, stream)
-                                          : launch_sums_ev<bf16, float>(*e, t, a.padding, blocks, stream);
+        err = e->table_dtype == CAME_BF16 ? launch_sums_ev<bf16, bf16>(*e, t, blocks, stream)
+                                          : launch_sums_ev<bf16, float>(*e, t, blocks, stream);
     else
-        err = e->table_dtype == CAME_BF16 ? launch_sums_ev<float, bf16>(*e, t, a.padding, blocks, stream)
-                                          : launch_sums_ev<float, float>(*e, t, a.padding, blocks, stream);
+        err = e->table_dtype == CAME_BF16 ? launch_sums_ev<float, bf16>(*e, t, blocks, stream)
+                                          : launch_sums_ev<float, float>(*e, t, blocks, stream);
     if (err == cudaSuccess) err = cudaGetLastError();
     return err == cudaSuccess ? CAME_OK : report_cuda(err, "kernel launch");
 }

@@ -132,6 +132,23 @@ def test_gradient_against_64_bits(env, ydt, gdt, k):
         assert torch.equal(grad[untouched], old[untouched] if accumulate else torch.zeros_like(old[untouched]))
 
 
+@pytest.mark.parametrize("tokens,rows,kind", [
+    (1, 1000, "any"), (511, 1000, "hot"), (512, 1000, "any"), (513, 1000, "hot"), (300, (1 << 22) + 5, "any"), (4096, 5, "hot"),
+    (4097, 70000, "any"), (151_553, 1000, "hot"), (620_001, 300, "hot"), (620_001, 300_000, "any"), (100_000, 1, "any"), (200_000, 40, "same"),
+])
+def test_sorting_of_every_length(env, tokens, rows, kind):
+    """Every way the tokens are sorted: whole numbers small enough that fp32 sums are exact, so the
+    result must equal the exact one; few columns, many tokens."""
+    torch, binding = env
+    ids = _ids(torch, kind, tokens, rows, torch.int32, tokens)
+    dy = torch.randint(-3, 4, (tokens, 2), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).float()
+    got = binding.embed_backward(dy, ids, torch.empty(rows, 2, device="cuda"))
+    ok = (ids >= 0) & (ids < rows)
+    want = torch.zeros(rows, 2, device="cuda", dtype=torch.int64)
+    want.index_add_(0, ids[ok].long(), dy[ok].long())
+    assert torch.equal(got, want.float())
+
+
 def test_gradient_against_differences(env):
     """The lookup is linear in the table: <dW, E> = <c, out(W + E) - out(W - E)> / 2 for any E.
     The right side rounds each product by 2^-24 of an output; the left each sum as above."""
