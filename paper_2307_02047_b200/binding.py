@@ -410,24 +410,18 @@ def _torch():
     return _torch_module
 
 
-class _on:
-    """``with _on(device) as stream:`` makes ``device`` current for the block (nothing to do when it
-    is already) and gives the address of its current stream."""
-    __slots__ = ("index", "before")
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        cuda = _torch().cuda
-        self.before = cuda.current_device()
-        if self.before != self.index:
-            cuda.set_device(self.index)
-        return cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            _torch().cuda.set_device(self.before)
+def _call_on(device, call, *args) -> None:
+    """``call(*args, stream)`` with ``device`` current, ``stream`` its current stream's address."""
+    torch = _torch()
+    index, before = device.index, torch.cuda.current_device()
+    if before != index:
+        torch.cuda.set_device(index)
+    try:
+        # (a Stream object costs more than the launch)
+        call(*args, torch._C._cuda_getCurrentRawStream(index))
+    finally:
+        if before != index:
+            torch.cuda.set_device(before)
 
 
 # --- gradient norm and clipping ------------------------------------------------------------
@@ -486,7 +480,7 @@ class GradClip:
         self.total_norm, self.coef, self.tensor_norms = self.results[0], self.results[1], self.results[2:]
         self._results_at = self.results.data_ptr()
         self._params = came_clip_params()
-        with _on(self.device):
+        with torch.cuda.device(self.device):
             self.ctx = came_clip_create(descs, self.device.index)
 
     def _check_tensor(self, x, name):
@@ -507,8 +501,7 @@ class GradClip:
             at = [g.data_ptr() for g in grads]
         p = self._params
         p.max_norm, p.eps, p.grad_scale = max_norm, eps, grad_scale
-        with _on(self.device) as stream:
-            call(self.ctx, p, self._results_at, at, stream)
+        _call_on(self.device, call, self.ctx, p, self._results_at, at)
         if grads is not None:
             self.grads = grads
         return self.total_norm, self.coef, self.tensor_norms
@@ -590,8 +583,7 @@ def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
     elif out_dtype is not None and out.dtype != out_dtype:
         raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
     e, device = _embed_args(table, "table", out, "out", ids, scale)
-    with _on(device) as stream:
-        came_embed_forward(e, device.index, stream)
+    _call_on(device, came_embed_forward, e, device.index)
     return out
 
 
@@ -609,11 +601,10 @@ def embed_backward(grad_out, ids, grad, scale: float = 1.0, padding_row: Optiona
     if padding_row is not None:
         e.flags |= CAME_EMBED_PADDING_ROW
         e.padding_row = padding_row
-    with _on(device) as stream:
-        size = came_embed_workspace(e)
-        # from torch's allocator, on the stream of the call: kept from reuse until the call is done
-        ws = grad_out.new_empty(-(-size // 4), dtype=_torch().float32)
-        came_embed_backward(e, ws.data_ptr(), size, device.index, stream)
+    size = came_embed_workspace(e)
+    # from torch's allocator, for the device's current stream: not reused before the call is done
+    ws = grad_out.new_empty(-(-size // 4), dtype=_torch().float32)
+    _call_on(device, came_embed_backward, e, ws.data_ptr(), size, device.index)
     return grad
 
 

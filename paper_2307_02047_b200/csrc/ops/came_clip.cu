@@ -23,6 +23,7 @@ using namespace came_ops;
 
 constexpr int kThreads = 256;
 constexpr int kUnroll = 4;               // 32-byte loads in flight per thread
+constexpr int kFlatTiles = 512, kFlatTensors = 64;
 
 struct ClipTensor {
     const void* g;
@@ -153,53 +154,97 @@ __device__ __forceinline__ double tile_squares(const ClipTensor& d, int index)
     return wide;
 }
 
+__device__ __forceinline__ void store_total(double sum, const ClipConsts& hc, float* results)
+{
+    const double norm = fabs(hc.scale) * sqrt(sum);
+    const double reach = norm + hc.eps;
+    results[0] = static_cast<float>(norm);
+    results[1] = static_cast<float>(reach <= hc.max_norm ? 1.0 : hc.max_norm / reach);   // NaN stays NaN
+}
+
+// A warp's sum of count values that other blocks have written.
+__device__ __forceinline__ double warp_sum_of(const double* p, int count, int lane)
+{
+    double s = 0.0;
+#pragma unroll 4
+    for (int k = lane; k < count; k += 32) s += __ldcg(p + k);
+    return warp_sum(s);
+}
+
+// kFlat: one count of arrivals, and the last block finishes everything, a warp per tensor.  It
+// saves a round of store, fence and atomic (1.5 us of a small call), but one block reads
+// all partial sums: for lists of up to kFlatTiles tiles.  Else the last tile of each tensor adds the
+// tensor's sums, and the last tensor the tensors'.
+template <bool kFlat>
 __global__ void __launch_bounds__(kThreads)
 k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles, int n, ClipWork w,
             ClipConsts hc, float* __restrict__ results)
 {
     __shared__ double red[kThreads / 32];
+    __shared__ unsigned s_last;
     release_dependents();
     const ClipTile t = tiles[blockIdx.x];
     const ClipTensor d = T[t.tensor];
     double s = d.g_bf16 ? tile_squares<__nv_bfloat16>(d, t.index) : tile_squares<float>(d, t.index);
     s = warp_sum(s);
-    const int lane = threadIdx.x & 31;
-    if (lane == 0) red[threadIdx.x >> 5] = s;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lane == 0) red[warp] = s;
     __syncthreads();
-    if (threadIdx.x >= 32) return;
-    // from here on one warp: arrive, and finish the tensor / the whole list when last
-    unsigned last = 0;
-    if (lane == 0) {
-        s = 0.0;
-        for (int k = 0; k < kThreads / 32; ++k) s += red[k];
-        w.tile_sum[blockIdx.x] = s;
-        __threadfence();
-        last = atomicAdd(&w.arrived[t.tensor], 1u) == static_cast<unsigned>(d.ntiles - 1);
-        __threadfence();
-    }
-    if (!__shfl_sync(0xffffffffu, last, 0)) return;
-    s = 0.0;
-    for (int k = lane; k < d.ntiles; k += 32) s += __ldcg(w.tile_sum + d.tile0 + k);
-    s = warp_sum(s);
     const double scale = fabs(hc.scale);
-    if (lane == 0) {
-        w.arrived[t.tensor] = 0u;
-        w.tensor_sum[t.tensor] = s;
-        results[2 + t.tensor] = static_cast<float>(scale * sqrt(s));
-        __threadfence();
-        last = atomicAdd(&w.arrived[n], 1u) == static_cast<unsigned>(n - 1);
-        __threadfence();
-    }
-    if (!__shfl_sync(0xffffffffu, last, 0)) return;
-    s = 0.0;
-    for (int k = lane; k < n; k += 32) s += __ldcg(w.tensor_sum + k);
-    s = warp_sum(s);
-    if (lane == 0) {
-        w.arrived[n] = 0u;
-        const double norm = scale * sqrt(s);
-        const double reach = norm + hc.eps;
-        results[0] = static_cast<float>(norm);
-        results[1] = static_cast<float>(reach <= hc.max_norm ? 1.0 : hc.max_norm / reach);   // NaN stays NaN
+    if constexpr (kFlat) {
+        if (threadIdx.x == 0) {
+            s = 0.0;
+            for (int k = 0; k < kThreads / 32; ++k) s += red[k];
+            w.tile_sum[blockIdx.x] = s;
+            __threadfence();
+            s_last = atomicAdd(&w.arrived[n], 1u) == gridDim.x - 1u;
+            __threadfence();
+        }
+        __syncthreads();
+        if (!s_last) return;
+        double total = 0.0;                              // of this warp's tensors, in their order
+        for (int k = warp; k < n; k += kThreads / 32) {
+            const int tile0 = T[k].tile0, ntiles = T[k].ntiles;
+            s = warp_sum_of(w.tile_sum + tile0, ntiles, lane);
+            if (lane == 0) results[2 + k] = static_cast<float>(scale * sqrt(s));
+            total += s;
+        }
+        if (lane == 0) red[warp] = total;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            w.arrived[n] = 0u;
+            s = 0.0;
+            for (int k = 0; k < kThreads / 32; ++k) s += red[k];
+            store_total(s, hc, results);
+        }
+    } else {
+        if (warp > 0) return;
+        // one warp: arrive, and finish the tensor / the whole list when last
+        unsigned last = 0;
+        if (lane == 0) {
+            s = 0.0;
+            for (int k = 0; k < kThreads / 32; ++k) s += red[k];
+            w.tile_sum[blockIdx.x] = s;
+            __threadfence();
+            last = atomicAdd(&w.arrived[t.tensor], 1u) == static_cast<unsigned>(d.ntiles - 1);
+            __threadfence();
+        }
+        if (!__shfl_sync(0xffffffffu, last, 0)) return;
+        s = warp_sum_of(w.tile_sum + d.tile0, d.ntiles, lane);
+        if (lane == 0) {
+            w.arrived[t.tensor] = 0u;
+            w.tensor_sum[t.tensor] = s;
+            results[2 + t.tensor] = static_cast<float>(scale * sqrt(s));
+            __threadfence();
+            last = atomicAdd(&w.arrived[n], 1u) == static_cast<unsigned>(n - 1);
+            __threadfence();
+        }
+        if (!__shfl_sync(0xffffffffu, last, 0)) return;
+        s = warp_sum_of(w.tensor_sum, n, lane);
+        if (lane == 0) {
+            w.arrived[n] = 0u;
+            store_total(s, hc, results);
+        }
     }
 }
 
@@ -435,7 +480,10 @@ came_status run_clip(came_clip_ctx* c, const came_clip_params* p, const void* co
     if (grads && (s = rebind(c, grads, stream)) != CAME_OK) return s;
     const double scale = p->grad_scale == 0.0 ? 1.0 : p->grad_scale;
     const ClipConsts hc{p->max_norm, p->eps, scale};
-    k_clip_norm<<<c->ntiles, kThreads, 0, stream>>>(c->d_table, c->d_tiles, c->n, c->work, hc, results);
+    if (c->ntiles <= kFlatTiles && c->n <= kFlatTensors)
+        k_clip_norm<true><<<c->ntiles, kThreads, 0, stream>>>(c->d_table, c->d_tiles, c->n, c->work, hc, results);
+    else
+        k_clip_norm<false><<<c->ntiles, kThreads, 0, stream>>>(c->d_table, c->d_tiles, c->n, c->work, hc, results);
     if (apply) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(static_cast<unsigned>(c->ntiles));

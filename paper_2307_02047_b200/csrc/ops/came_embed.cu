@@ -811,7 +811,7 @@ cudaError_t launch_dependent(K kernel, bool early, long long blocks, int threads
 }
 
 template <typename I>
-cudaError_t launch_sort(const came_embed& e, const SortArgs& a, cudaStream_t stream)
+cudaError_t launch_sort(const came_embed& e, const SortArgs& a, int32_t device, cudaStream_t stream)
 {
     const I* const ids = static_cast<const I*>(e.ids);
     if (e.tokens <= kFewTokens && a.rows < kFewRows) {
@@ -819,14 +819,14 @@ cudaError_t launch_sort(const came_embed& e, const SortArgs& a, cudaStream_t str
         return cudaGetLastError();
     }
     if (e.tokens <= kOneTokens) {
-        const cudaError_t err = cudaFuncSetAttribute(k_embed_sort_one<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                     static_cast<int>(kOneBytes));
+        static std::atomic<uint64_t> done{0};
+        const cudaError_t err = allow_smem(k_embed_sort_one<I>, kOneBytes, device, done);
         if (err != cudaSuccess) return err;
         k_embed_sort_one<I><<<1, kSortThreads, kOneBytes, stream>>>(ids, a);
         return cudaGetLastError();
     }
-    cudaError_t err = cudaFuncSetAttribute(k_embed_move<I>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           static_cast<int>(kHistBytes));
+    static std::atomic<uint64_t> done{0};
+    cudaError_t err = allow_smem(k_embed_move<I>, kHistBytes, device, done);
     if (err != cudaSuccess) return err;
     k_embed_count<I><<<a.blocks, kSortThreads, 0, stream>>>(ids, a);
     for (int pass = 0; pass < a.passes && err == cudaSuccess; ++pass)
@@ -936,7 +936,8 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     if (e->tokens == 0 && t.accumulate) return CAME_OK;
     cudaError_t err = cudaSuccess;
     if (e->tokens > 0)
-        err = e->id_dtype == CAME_I64 ? launch_sort<long long>(*e, a, stream) : launch_sort<int>(*e, a, stream);
+        err = e->id_dtype == CAME_I64 ? launch_sort<long long>(*e, a, device, stream)
+                                       : launch_sort<int>(*e, a, device, stream);
     if (err != cudaSuccess) return report_cuda(err, "kernel launch(sort)");
     using bf16 = __nv_bfloat16;
     const long long blocks = l.blocks * l.slices;

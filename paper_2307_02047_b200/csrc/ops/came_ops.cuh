@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace came_ops {
 
 // Text for came_last_error(NULL) on the calling thread; returns `s`.  Defined with the step's API.
@@ -18,6 +20,17 @@ came_status require_current_device(int32_t device);
 inline bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline size_t dtype_bytes(int32_t dt) { return dt == CAME_BF16 ? 2 : 4; }
 inline bool known_dtype(int32_t dt) { return dt == CAME_F32 || dt == CAME_BF16; }
+
+// Lets `kernel` use `bytes` of dynamic shared memory; the runtime is asked once per device.
+template <typename K>
+inline cudaError_t allow_smem(K kernel, size_t bytes, int32_t device, std::atomic<uint64_t>& done)
+{
+    const uint64_t bit = device < 64 ? 1ull << device : 0ull;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 __device__ __forceinline__ float to_float(float x) { return x; }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
