@@ -398,9 +398,9 @@ typedef struct {
     void*       table;        /* DEVICE table_dtype [rows][table_ld]: W (read) or dW (written) */
     void*       data;         /* DEVICE data_dtype [tokens][data_ld]: out (written) or dY (read) */
     const void* ids;          /* DEVICE id_dtype [tokens]                                    */
-    int64_t     rows, cols;   /* >= 1                                                        */
-    int64_t     tokens;       /* >= 0 (data and ids may then be NULL)                        */
-    int64_t     table_ld, data_ld;      /* elements from row to row, >= cols                 */
+    int64_t     rows, cols;   /* >= 1; rows < 2^31 - 1, cols <= 2^29                         */
+    int64_t     tokens;       /* 0 (data and ids may then be NULL) .. 2^31 - 1               */
+    int64_t     table_ld, data_ld;      /* elements from row to row, cols .. 2^29            */
     int64_t     padding_row;  /* used with CAME_EMBED_PADDING_ROW                            */
     double      scale;        /* finite                                                      */
     int32_t     table_dtype, data_dtype;   /* came_dtype                                     */

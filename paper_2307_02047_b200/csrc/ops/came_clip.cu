@@ -76,11 +76,9 @@ template <> struct Pack<__nv_bfloat16> {
     __device__ __forceinline__ void add_squares(float (&a)[4]) const
     {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float lo = __uint_as_float(w[j] << 16), hi = __uint_as_float(w[j] & 0xffff0000u);
-            a[(2 * j) & 3] = fmaf(lo, lo, a[(2 * j) & 3]);
-            a[(2 * j + 1) & 3] = fmaf(hi, hi, a[(2 * j + 1) & 3]);
-        }
+        for (int j = 0; j < 8; ++j)                      // bf16 factors, fp32 sum, without unpacking
+            asm("{ .reg .b16 l, h; mov.b32 {l, h}, %2; fma.rn.f32.bf16 %0, l, l, %0; fma.rn.f32.bf16 %1, h, h, %1; }"
+                : "+f"(a[(2 * j) & 3]), "+f"(a[(2 * j + 1) & 3]) : "r"(w[j]));
     }
 };
 
@@ -196,9 +194,9 @@ k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles
             s = 0.0;
             for (int k = 0; k < kThreads / 32; ++k) s += red[k];
             w.tile_sum[blockIdx.x] = s;
-            __threadfence();
+            publish();
             s_last = atomicAdd(&w.arrived[n], 1u) == gridDim.x - 1u;
-            __threadfence();
+            publish();
         }
         __syncthreads();
         if (!s_last) return;
@@ -225,9 +223,9 @@ k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles
             s = 0.0;
             for (int k = 0; k < kThreads / 32; ++k) s += red[k];
             w.tile_sum[blockIdx.x] = s;
-            __threadfence();
+            publish();
             last = atomicAdd(&w.arrived[t.tensor], 1u) == static_cast<unsigned>(d.ntiles - 1);
-            __threadfence();
+            publish();
         }
         if (!__shfl_sync(0xffffffffu, last, 0)) return;
         s = warp_sum_of(w.tile_sum + d.tile0, d.ntiles, lane);
@@ -235,9 +233,9 @@ k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles
             w.arrived[t.tensor] = 0u;
             w.tensor_sum[t.tensor] = s;
             results[2 + t.tensor] = static_cast<float>(scale * sqrt(s));
-            __threadfence();
+            publish();
             last = atomicAdd(&w.arrived[n], 1u) == static_cast<unsigned>(n - 1);
-            __threadfence();
+            publish();
         }
         if (!__shfl_sync(0xffffffffu, last, 0)) return;
         s = warp_sum_of(w.tensor_sum, n, lane);

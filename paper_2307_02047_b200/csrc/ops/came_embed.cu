@@ -8,9 +8,13 @@
 // bit-reproducible.
 #include "came_ops.cuh"
 
+#include <cooperative_groups.h>
+
 #include <algorithm>
 #include <cmath>
 #include <cstdio>
+
+namespace cg = cooperative_groups;
 
 namespace {
 
@@ -18,7 +22,8 @@ using namespace came_ops;
 
 constexpr int kSlice = 256;              // columns one warp works on: 8 per lane
 
-// EV consecutive elements as they are stored: one access of EV * sizeof(T) bytes.
+// EV consecutive elements as they are stored: one access of EV * sizeof(T) bytes.  (Volatile, so
+// that the loads of a batch stay together in front of what uses them.)
 template <int EV, typename T>
 struct Raw {
     static constexpr int B = EV * static_cast<int>(sizeof(T));
@@ -32,15 +37,30 @@ struct Raw {
                          : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]),
                            "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
         } else if constexpr (B == 16) {
-            const uint4 v = *reinterpret_cast<const uint4*>(p);
-            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            asm volatile("ld.global.v4.b32 {%0,%1,%2,%3}, [%4];"
+                         : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
         } else if constexpr (B == 8) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            w[0] = v.x; w[1] = v.y;
+            asm volatile("ld.global.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
         } else if constexpr (B == 4) {
-            w[0] = *reinterpret_cast<const uint32_t*>(p);
+            asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p));
         } else {
-            w[0] = *reinterpret_cast<const uint16_t*>(p);
+            uint16_t h;
+            asm volatile("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p));
+            w[0] = h;
+        }
+    }
+
+    // acc[k] += element k: for bf16 the addition that widens one operand, without unpacking
+    __device__ __forceinline__ void add_to(float* acc) const
+    {
+#pragma unroll
+        for (int k = 0; k < EV; ++k) {
+            if constexpr (sizeof(T) == 4) {
+                acc[k] += __uint_as_float(w[k]);
+            } else {
+                const uint16_t h = static_cast<uint16_t>(k & 1 ? w[k >> 1] >> 16 : w[k >> 1] & 0xffffu);
+                asm("add.rn.f32.bf16 %0, %1, %0;" : "+f"(acc[k]) : "h"(h));
+            }
         }
     }
 
@@ -72,6 +92,22 @@ __device__ __forceinline__ void store_ev(T* p, const float* x)
         else *reinterpret_cast<uint32_t*>(p) = w[0];
     } else {
         *p = from_float<T>(x[0]);
+    }
+}
+
+// p[k] += x[k], EV consecutive fp32
+template <int EV>
+__device__ __forceinline__ void reduce_ev(float* p, const float* x)
+{
+    if constexpr (EV >= 4) {
+#pragma unroll
+        for (int k = 0; k < EV; k += 4)
+            asm volatile("red.global.add.v4.f32 [%0], {%1, %2, %3, %4};"
+                         :: "l"(p + k), "f"(x[k]), "f"(x[k + 1]), "f"(x[k + 2]), "f"(x[k + 3]) : "memory");
+    } else if constexpr (EV == 2) {
+        asm volatile("red.global.add.v2.f32 [%0], {%1, %2};" :: "l"(p), "f"(x[0]), "f"(x[1]) : "memory");
+    } else {
+        asm volatile("red.global.add.f32 [%0], %1;" :: "l"(p), "f"(x[0]) : "memory");
     }
 }
 
@@ -137,7 +173,10 @@ constexpr int kMaxPasses = 4;            // keys below 2^31 in digits of 8 bits
 constexpr int kFewTokens = 512;          // up to here every token counts the tokens before it
 constexpr unsigned kFewRows = 1u << 22;  // (key and position then fit one word)
 constexpr int kOneTokens = 4096;         // up to here one block sorts in its shared memory
-constexpr int kSortBlocks = 148;         // beyond that one block per SM at most
+constexpr int kMoveThreads = 512;        // beyond that a grid of blocks that leave room for others on their SM
+constexpr int kMoveWarps = kMoveThreads / 32;
+constexpr int kMoveTile = 1024;          // tokens per block, or a multiple of it ...
+constexpr int kMoveBlocks = 148;         // ... so that there are no more blocks than SMs
 constexpr size_t kHistBytes = sizeof(unsigned) * kSortWarps * kMaxBins;
 constexpr size_t kOneBytes = kHistBytes + sizeof(uint2) * kOneTokens;
 
@@ -151,7 +190,8 @@ struct SortArgs {
     int       digit_bits, passes, blocks;
 };
 
-// Exclusive sum over the block's threads (kSortThreads of them); `totals` has room for a warp.
+// Exclusive sum over the block's WARPS warps; `totals` has room for a warp.
+template <int WARPS>
 __device__ __forceinline__ unsigned block_exclusive_scan(unsigned v, unsigned* totals)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -166,7 +206,7 @@ __device__ __forceinline__ unsigned block_exclusive_scan(unsigned v, unsigned* t
     const unsigned s = warp_scan(v);
     if (lane == 31) totals[warp] = s;
     __syncthreads();
-    const unsigned t = totals[lane], upto = warp_scan(t);
+    const unsigned t = lane < WARPS ? totals[lane] : 0u, upto = warp_scan(t);
     return __shfl_sync(0xffffffffu, upto - t, warp) + s - v;
 }
 
@@ -206,16 +246,17 @@ __device__ __forceinline__ unsigned rank_and_count(unsigned digit, bool in, int 
 }
 
 // hist[warp][digit] becomes the count in the warps before; returns the block's count of digit tid.
+template <int WARPS>
 __device__ __forceinline__ unsigned sum_over_warps(unsigned* hist, int bins)
 {
     unsigned s = 0;
     if (static_cast<int>(threadIdx.x) < bins) {
-        unsigned v[kSortWarps];
+        unsigned v[WARPS];
 #pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) v[w] = hist[w * kMaxBins + threadIdx.x];
+        for (int w = 0; w < WARPS; ++w) v[w] = hist[w * bins + threadIdx.x];
 #pragma unroll
-        for (int w = 0; w < kSortWarps; ++w) {
-            hist[w * kMaxBins + threadIdx.x] = s;
+        for (int w = 0; w < WARPS; ++w) {
+            hist[w * bins + threadIdx.x] = s;
             s += v[w];
         }
     }
@@ -258,7 +299,7 @@ k_embed_sort_one(const I* __restrict__ ids, SortArgs a)
     for (long long k = tid; k < a.n_arrived; k += kSortThreads) a.arrived[k] = 0u;
     const int per = (n + kSortThreads - 1) / kSortThreads * 32;
     const int begin = min(n, warp * per), end = min(n, begin + per);
-    unsigned* const mine = hist + warp * kMaxBins;
+    unsigned* const mine = hist + warp * bins;
     uint2 pair[kRounds];
     unsigned rank[kRounds];
 #pragma unroll
@@ -283,7 +324,7 @@ k_embed_sort_one(const I* __restrict__ ids, SortArgs a)
             rank[r] = rank_and_count(pair[r].x >> shift & (bins - 1), begin + r * 32 + lane < end, a.digit_bits, mine);
         }
         __syncthreads();
-        const unsigned first = block_exclusive_scan(sum_over_warps(hist, bins), scan_totals);
+        const unsigned first = block_exclusive_scan<kSortWarps>(sum_over_warps<kSortWarps>(hist, bins), scan_totals);
         if (tid < bins) base[tid] = first;
         __syncthreads();
 #pragma unroll
@@ -300,60 +341,47 @@ k_embed_sort_one(const I* __restrict__ ids, SortArgs a)
 // More tokens: a counting grid, then one moving grid per digit.  Block b has the tokens (in the
 // order of the pass's input) from b * tile on.
 template <typename I>
-__global__ void __launch_bounds__(kSortThreads)
+__global__ void __launch_bounds__(kMoveThreads)
 k_embed_count(const I* __restrict__ ids, SortArgs a)
 {
     __shared__ unsigned count[kMaxBins];
     release_dependents();
     const int tid = threadIdx.x, bins = 1 << a.digit_bits;
-    const long long at = static_cast<long long>(blockIdx.x) * kSortThreads + tid;
-    const long long all = static_cast<long long>(a.blocks) * kSortThreads;
+    const long long at = static_cast<long long>(blockIdx.x) * kMoveThreads + tid;
+    const long long all = static_cast<long long>(a.blocks) * kMoveThreads;
     for (long long k = at; k < a.n_arrived; k += all) a.arrived[k] = 0u;
     // the moving grids count the digits of the pass after theirs
     for (int pass = 1; pass < a.passes; ++pass)
-        for (int k = tid; k < bins; k += kSortThreads) a.count[pass][static_cast<long long>(blockIdx.x) * bins + k] = 0u;
+        for (int k = tid; k < bins; k += kMoveThreads) a.count[pass][static_cast<long long>(blockIdx.x) * bins + k] = 0u;
     if (tid < bins) count[tid] = 0u;
     __syncthreads();
     const long long begin = static_cast<long long>(blockIdx.x) * a.tile, end = min(a.tokens, begin + a.tile);
 #pragma unroll 4
-    for (long long k = begin + tid; k < end; k += kSortThreads) atomicAdd(&count[key_of(ids[k], a) & (bins - 1)], 1u);
+    for (long long k = begin + tid; k < end; k += kMoveThreads) atomicAdd(&count[key_of(ids[k], a) & (bins - 1)], 1u);
     __syncthreads();
     if (tid < bins) a.count[0][static_cast<long long>(blockIdx.x) * bins + tid] = count[tid];
 }
 
 template <typename I>
-__global__ void __launch_bounds__(kSortThreads)
+__global__ void __launch_bounds__(kMoveThreads)
 k_embed_move(const I* __restrict__ ids, SortArgs a, int pass)
 {
     constexpr int kRounds = 4;                           // elements per lane that are loaded at once
     extern __shared__ __align__(16) unsigned hist[];     // [warp][digit]
-    __shared__ unsigned sum_before[kSortThreads], sum_all[kSortThreads], base[kMaxBins], scan_totals[32];
+    __shared__ uint4 sum_before[kMoveThreads], sum_all[kMoveThreads];      // [part of the blocks][digits]
+    __shared__ unsigned base[kMaxBins], scan_totals[32];
     release_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int bins = 1 << a.digit_bits, shift = pass * a.digit_bits, me = static_cast<int>(blockIdx.x);
     const int to_buffer = (a.passes - 1 - pass) & 1;
     const uint2* const src = a.pair[to_buffer ^ 1];
     uint2* const dst = a.pair[to_buffer];
-    const long long per = a.tile / kSortWarps;
+    const long long per = a.tile / kMoveWarps;
     const long long begin = min(a.tokens, static_cast<long long>(me) * a.tile + warp * per);
     const long long end = min(a.tokens, begin + per);
-    unsigned* const mine = hist + warp * kMaxBins;
+    unsigned* const mine = hist + warp * bins;
     for (int k = lane; k < bins; k += 32) mine[k] = 0u;
     wait_for_previous_grid();
-    // digit tid % bins: all of it, and what the blocks before this one have (bins divides the threads)
-    {
-        const unsigned* const count = a.count[pass];
-        const int digit = tid & (bins - 1), step = kSortThreads >> a.digit_bits;
-        unsigned before = 0, all = 0;
-#pragma unroll 8
-        for (int b = tid >> a.digit_bits; b < a.blocks; b += step) {
-            const unsigned v = __ldcg(count + static_cast<long long>(b) * bins + digit);
-            all += v;
-            if (b < me) before += v;
-        }
-        sum_before[tid] = before;
-        sum_all[tid] = all;
-    }
     uint2 pair[kRounds];
     unsigned rank[kRounds];
     auto load = [&](long long at) {
@@ -372,20 +400,36 @@ k_embed_move(const I* __restrict__ ids, SortArgs a, int pass)
         }
     };
     const bool kept = per <= 32 * kRounds;               // a warp's run fits its registers
+    load(begin);
+    // four neighbouring digits per thread: all of them, and what the blocks before this one have
+    {
+        const int quads = bins >> 2, quad = tid & (quads - 1), step = kMoveThreads / quads;
+        const uint4* const count = reinterpret_cast<const uint4*>(a.count[pass]) + quad;
+        uint4 before = make_uint4(0u, 0u, 0u, 0u), all = before;
+#pragma unroll 8
+        for (int b = tid / quads; b < a.blocks; b += step) {
+            const uint4 v = __ldcg(count + static_cast<long long>(b) * quads);
+            all.x += v.x; all.y += v.y; all.z += v.z; all.w += v.w;
+            if (b < me) { before.x += v.x; before.y += v.y; before.z += v.z; before.w += v.w; }
+        }
+        sum_before[tid] = before;
+        sum_all[tid] = all;
+    }
     __syncwarp();
     for (long long at = begin; at < end; at += 32 * kRounds) {
-        load(at);
+        if (at > begin) load(at);
         count_ranks(at);
     }
     __syncthreads();
-    sum_over_warps(hist, bins);
+    sum_over_warps<kMoveWarps>(hist, bins);
     unsigned before = 0, all = 0;
     if (tid < bins)
-        for (int k = tid; k < kSortThreads; k += bins) {
-            before += sum_before[k];
-            all += sum_all[k];
+#pragma unroll 8
+        for (int k = tid; k < 4 * kMoveThreads; k += bins) {
+            before += reinterpret_cast<const unsigned*>(sum_before)[k];
+            all += reinterpret_cast<const unsigned*>(sum_all)[k];
         }
-    const unsigned first = block_exclusive_scan(all, scan_totals);
+    const unsigned first = block_exclusive_scan<kMoveWarps>(all, scan_totals);
     if (tid < bins) base[tid] = first + before;
     __syncthreads();
     for (long long at = begin; at < end; at += 32 * kRounds) {
@@ -415,8 +459,8 @@ k_embed_move(const I* __restrict__ ids, SortArgs a, int pass)
 // The first zero_blocks blocks write the rows without tokens instead.  They need the ids only, so
 // they do not wait for the sort: the zeros are written while it runs.
 constexpr int kSumWarps = 8;
-constexpr int kZeroBlocks = 256;
-constexpr int kZeroWords = 4096;         // bits of rows per round: 131072
+constexpr int kClusterBlocks = 8, kZeroClusters = 64, kZeroBlocks = kClusterBlocks * kZeroClusters;
+constexpr int kZeroWords = 2048;         // of the bit map: 65536 of a cluster's rows per round
 enum : int { kLinkHead = 1, kLinkTail = 2, kLinkThrough = 4 };
 
 struct SumArgs {
@@ -424,10 +468,13 @@ struct SumArgs {
     float*    part;            // [blocks of tokens][2][slices][kSlice]: 0 = run from before, 1 = run that goes on
     unsigned* arrived;         // [blocks of tokens][slices]
     const void* ids;
-    long long tokens, cols, dy_ld, grad_ld;
+    long long tokens, cols, grad_ld;
+    unsigned  dy_bytes;        // from row to row of dY
     unsigned  rows, padding;
     int       slices, per_warp, accumulate, id64;
-    int       zero_blocks;     // 0 or a power of two
+    int       zero_blocks;     // 0 or kZeroBlocks
+    int       zero_group;      // log2 of the neighbouring rows a cluster takes at once
+    unsigned  sum_blocks;      // the grid is rounded up to whole clusters
     float     scale;
 };
 
@@ -440,14 +487,20 @@ __device__ __forceinline__ void store_row(const SumArgs& a, O* grad, unsigned ro
         const long long c = column<EV>(slice, g, lane);
         if (c >= a.cols) continue;
         float y[EV];
+#pragma unroll
+        for (int k = 0; k < EV; ++k) y[k] = a.scale * sum[g * EV + k];
         if (a.accumulate) {
-            Raw<EV, O> old;
-            old.load(dst + c);
+            if constexpr (sizeof(O) == 4) {
+                // The only addition to these elements in the whole call, so its order cannot matter;
+                // done in the L2, it keeps the warp from waiting for the old value.
+                reduce_ev<EV>(dst + c, y);
+                continue;
+            } else {
+                Raw<EV, O> old;
+                old.load(dst + c);
 #pragma unroll
-            for (int k = 0; k < EV; ++k) y[k] = fmaf(a.scale, sum[g * EV + k], old.value(k));
-        } else {
-#pragma unroll
-            for (int k = 0; k < EV; ++k) y[k] = a.scale * sum[g * EV + k];
+                for (int k = 0; k < EV; ++k) y[k] += old.value(k);
+            }
         }
         store_ev<EV, O>(dst + c, y);
     }
@@ -482,13 +535,13 @@ __device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned 
         last += found ? __ffs(found) : 32;
         ends = found != 0;
     }
-    __threadfence();
+    publish();
     __syncwarp();
     unsigned final = 0;
     if (lane == 0)
         final = atomicAdd(&a.arrived[static_cast<long long>(first) * a.slices + slice], 1u) == static_cast<unsigned>(last - first);
     if (!__shfl_sync(0xffffffffu, final, 0)) return;
-    __threadfence();
+    publish();
     float total[8];
     {
         const float* const p = at(first, 1);
@@ -511,37 +564,48 @@ __device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned 
     store_row<O, EV>(a, grad, row, slice, lane, total);
 }
 
-// Block `own` of zero_blocks: the rows r = own mod zero_blocks (frequent ids are neighbours in
-// most vocabularies: this spreads them), marked in a bit map when a token has them, else zeroed.
+// Cluster c of kZeroClusters takes every kZeroClusters-th group of 2^group rows (frequent ids are
+// neighbours in most vocabularies: this spreads them).  Its blocks share the reading of the ids: each
+// marks what its part of them touches in a bit map of the cluster's rows, then takes the
+// rows that no block has marked, every kClusterBlocks-th group of them, and zeroes them.
+//   cluster = (r >> group) mod kZeroClusters,   bit = (r >> group) / kZeroClusters << group | r mod 2^group
+// (Every block reading all ids for itself cost 70 us at 131072 tokens.)
 template <typename I, typename O, int EV>
 __device__ __forceinline__ void zero_rows(const I* __restrict__ ids, O* __restrict__ grad, const SumArgs& a, unsigned* seen)
 {
-    constexpr int kPer = 16 / static_cast<int>(sizeof(I)), kBatch = 8;       // 16-byte loads, eight at a time
+    constexpr int kPer = 16 / static_cast<int>(sizeof(I)), kBatch = 4;       // 16-byte loads, four at a time
     constexpr int kThreads = kSumWarps * 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned own = blockIdx.x, mask = static_cast<unsigned>(a.zero_blocks) - 1u;
-    const int shift = __popc(mask);
-    const unsigned owned = own < a.rows ? ((a.rows - 1u - own) >> shift) + 1u : 0u;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, me = static_cast<int>(cluster.block_rank()), group = a.zero_group;
+    const unsigned own = blockIdx.x / kClusterBlocks;
+    const unsigned inner = (1u << group) - 1u, mine = own << group, filter = (kZeroClusters - 1u) << group;
+    // bits up to the last group of this cluster; rows behind the table's end are left out below
+    const unsigned groups = ((a.rows - 1u) >> group) + 1u;
+    const unsigned bits = own < groups ? ((groups - 1u - own) / kZeroClusters + 1u) << group : 0u;
     // the ids from the first 16-byte boundary on go in whole loads, the others one by one
     const long long lead = min(a.tokens, static_cast<long long>((16 - reinterpret_cast<uintptr_t>(ids) % 16) % 16 / sizeof(I)));
     const long long whole = (a.tokens - lead) / kPer;
+    const uint4* const packs = reinterpret_cast<const uint4*>(ids + lead);
+    const int per_row = EV * 32 <= a.cols ? 32 : 1 << (32 - __clz(static_cast<int>((a.cols + EV - 1) / EV - 1)));  // lanes
     const float zeros[EV] = {};
-    for (unsigned first = 0; first < owned; first += kZeroWords * 32u) {
-        const unsigned count = min(owned - first, kZeroWords * 32u);
+    for (unsigned first = 0; first < bits; first += kZeroWords * 32u) {
+        const unsigned count = min(bits - first, kZeroWords * 32u);
         for (unsigned k = tid; k < (count + 31u) / 32u; k += kThreads) seen[k] = 0u;
         __syncthreads();
         auto mark = [&](I raw) {
+            if ((static_cast<unsigned>(raw) & filter) != mine) return;
             const long long id = static_cast<long long>(raw);
-            if (id < 0 || id >= a.rows || (static_cast<unsigned>(id) & mask) != own || id == a.padding) return;
-            const unsigned bit = (static_cast<unsigned>(id) >> shift) - first;
+            if (id < 0 || id >= a.rows || id == a.padding) return;
+            const unsigned r = static_cast<unsigned>(id), bit = ((r >> group) / kZeroClusters << group | (r & inner)) - first;
             if (bit < count && !(seen[bit >> 5] >> (bit & 31u) & 1u)) atomicOr(&seen[bit >> 5], 1u << (bit & 31u));
         };
-        for (long long k = tid; k < whole; k += kBatch * kThreads) {
+        for (long long k = me * kThreads + tid; k < whole; k += kBatch * kClusterBlocks * kThreads) {
             uint4 w[kBatch];
 #pragma unroll
-            for (int u = 0; u < kBatch; ++u)
-                w[u] = k + u * kThreads < whole ? reinterpret_cast<const uint4*>(ids + lead)[k + u * kThreads]
-                                                : make_uint4(~0u, ~0u, ~0u, ~0u);        // -1: no row
+            for (int u = 0; u < kBatch; ++u) {
+                const long long q = k + u * (kClusterBlocks * kThreads);
+                w[u] = q < whole ? packs[q] : make_uint4(~0u, ~0u, ~0u, ~0u);            // -1: no row
+            }
 #pragma unroll
             for (int u = 0; u < kBatch; ++u) {
                 if constexpr (sizeof(I) == 4) {
@@ -553,24 +617,41 @@ __device__ __forceinline__ void zero_rows(const I* __restrict__ ids, O* __restri
                 }
             }
         }
-        if (tid < lead) mark(ids[tid]);
+        if (me == 0 && tid < lead) mark(ids[tid]);
         const long long rest = lead + whole * kPer + tid;
-        if (rest < a.tokens) mark(ids[rest]);
+        if (me == 0 && rest < a.tokens) mark(ids[rest]);
+        cluster.sync();
+        // every block's marks together
+        constexpr int kWords = kZeroWords / kThreads;
+        unsigned m[kWords] = {};
+#pragma unroll
+        for (int q = 0; q < kWords; ++q)
+            if (tid + q * kThreads < static_cast<int>((count + 31u) / 32u))
+#pragma unroll
+                for (int b = 0; b < kClusterBlocks; ++b) m[q] |= cluster.map_shared_rank(seen, b)[tid + q * kThreads];
+        cluster.sync();                                  // nobody overwrites, clears or leaves before all have read
+#pragma unroll
+        for (int q = 0; q < kWords; ++q) seen[tid + q * kThreads] = m[q];
         __syncthreads();
-        for (unsigned k = warp; k < count; k += kSumWarps) {
-            if (seen[k >> 5] >> (k & 31u) & 1u) continue;
-            O* const dst = grad + (static_cast<long long>(first + k) * (mask + 1u) + own) * a.grad_ld;
-            for (long long c = static_cast<long long>(lane) * EV; c < a.cols; c += 32 * EV) store_ev<EV, O>(dst + c, zeros);
+        const int rows_at_once = 32 / per_row;           // a warp's, where rows are shorter than its store
+        for (unsigned k = static_cast<unsigned>((warp * kClusterBlocks + me) * rows_at_once + lane / per_row); k < count;
+             k += kClusterBlocks * kSumWarps * rows_at_once) {
+            const unsigned bit = first + k;
+            const unsigned r = (((bit >> group) * kZeroClusters + own) << group) | (bit & inner);
+            if ((seen[k >> 5] >> (k & 31u) & 1u) || r >= a.rows) continue;
+            O* const dst = grad + static_cast<long long>(r) * a.grad_ld;
+            for (long long c = static_cast<long long>(lane & (per_row - 1)) * EV; c < a.cols; c += per_row * EV)
+                store_ev<EV, O>(dst + c, zeros);
         }
         __syncthreads();
     }
 }
 
 template <typename T, typename O, int EV>
-__global__ void __launch_bounds__(kSumWarps * 32)
+__global__ void __launch_bounds__(kSumWarps * 32, 4)
 k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
 {
-    constexpr int U = sizeof(T) == 2 ? 8 : 4;            // rows in flight: 8 * 16 or 4 * 32 bytes per lane
+    constexpr int U = sizeof(T) == 2 && EV > 1 ? 4 : 2;  // rows per batch
     __shared__ float part[kSumWarps][2][8][32];          // [warp][head, tail][element][lane]
     static_assert(sizeof(part) >= sizeof(unsigned) * kZeroWords, "the bit map takes the parts' place");
     __shared__ int link[kSumWarps];
@@ -582,21 +663,27 @@ k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
     }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const unsigned at = blockIdx.x - static_cast<unsigned>(a.zero_blocks);
+    if (at >= a.sum_blocks) return;
     const unsigned block = at / static_cast<unsigned>(a.slices);
     const int slice = static_cast<int>(at - block * static_cast<unsigned>(a.slices));
     const int K = a.per_warp;
     const long long p0 = (static_cast<long long>(block) * kSumWarps + warp) * K;
     wait_for_previous_grid();
 
-    const long long p = p0 + lane;
-    const bool in = lane < K && p < a.tokens;
-    const uint2 pair = in ? __ldcg(a.pair + p) : make_uint2(a.rows, 0u);
-    const unsigned key = pair.x, token = pair.y;
-    const int n = __popc(__ballot_sync(0xffffffffu, key < a.rows));          // keys that are rows come first
-    const unsigned key_first = __shfl_sync(0xffffffffu, key, 0);
-    const unsigned key_last = __shfl_sync(0xffffffffu, key, K - 1);
-    const bool head = n > 0 && p0 > 0 && __ldcg(&a.pair[p0 - 1].x) == key_first;
-    const bool tail = n == K && p0 + K < a.tokens && __ldcg(&a.pair[p0 + K].x) == key_last;
+    // The warp's tokens, a group of (up to) 32 at a time, a lane each; keys that are rows come first.
+    const int size = min(K, 32), groups = K / size;
+    auto group_at = [&](int m) {
+        const long long p = p0 + m * 32 + lane;
+        return m < groups && lane < size && p < a.tokens ? __ldcg(a.pair + p) : make_uint2(a.rows, 0u);
+    };
+    uint2 now = group_at(0), next = group_at(1);
+    const unsigned key_last = p0 + K <= a.tokens ? __ldcg(&a.pair[p0 + K - 1].x) : a.rows;
+    const unsigned key_before = p0 > 0 && p0 <= a.tokens ? __ldcg(&a.pair[p0 - 1].x) : a.rows;
+    const unsigned key_after = p0 + K < a.tokens ? __ldcg(&a.pair[p0 + K].x) : a.rows;
+    const unsigned key_first = __shfl_sync(0xffffffffu, now.x, 0);
+    const bool any = key_first < a.rows;
+    const bool head = any && key_before == key_first;
+    const bool tail = key_last < a.rows && key_after == key_last;
     const bool through = head && tail && key_first == key_last;
     if (lane == 0) link[warp] = (head ? kLinkHead : 0) | (tail ? kLinkTail : 0) | (through ? kLinkThrough : 0);
 
@@ -607,37 +694,69 @@ k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) part[warp][which][j][lane] = acc[j];
     };
-    unsigned current = key_first;
-    bool open_head = head;                               // the run being added began in an earlier warp
-    for (int k = 0; k < n; k += U) {
-        Raw<EV, T> x[U][8 / EV];
+    const int width = static_cast<int>(min(a.cols - slice * static_cast<long long>(kSlice), static_cast<long long>(kSlice))) - lane * EV;
+    const char* const column0 = reinterpret_cast<const char*>(dy + slice * static_cast<long long>(kSlice) + lane * EV);
+    int n = __popc(__ballot_sync(0xffffffffu, now.x < a.rows)), n_next = __popc(__ballot_sync(0xffffffffu, next.x < a.rows));
+    // Two batches of rows in registers: while one is added, the other is on its way.
+    Raw<EV, T> x[2][U][8 / EV];
+    auto fetch = [&](Raw<EV, T> (&to)[8 / EV], unsigned tokens, int k, int count) {
+        const T* const row = reinterpret_cast<const T*>(
+            column0 + static_cast<unsigned long long>(__shfl_sync(0xffffffffu, tokens, k)) * a.dy_bytes);
+        if (k < count)
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const unsigned t = __shfl_sync(0xffffffffu, token, (k + u) & 31);
+            for (int g = 0; g < 8 / EV; ++g)
+                if (g * (32 * EV) < width) to[g].load(row + g * (32 * EV));
+    };
+    auto add = [&](const Raw<EV, T> (&row)[8 / EV]) {
 #pragma unroll
-            for (int g = 0; g < 8 / EV; ++g) {
-                const long long c = column<EV>(slice, g, lane);
-                if (k + u < n && c < a.cols) x[u][g].load(dy + static_cast<long long>(t) * a.dy_ld + c);
-            }
-        }
+        for (int g = 0; g < 8 / EV; ++g) row[g].add_to(acc + g * EV);
+    };
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const unsigned v = __shfl_sync(0xffffffffu, key, (k + u) & 31);
-            if (k + u < n) {
-                if (v != current) {
-                    if (open_head) keep(0);
-                    else store_row<O, EV>(a, grad, current, slice, lane, acc);
-                    open_head = false;
-                    current = v;
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+        for (int u = 0; u < U; ++u) fetch(x[b][u], now.y, b * U + u, n);
+    unsigned current = key_first;                        // the run being added ...
+    bool open_head = head;                               // ... began in an earlier warp
+    for (int m = 0; n > 0;) {
+        unsigned left = __shfl_up_sync(0xffffffffu, now.x, 1);
+        if (lane == 0) left = current;
+        const unsigned starts = __ballot_sync(0xffffffffu, lane < n && now.x != left);   // bit k: token k begins a run
+        for (int k0 = 0; k0 < n; k0 += 2 * U) {
+            const bool last = k0 + 2 * U >= 32;          // what is fetched belongs to the next group
+            const unsigned tokens = last ? next.y : now.y;
+            const int count = last ? n_next : n;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                const int k = k0 + b * U;
+                if (k + U <= n && (starts >> k & ((1u << U) - 1u)) == 0u) {              // all of one run
+#pragma unroll
+                    for (int u = 0; u < U; ++u) add(x[b][u]);
+                } else {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        if (k + u >= n) break;
+                        if (starts >> (k + u) & 1u) {
+                            if (open_head) keep(0);
+                            else store_row<O, EV>(a, grad, current, slice, lane, acc);
+                            open_head = false;
+                            current = __shfl_sync(0xffffffffu, now.x, k + u);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) acc[j] = 0.f;
+                        }
+                        add(x[b][u]);
+                    }
                 }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) acc[j] += x[u][j / EV].value(j % EV);
+                for (int u = 0; u < U; ++u) fetch(x[b][u], tokens, (k + 2 * U + u) & 31, count);
             }
         }
+        if (++m >= groups) break;
+        now = next;
+        n = n_next;
+        next = group_at(m + 1);
+        n_next = __popc(__ballot_sync(0xffffffffu, next.x < a.rows));
     }
-    if (n > 0) {
+    if (any) {
         if (open_head) keep(0);                          // ends here, or goes through
         else if (tail) keep(1);
         else store_row<O, EV>(a, grad, current, slice, lane, acc);
@@ -674,12 +793,14 @@ k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
 
 inline long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
 
-// Sorted tokens per warp of the sums' grid: enough to cover the latency of a row's load, few
-// enough that there are several thousand warps.  Fixed by the sizes alone, as the order of the sums is.
+// Sorted tokens per warp of the sums' grid: many, so that few runs cross blocks (a crossing costs its
+// block about 3 us), but so few that there are 4000 to 16000 warps.  Measured: 128k tokens x 16 slices
+// 354 / 259 / 230 / 225 / 229 us at 8 / 16 / 32 / 64 / 128 per warp, 16k x 4 slices 37 / 36 / 38 / 42 / 52,
+// 2k x 4 slices 17 / 17 / 22 / 30 / 47.  Fixed by the sizes alone, as the order of the sums is.
 int tokens_per_warp(const came_embed& e)
 {
     const long long work = e.tokens * ceil_div(e.cols, kSlice);
-    return work >= 32 * 8192 ? 32 : work >= 16 * 8192 ? 16 : 8;
+    return work >= 1ll << 22 ? 128 : work >= 1ll << 20 ? 64 : work >= 1ll << 18 ? 32 : work >= 1ll << 16 ? 16 : 8;
 }
 
 struct Layout {
@@ -701,8 +822,8 @@ Layout layout(const came_embed& e)
     int bits = 1;
     while ((e.rows >> bits) != 0) ++bits;                 // the keys are 0 .. rows
     l.passes = static_cast<int>(ceil_div(bits, kMaxDigitBits));
-    l.digit_bits = static_cast<int>(ceil_div(bits, l.passes));
-    l.tile = static_cast<unsigned>(ceil_div(std::max<long long>(e.tokens, 1), kSortThreads * kSortBlocks) * kSortThreads);
+    l.digit_bits = std::max(2, static_cast<int>(ceil_div(bits, l.passes)));      // digits are counted four at a time
+    l.tile = static_cast<unsigned>(ceil_div(std::max<long long>(e.tokens, 1), kMoveTile * kMoveBlocks) * kMoveTile);
     l.sort_blocks = static_cast<int>(ceil_div(e.tokens, l.tile));
     for (int k = 0; k < 2; ++k) l.pair[k] = take(sizeof(uint2) * e.tokens);
     for (int k = 0; k < l.passes; ++k)
@@ -716,12 +837,14 @@ Layout layout(const came_embed& e)
 came_status validate_embed(const came_embed* e, bool backward)
 {
     if (!e) return report(CAME_ERR_NULL, "descriptor is NULL");
-    if (e->rows < 1 || e->rows >= (1ll << 31) - 1 || e->cols < 1 || e->cols >= (1ll << 31))
-        return report(CAME_ERR_SHAPE, "rows and cols must be >= 1 and below 2^31 - 1");
+    if (e->rows < 1 || e->rows >= (1ll << 31) - 1 || e->cols < 1 || e->cols > (1ll << 29))
+        return report(CAME_ERR_SHAPE, "rows must lie in [1, 2^31 - 2], cols in [1, 2^29]");
     if (e->tokens < 0 || e->tokens >= (1ll << 31)) return report(CAME_ERR_SHAPE, "tokens must lie in [0, 2^31)");
     if (e->table_ld < e->cols || e->data_ld < e->cols || e->table_ld > (1ll << 40) / e->rows ||
         e->data_ld > (1ll << 40) / std::max<int64_t>(1, e->tokens))
         return report(CAME_ERR_SHAPE, "a row stride is below cols, or the tensor is too large");
+    if (e->table_ld > (1ll << 29) || e->data_ld > (1ll << 29))
+        return report(CAME_ERR_SHAPE, "a row stride is beyond 2^29 elements");
     if (!known_dtype(e->table_dtype) || !known_dtype(e->data_dtype)) return report(CAME_ERR_DTYPE, "unknown dtype");
     if (e->id_dtype != CAME_I32 && e->id_dtype != CAME_I64) return report(CAME_ERR_DTYPE, "unknown id_dtype");
     if (e->flags & ~static_cast<uint32_t>(CAME_EMBED_ACCUMULATE | CAME_EMBED_PADDING_ROW))
@@ -795,18 +918,23 @@ void launch_forward_types(const came_embed& e, cudaStream_t stream)
 // Launched with programmatic stream serialisation: the kernel waits for the grid before it itself.
 // (early = false: an ordinary launch.)
 template <typename K, typename... A>
-cudaError_t launch_dependent(K kernel, bool early, long long blocks, int threads, size_t smem, cudaStream_t stream, A... args)
+cudaError_t launch_dependent(K kernel, bool early, int cluster, long long blocks, int threads, size_t smem, cudaStream_t stream, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(blocks));
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[3];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    attr[2].id = cudaLaunchAttributeClusterSchedulingPolicyPreference;       // a block of a cluster per SM
+    attr[2].val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicySpread;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 3 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
@@ -826,11 +954,13 @@ cudaError_t launch_sort(const came_embed& e, const SortArgs& a, int32_t device, 
         return cudaGetLastError();
     }
     static std::atomic<uint64_t> done{0};
-    cudaError_t err = allow_smem(k_embed_move<I>, kHistBytes, device, done);
+    cudaError_t err = allow_smem(k_embed_move<I>, sizeof(unsigned) * kMoveWarps * kMaxBins, device, done);
     if (err != cudaSuccess) return err;
-    k_embed_count<I><<<a.blocks, kSortThreads, 0, stream>>>(ids, a);
+    k_embed_count<I><<<a.blocks, kMoveThreads, 0, stream>>>(ids, a);
+    err = cudaGetLastError();
+    const size_t hist = sizeof(unsigned) * kMoveWarps << a.digit_bits;
     for (int pass = 0; pass < a.passes && err == cudaSuccess; ++pass)
-        err = launch_dependent(k_embed_move<I>, true, a.blocks, kSortThreads, kHistBytes, stream, ids, a, pass);
+        err = launch_dependent(k_embed_move<I>, true, 1, a.blocks, kMoveThreads, hist, stream, ids, a, pass);
     return err;
 }
 
@@ -839,7 +969,9 @@ cudaError_t launch_sums(const came_embed& e, const SumArgs& s, long long blocks,
 {
     // the rows without tokens may be written while the sort runs, but only behind a sort: it has
     // waited for everything that came before
-    return launch_dependent(k_embed_sum<T, O, EV>, e.tokens > 0, s.zero_blocks + blocks, kSumWarps * 32, 0, stream,
+    const int cluster = s.zero_blocks ? kClusterBlocks : 1;
+    return launch_dependent(k_embed_sum<T, O, EV>, e.tokens > 0, cluster, ceil_div(s.zero_blocks + blocks, cluster) * cluster,
+                            kSumWarps * 32, 0, stream,
                             static_cast<const T*>(e.data), static_cast<O*>(e.table), s);
 }
 
@@ -919,7 +1051,7 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     t.arrived = a.arrived;
     t.tokens = e->tokens;
     t.cols = e->cols;
-    t.dy_ld = e->data_ld;
+    t.dy_bytes = static_cast<unsigned>(e->data_ld * dtype_bytes(e->data_dtype));
     t.grad_ld = e->table_ld;
     t.rows = a.rows;
     t.slices = static_cast<int>(l.slices);
@@ -930,8 +1062,9 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     t.id64 = e->id_dtype == CAME_I64;
     t.padding = a.padding;
     if (!t.accumulate) {
-        t.zero_blocks = 1;
-        while (t.zero_blocks < kZeroBlocks && 2ll * t.zero_blocks <= e->rows) t.zero_blocks *= 2;
+        t.zero_blocks = kZeroBlocks;
+        // at least 2 KB of neighbouring rows together
+        while (t.zero_group < 5 && (static_cast<unsigned long long>(e->cols) * dtype_bytes(e->table_dtype) << t.zero_group) < 2048) ++t.zero_group;
     }
     if (e->tokens == 0 && t.accumulate) return CAME_OK;
     cudaError_t err = cudaSuccess;
@@ -941,6 +1074,7 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
     if (err != cudaSuccess) return report_cuda(err, "kernel launch(sort)");
     using bf16 = __nv_bfloat16;
     const long long blocks = l.blocks * l.slices;
+    t.sum_blocks = static_cast<unsigned>(blocks);
     if (e->data_dtype == CAME_BF16)
         err = e->table_dtype == CAME_BF16 ? launch_sums_ev<bf16, bf16>(*e, t, blocks, stream)
                                           : launch_sums_ev<bf16, float>(*e, t, blocks, stream);

@@ -48,6 +48,10 @@ __device__ __forceinline__ double warp_sum(double v)
     return v;
 }
 
+// Orders this thread's writes before, and its reads after, a counter that other blocks see (the
+// acquire-release fence; __threadfence is the sequentially consistent one, which takes longer).
+__device__ __forceinline__ void publish() { asm volatile("fence.acq_rel.gpu;" ::: "memory"); }
+
 // Programmatic dependent launch: let the next grid of the stream be scheduled / wait until the
 // grids before this one have finished and their memory is visible.
 __device__ __forceinline__ void release_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
