@@ -376,18 +376,24 @@ def came_clip_destroy(ctx) -> None:
 
 
 def came_embed_forward(e: came_embed, device: int = 0, stream: int = 0) -> None:
-    _check(load().came_embed_forward(e, device, stream))
+    status = (_lib or load()).came_embed_forward(e, device, stream)
+    if status:
+        _check(status)
 
 
 def came_embed_workspace(e: came_embed) -> int:
     out = ctypes.c_int64()
-    _check(load().came_embed_workspace(e, out))
+    status = (_lib or load()).came_embed_workspace(e, out)
+    if status:
+        _check(status)
     return out.value
 
 
 def came_embed_backward(e: came_embed, workspace: int, workspace_bytes: int, device: int = 0,
                         stream: int = 0) -> None:
-    _check(load().came_embed_backward(e, workspace, workspace_bytes, device, stream))
+    status = (_lib or load()).came_embed_backward(e, workspace, workspace_bytes, device, stream)
+    if status:
+        _check(status)
 
 
 def make_hparams(step: int, **kw) -> came_hparams:
@@ -411,17 +417,18 @@ def _torch():
 
 
 def _call_on(device, call, *args) -> None:
-    """``call(*args, stream)`` with ``device`` current, ``stream`` its current stream's address."""
+    """``call(*args, index, stream)`` with ``device`` current: its index, its current stream's address."""
     torch = _torch()
     index, before = device.index, torch.cuda.current_device()
-    if before != index:
-        torch.cuda.set_device(index)
+    stream = torch._C._cuda_getCurrentRawStream(index)      # (a Stream object costs more than a launch)
+    if before == index:
+        call(*args, index, stream)
+        return
+    torch.cuda.set_device(index)
     try:
-        # (a Stream object costs more than the launch)
-        call(*args, torch._C._cuda_getCurrentRawStream(index))
+        call(*args, index, stream)
     finally:
-        if before != index:
-            torch.cuda.set_device(before)
+        torch.cuda.set_device(before)
 
 
 # --- gradient norm and clipping ------------------------------------------------------------
@@ -506,14 +513,22 @@ class GradClip:
             self.grads = grads
         return self.total_norm, self.coef, self.tensor_norms
 
+    @staticmethod
+    def _norm_call(ctx, p, results, at, index, stream):
+        came_clip_norm(ctx, p, results, at, stream)
+
+    @staticmethod
+    def _clip_call(ctx, p, results, at, index, stream):
+        came_clip_grads(ctx, p, results, at, stream)
+
     def norm(self, max_norm: float = float("inf"), eps: float = 1e-6, grad_scale: float = 1.0,
              grads=None):
         """``(total_norm, coef, tensor_norms)``; ``grads`` replaces the tensors of earlier calls."""
-        return self._run(came_clip_norm, max_norm, eps, grad_scale, grads)
+        return self._run(self._norm_call, max_norm, eps, grad_scale, grads)
 
     def clip(self, max_norm: float, eps: float = 1e-6, grad_scale: float = 1.0, grads=None):
         """``norm``, and ``outs = grads * (grad_scale * coef)``."""
-        return self._run(came_clip_grads, max_norm, eps, grad_scale, grads)
+        return self._run(self._clip_call, max_norm, eps, grad_scale, grads)
 
     def close(self) -> None:
         if self.ctx is not None:
@@ -531,43 +546,45 @@ class GradClip:
 
 # --- embedding lookup and its gradient -------------------------------------------------------
 
-_ID_CODES = {}          # torch dtype -> came_id_dtype, filled on first use (torch is imported late)
+_ID_CODES = {}          # torch dtype -> came_id_dtype
 
 
-def _embed_args(table, table_name, data, data_name, ids, scale):
-    """The descriptor of a call, and the device; every refusal that needs the tensors is here."""
-    if table.dim() != 2:
-        raise CameError(CAME_ERR_SHAPE, f"{table_name} must be a matrix")
-    rows, cols = table.shape
-    table_ld, one = table.stride()
-    if one != 1 and cols > 1:
-        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {table_name} must be contiguous")
-    device = table.device
-    _cuda_tensor(table, table_name)
-    _cuda_tensor(ids, "ids", None, device)
-    _cuda_tensor(data, data_name, None, device)
+def _embed_args(table, table_name, data, data_name, ids, scale, flags=0, padding_row=0):
+    """The descriptor of a call; every refusal that needs the tensors is here.  (Written for small
+    calls, whose time is the host's: one look at each attribute.)"""
     if not _ID_CODES:
-        _ID_CODES.update({_torch().int32: CAME_I32, _torch().int64: CAME_I64})
-    code = _ID_CODES.get(ids.dtype)
-    if code is None:
+        torch = _torch()
+        _ID_CODES.update({torch.int32: CAME_I32, torch.int64: CAME_I64})
+        _DTYPE_CODES.update({torch.float32: CAME_F32, torch.bfloat16: CAME_BF16})
+    shape, ids_shape, data_shape, device = table.shape, ids.shape, data.shape, table.device
+    if len(shape) != 2:
+        raise CameError(CAME_ERR_SHAPE, f"{table_name} must be a matrix")
+    rows, cols = shape
+    if not table.is_cuda or ids.device != device or data.device != device:
+        raise CameError(CAME_ERR_DEVICE, f"{table_name}, ids and {data_name} must be on one GPU")
+    id_code = _ID_CODES.get(ids.dtype)
+    if id_code is None:
         raise CameError(CAME_ERR_DTYPE, f"ids must be int32 or int64, got {ids.dtype}")
+    table_code, data_code = _DTYPE_CODES.get(table.dtype), _DTYPE_CODES.get(data.dtype)
+    if table_code is None or data_code is None:
+        raise CameError(CAME_ERR_DTYPE, f"{table_name} and {data_name} must be fp32 or bf16, got {table.dtype} and {data.dtype}")
+    if data_shape[:-1] != ids_shape or data_shape[-1] != cols:
+        raise CameError(CAME_ERR_SHAPE, f"{data_name} must have the shape of ids and the columns of {table_name}")
     if not ids.is_contiguous():
         raise CameError(CAME_ERR_UNSUPPORTED, "ids must be contiguous")
-    if data.shape != (*ids.shape, cols):
-        raise CameError(CAME_ERR_SHAPE, f"{data_name} must have the shape of ids and the columns of {table_name}")
-    if data.dim() != 2:
+    if len(data_shape) != 2:
         data = data.view(-1, cols)
-    data_ld, one = data.stride()
-    if one != 1 and cols > 1:
-        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {data_name} must be contiguous")
-    tokens = data.shape[0]
+    tokens = ids.numel()
+    table_ld, one = table.stride()
+    data_ld, two = data.stride()
+    if cols > 1 and (one != 1 or two != 1):
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {table_name} and of {data_name} must be contiguous")
     if rows == 1:                       # the stride of a single row says nothing
         table_ld = cols
     if tokens <= 1:
         data_ld = cols
-    return came_embed(table.data_ptr(), data.data_ptr(), ids.data_ptr(), rows, cols, tokens, table_ld,
-                      data_ld, 0, scale, _dtype_code(table, table_name), _dtype_code(data, data_name),
-                      code, 0, 0), device
+    return came_embed(table.data_ptr(), data.data_ptr(), ids.data_ptr(), rows, cols, tokens, table_ld, data_ld,
+                      padding_row, scale, table_code, data_code, id_code, flags, 0)
 
 
 def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
@@ -582,8 +599,8 @@ def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
         out = table.new_empty((*ids.shape, table.shape[1]), dtype=out_dtype)
     elif out_dtype is not None and out.dtype != out_dtype:
         raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
-    e, device = _embed_args(table, "table", out, "out", ids, scale)
-    _call_on(device, came_embed_forward, e, device.index)
+    e = _embed_args(table, "table", out, "out", ids, scale)
+    _call_on(table.device, came_embed_forward, e)
     return out
 
 
@@ -595,16 +612,14 @@ def embed_backward(grad_out, ids, grad, scale: float = 1.0, padding_row: Optiona
     ``grad_out``: fp32 or bf16, shape ``(*ids.shape, cols)``; ``grad``: fp32 or bf16 matrix, every
     row of it written unless ``accumulate``; tokens of ``padding_row`` add nothing.  Returns
     ``grad``.  Bit-reproducible: a row's tokens are added in an order fixed by the ids."""
-    e, device = _embed_args(grad, "grad", grad_out, "grad_out", ids, scale)
-    if accumulate:
-        e.flags |= CAME_EMBED_ACCUMULATE
+    flags = CAME_EMBED_ACCUMULATE if accumulate else 0
     if padding_row is not None:
-        e.flags |= CAME_EMBED_PADDING_ROW
-        e.padding_row = padding_row
+        flags |= CAME_EMBED_PADDING_ROW
+    e = _embed_args(grad, "grad", grad_out, "grad_out", ids, scale, flags, padding_row or 0)
     size = came_embed_workspace(e)
     # from torch's allocator, for the device's current stream: not reused before the call is done
-    ws = grad_out.new_empty(-(-size // 4), dtype=_torch().float32)
-    _call_on(device, came_embed_backward, e, ws.data_ptr(), size, device.index)
+    ws = grad_out.new_empty((size + 3) // 4, dtype=_torch().float32)
+    _call_on(grad.device, came_embed_backward, e, ws.data_ptr(), size)
     return grad
 
 
