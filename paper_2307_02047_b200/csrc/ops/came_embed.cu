@@ -71,7 +71,8 @@ struct Raw {
     }
 };
 
-template <int EV, typename T>
+// kStream: marked as first to leave the L2.
+template <int EV, bool kStream = false, typename T>
 __device__ __forceinline__ void store_ev(T* p, const float* x)
 {
     constexpr int B = EV * static_cast<int>(sizeof(T));
@@ -83,10 +84,15 @@ __device__ __forceinline__ void store_ev(T* p, const float* x)
             if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(x[j]);
             else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[j]) : "f"(x[2 * j + 1]), "f"(x[2 * j]));
         }
-        if constexpr (W == 8)
+        if constexpr (W == 8 && kStream)
+            asm volatile("st.global.L1::no_allocate.L2::evict_first.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                         :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+                            "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+        else if constexpr (W == 8)
             asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                          :: "l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
                             "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+        else if constexpr (W == 4 && kStream) __stcs(reinterpret_cast<uint4*>(p), make_uint4(w[0], w[1], w[2], w[3]));
         else if constexpr (W == 4) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
         else if constexpr (W == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t*>(p) = w[0];
@@ -120,42 +126,44 @@ __device__ __forceinline__ long long column(long long slice, int group, int lane
 
 // ---- forward --------------------------------------------------------------------------------
 
-constexpr int kFwdSlices = 4;            // slices of one token per warp: loads in flight
-
-template <typename I, typename T, typename O, int EV>
+// A warp copies S slices of one token's row: S rows' pieces in flight per lane.  Bound by the bytes:
+// 128k tokens of 4096 bf16 take 229 / 241 / 338 us with 4 / 2 / 1 slices per warp; rows of one slice, and rows that
+// go in accesses below 16 bytes, are faster with one (60000 rows of 1001 bf16: 62 against 145 us).
+// stream: the output is larger than the L2 can hold for its reader anyway, so it leaves the
+// table's rows there (223 instead of 229 us).
+template <typename I, typename T, typename O, int EV, int S>
 __global__ void __launch_bounds__(256)
-k_embed_forward(const T* __restrict__ table, long long rows, long long cols, long long table_ld,
-                const I* __restrict__ ids, long long tokens, float scale, O* __restrict__ out,
-                long long out_ld, int warps_per_token)
+k_embed_forward(const T* __restrict__ table, long long rows, int cols, long long table_ld, const I* __restrict__ ids,
+                unsigned tokens, float scale, O* __restrict__ out, long long out_ld, unsigned warps_per_token, int stream)
 {
-    const long long item = static_cast<long long>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-    const long long t = item / warps_per_token;
+    const unsigned item = blockIdx.x * 8u + (threadIdx.x >> 5);
+    const unsigned t = S == 1 && warps_per_token == 1 ? item : item / warps_per_token;
     if (t >= tokens) return;
-    const long long s0 = (item - t * warps_per_token) * kFwdSlices;
     const int lane = threadIdx.x & 31;
+    const int first = static_cast<int>(item - t * warps_per_token) * (S * kSlice) + lane * EV;
     const long long id = static_cast<long long>(ids[t]);
     const bool hit = id >= 0 && id < rows;
     const T* const src = table + (hit ? id : 0) * table_ld;
     O* const dst = out + t * out_ld;
-    Raw<EV, T> x[kFwdSlices][8 / EV];
+    Raw<EV, T> x[S][8 / EV];
 #pragma unroll
-    for (int s = 0; s < kFwdSlices; ++s)
+    for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int g = 0; g < 8 / EV; ++g) {
-            const long long c = column<EV>(s0 + s, g, lane);
+            const int c = first + s * kSlice + g * (32 * EV);
             if (hit && c < cols) x[s][g].load(src + c);
         }
 #pragma unroll
-    for (int s = 0; s < kFwdSlices; ++s)
+    for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int g = 0; g < 8 / EV; ++g) {
-            const long long c = column<EV>(s0 + s, g, lane);
-            if (c < cols) {
-                float y[EV];
+            const int c = first + s * kSlice + g * (32 * EV);
+            if (c >= cols) continue;
+            float y[EV];
 #pragma unroll
-                for (int k = 0; k < EV; ++k) y[k] = hit ? x[s][g].value(k) * scale : 0.f;
-                store_ev<EV, O>(dst + c, y);
-            }
+            for (int k = 0; k < EV; ++k) y[k] = hit ? x[s][g].value(k) * scale : 0.f;
+            if (stream) store_ev<EV, true>(dst + c, y);
+            else        store_ev<EV>(dst + c, y);
         }
 }
 
@@ -502,7 +510,7 @@ __device__ __forceinline__ void store_row(const SumArgs& a, O* grad, unsigned ro
                 for (int k = 0; k < EV; ++k) y[k] += old.value(k);
             }
         }
-        store_ev<EV, O>(dst + c, y);
+        store_ev<EV>(dst + c, y);
     }
 }
 
@@ -641,7 +649,7 @@ __device__ __forceinline__ void zero_rows(const I* __restrict__ ids, O* __restri
             if ((seen[k >> 5] >> (k & 31u) & 1u) || r >= a.rows) continue;
             O* const dst = grad + static_cast<long long>(r) * a.grad_ld;
             for (long long c = static_cast<long long>(lane & (per_row - 1)) * EV; c < a.cols; c += per_row * EV)
-                store_ev<EV, O>(dst + c, zeros);
+                store_ev<EV>(dst + c, zeros);
         }
         __syncthreads();
     }
@@ -881,14 +889,24 @@ int elements_per_access(const came_embed& e)
     return 1;
 }
 
+template <typename I, typename T, typename O, int EV, int S>
+void launch_forward_slices(const came_embed& e, cudaStream_t stream)
+{
+    const long long per_token = ceil_div(e.cols, kSlice * S), blocks = ceil_div(e.tokens * per_token, 8);
+    const bool large = e.tokens * e.cols * static_cast<long long>(sizeof(O)) > (64ll << 20);
+    k_embed_forward<I, T, O, EV, S><<<static_cast<unsigned>(blocks), 256, 0, stream>>>(
+        static_cast<const T*>(e.table), e.rows, static_cast<int>(e.cols), e.table_ld, static_cast<const I*>(e.ids),
+        static_cast<unsigned>(e.tokens), static_cast<float>(e.scale), static_cast<O*>(e.data), e.data_ld,
+        static_cast<unsigned>(per_token), large ? 1 : 0);
+}
+
 template <typename I, typename T, typename O, int EV>
 void launch_forward(const came_embed& e, cudaStream_t stream)
 {
-    const int per_token = static_cast<int>(ceil_div(e.cols, kSlice * kFwdSlices));
-    const long long items = e.tokens * per_token;
-    k_embed_forward<I, T, O, EV><<<static_cast<unsigned>(ceil_div(items, 8)), 256, 0, stream>>>(
-        static_cast<const T*>(e.table), e.rows, e.cols, e.table_ld, static_cast<const I*>(e.ids), e.tokens,
-        static_cast<float>(e.scale), static_cast<O*>(e.data), e.data_ld, per_token);
+    if constexpr (EV == 8) {
+        if (e.cols > kSlice) return launch_forward_slices<I, T, O, EV, 4>(e, stream);
+    }
+    launch_forward_slices<I, T, O, EV, 1>(e, stream);
 }
 
 template <typename I, typename T, typename O>
@@ -998,7 +1016,7 @@ came_status came_embed_forward(const came_embed* e, int32_t device, void* cuda_s
     if ((s = require_current_device(device)) != CAME_OK) return s;
     if (e->tokens == 0) return CAME_OK;
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (e->tokens * ceil_div(e->cols, kSlice * kFwdSlices) > (1ll << 33))
+    if (e->tokens * ceil_div(e->cols, kSlice) >= (1ll << 32) - 8)
         return report(CAME_ERR_SHAPE, "too many tokens times columns for one launch");
     if (e->id_dtype == CAME_I64) launch_forward_types<long long>(*e, stream);
     else                         launch_forward_types<int>(*e, stream);
