@@ -183,7 +183,7 @@ constexpr unsigned kFewRows = 1u << 22;  // (key and position then fit one word)
 constexpr int kOneTokens = 4096;         // up to here one block sorts in its shared memory
 constexpr int kMoveThreads = 512;        // beyond that a grid of blocks that leave room for others on their SM
 constexpr int kMoveWarps = kMoveThreads / 32;
-constexpr int kMoveTile = 1024;          // tokens per block, or a multiple of it ...
+constexpr int kMoveTile = 512;           // tokens per block, or a multiple of it ...
 constexpr int kMoveBlocks = 148;         // ... so that there are no more blocks than SMs
 constexpr size_t kHistBytes = sizeof(unsigned) * kSortWarps * kMaxBins;
 constexpr size_t kOneBytes = kHistBytes + sizeof(uint2) * kOneTokens;
@@ -467,6 +467,7 @@ k_embed_move(const I* __restrict__ ids, SortArgs a, int pass)
 // The first zero_blocks blocks write the rows without tokens instead.  They need the ids only, so
 // they do not wait for the sort: the zeros are written while it runs.
 constexpr int kSumWarps = 8;
+constexpr int kTinyTokens = 64;          // one block's: no run crosses blocks
 constexpr int kClusterBlocks = 8, kZeroClusters = 64, kZeroBlocks = kClusterBlocks * kZeroClusters;
 constexpr int kZeroWords = 2048;         // of the bit map: 65536 of a cluster's rows per round
 enum : int { kLinkHead = 1, kLinkTail = 2, kLinkThrough = 4 };
@@ -480,6 +481,7 @@ struct SumArgs {
     unsigned  dy_bytes;        // from row to row of dY
     unsigned  rows, padding;
     int       slices, per_warp, accumulate, id64;
+    int       tiny;            // up to kTinyTokens: every block sorts the ids for itself
     int       zero_blocks;     // 0 or kZeroBlocks
     int       zero_group;      // log2 of the neighbouring rows a cluster takes at once
     unsigned  sum_blocks;      // the grid is rounded up to whole clusters
@@ -655,6 +657,27 @@ __device__ __forceinline__ void zero_rows(const I* __restrict__ ids, O* __restri
     }
 }
 
+// The sorted (key, token) pairs of up to kTinyTokens ids.
+template <typename I>
+__device__ __forceinline__ void sort_tiny(const I* __restrict__ ids, const SumArgs& a, unsigned long long* word, uint2* sorted)
+{
+    const unsigned t = threadIdx.x, n = static_cast<unsigned>(a.tokens);
+    unsigned long long mine = 0;
+    if (t < n) {
+        const long long id = static_cast<long long>(ids[t]);
+        const unsigned key = id >= 0 && id < a.rows && id != a.padding ? static_cast<unsigned>(id) : a.rows;
+        mine = static_cast<unsigned long long>(key) << 32 | t;
+        word[t] = mine;
+    }
+    __syncthreads();
+    if (t < n) {
+        unsigned before = 0;
+        for (unsigned j = 0; j < n; ++j) before += word[j] < mine;
+        sorted[before] = make_uint2(static_cast<unsigned>(mine >> 32), t);
+    }
+    __syncthreads();
+}
+
 template <typename T, typename O, int EV>
 __global__ void __launch_bounds__(kSumWarps * 32, 4)
 k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
@@ -676,18 +699,26 @@ k_embed_sum(const T* __restrict__ dy, O* __restrict__ grad, SumArgs a)
     const int slice = static_cast<int>(at - block * static_cast<unsigned>(a.slices));
     const int K = a.per_warp;
     const long long p0 = (static_cast<long long>(block) * kSumWarps + warp) * K;
-    wait_for_previous_grid();
+    __shared__ uint2 tiny_pair[kTinyTokens];
+    if (a.tiny) {
+        unsigned long long* const word = reinterpret_cast<unsigned long long*>(part);
+        if (a.id64) sort_tiny(static_cast<const long long*>(a.ids), a, word, tiny_pair);
+        else        sort_tiny(static_cast<const int*>(a.ids), a, word, tiny_pair);
+    } else {
+        wait_for_previous_grid();
+    }
+    auto pair_at = [&](long long p) { return a.tiny ? tiny_pair[p] : __ldcg(a.pair + p); };
 
     // The warp's tokens, a group of (up to) 32 at a time, a lane each; keys that are rows come first.
     const int size = min(K, 32), groups = K / size;
     auto group_at = [&](int m) {
         const long long p = p0 + m * 32 + lane;
-        return m < groups && lane < size && p < a.tokens ? __ldcg(a.pair + p) : make_uint2(a.rows, 0u);
+        return m < groups && lane < size && p < a.tokens ? pair_at(p) : make_uint2(a.rows, 0u);
     };
     uint2 now = group_at(0), next = group_at(1);
-    const unsigned key_last = p0 + K <= a.tokens ? __ldcg(&a.pair[p0 + K - 1].x) : a.rows;
-    const unsigned key_before = p0 > 0 && p0 <= a.tokens ? __ldcg(&a.pair[p0 - 1].x) : a.rows;
-    const unsigned key_after = p0 + K < a.tokens ? __ldcg(&a.pair[p0 + K].x) : a.rows;
+    const unsigned key_last = p0 + K <= a.tokens ? pair_at(p0 + K - 1).x : a.rows;
+    const unsigned key_before = p0 > 0 && p0 <= a.tokens ? pair_at(p0 - 1).x : a.rows;
+    const unsigned key_after = p0 + K < a.tokens ? pair_at(p0 + K).x : a.rows;
     const unsigned key_first = __shfl_sync(0xffffffffu, now.x, 0);
     const bool any = key_first < a.rows;
     const bool head = any && key_before == key_first;
@@ -985,10 +1016,10 @@ cudaError_t launch_sort(const came_embed& e, const SortArgs& a, int32_t device, 
 template <typename T, typename O, int EV>
 cudaError_t launch_sums(const came_embed& e, const SumArgs& s, long long blocks, cudaStream_t stream)
 {
-    // the rows without tokens may be written while the sort runs, but only behind a sort: it has
-    // waited for everything that came before
+    // the rows without tokens may be written while the sort runs, but only behind a sort: that has
+    // waited for everything before it
     const int cluster = s.zero_blocks ? kClusterBlocks : 1;
-    return launch_dependent(k_embed_sum<T, O, EV>, e.tokens > 0, cluster, ceil_div(s.zero_blocks + blocks, cluster) * cluster,
+    return launch_dependent(k_embed_sum<T, O, EV>, e.tokens > 0 && !s.tiny, cluster, ceil_div(s.zero_blocks + blocks, cluster) * cluster,
                             kSumWarps * 32, 0, stream,
                             static_cast<const T*>(e.data), static_cast<O*>(e.table), s);
 }
@@ -1085,8 +1116,9 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
         while (t.zero_group < 5 && (static_cast<unsigned long long>(e->cols) * dtype_bytes(e->table_dtype) << t.zero_group) < 2048) ++t.zero_group;
     }
     if (e->tokens == 0 && t.accumulate) return CAME_OK;
+    t.tiny = e->tokens <= kTinyTokens;
     cudaError_t err = cudaSuccess;
-    if (e->tokens > 0)
+    if (!t.tiny)
         err = e->id_dtype == CAME_I64 ? launch_sort<long long>(*e, a, device, stream)
                                        : launch_sort<int>(*e, a, device, stream);
     if (err != cudaSuccess) return report_cuda(err, "kernel launch(sort)");
