@@ -1,9 +1,11 @@
 /*
  * came_b200.h -- C ABI of the B200 (sm_100a) CAME optimizer step.
  *
- * The library performs one thing: the per-step parameter update of the CAME
- * optimizer ("CAME: Confidence-guided Adaptive Memory Efficient Optimization",
- * Algorithm 2) over a list of parameter tensors resident on one GPU.
+ * The library performs the per-step parameter update of the CAME optimizer ("CAME:
+ * Confidence-guided Adaptive Memory Efficient Optimization", Algorithm 2) over a
+ * list of parameter tensors resident on one GPU, and the operators of a training
+ * step that stand next to it: the global gradient norm with clipping, the embedding
+ * lookup and its gradient (further below, each with its formulas).
  *
  * For a matrix parameter theta (n rows x m columns, row-major) with gradient g,
  * one step computes, in the notation of Algorithm 2 (all matrix squares,
