@@ -87,7 +87,7 @@ def train(steps=300, vocab=997, dim=128, batch=32, length=64, max_norm=1.0, lr=5
         losses.append(loss.detach())
         norms.append(total_norm.clone())
         if report and step % 50 == 0:
-            report(f"step {step}: loss {float(loss):.3f}, gradient norm {float(total_norm):.3f}")
+            report(f"step {step}: loss {float(losses[-1]):.3f}, gradient norm {float(total_norm):.3f}")
     opt.close()
     clip.close()
     return torch.stack(losses), torch.stack(norms)
