@@ -416,19 +416,16 @@ def _torch():
     return _torch_module
 
 
-def _call_on(device, call, *args) -> None:
-    """``call(*args, index, stream)`` with ``device`` current: its index, its current stream's address."""
-    torch = _torch()
-    index, before = device.index, torch.cuda.current_device()
-    stream = torch._C._cuda_getCurrentRawStream(index)      # (a Stream object costs more than a launch)
+def _call_on(index, call, *args) -> None:
+    """``call(*args, index, stream)`` with device ``index`` current; ``stream``: its current stream's
+    address (asked for directly: a Stream object costs more than a launch)."""
+    C = _torch()._C
+    before = C._cuda_getDevice()
     if before == index:
-        call(*args, index, stream)
+        call(*args, index, C._cuda_getCurrentRawStream(index))
         return
-    torch.cuda.set_device(index)
-    try:
-        call(*args, index, stream)
-    finally:
-        torch.cuda.set_device(before)
+    with _torch().cuda.device(index):
+        call(*args, index, C._cuda_getCurrentRawStream(index))
 
 
 # --- gradient norm and clipping ------------------------------------------------------------
@@ -508,7 +505,7 @@ class GradClip:
             at = [g.data_ptr() for g in grads]
         p = self._params
         p.max_norm, p.eps, p.grad_scale = max_norm, eps, grad_scale
-        _call_on(self.device, call, self.ctx, p, self._results_at, at)
+        _call_on(self.device.index, call, self.ctx, p, self._results_at, at)
         if grads is not None:
             self.grads = grads
         return self.total_norm, self.coef, self.tensor_norms
@@ -546,45 +543,60 @@ class GradClip:
 
 # --- embedding lookup and its gradient -------------------------------------------------------
 
+# (Written for small calls, whose time is the host's: one look at each attribute.)
+
 _ID_CODES = {}          # torch dtype -> came_id_dtype
 
 
-def _embed_args(table, table_name, data, data_name, ids, scale, flags=0, padding_row=0):
-    """The descriptor of a call; every refusal that needs the tensors is here.  (Written for small
-    calls, whose time is the host's: one look at each attribute.)"""
+def _embed_table(table, name):
+    """(rows, columns, row stride, dtype code, device index) of the table or its gradient."""
     if not _ID_CODES:
         torch = _torch()
-        _ID_CODES.update({torch.int32: CAME_I32, torch.int64: CAME_I64})
         _DTYPE_CODES.update({torch.float32: CAME_F32, torch.bfloat16: CAME_BF16})
-    shape, ids_shape, data_shape, device = table.shape, ids.shape, data.shape, table.device
+        _ID_CODES.update({torch.int32: CAME_I32, torch.int64: CAME_I64})
+    shape, index = table.shape, table.get_device()
     if len(shape) != 2:
-        raise CameError(CAME_ERR_SHAPE, f"{table_name} must be a matrix")
+        raise CameError(CAME_ERR_SHAPE, f"{name} must be a matrix")
+    if index < 0:
+        raise CameError(CAME_ERR_DEVICE, f"{name} must be a CUDA tensor")
     rows, cols = shape
-    if not table.is_cuda or ids.device != device or data.device != device:
-        raise CameError(CAME_ERR_DEVICE, f"{table_name}, ids and {data_name} must be on one GPU")
-    id_code = _ID_CODES.get(ids.dtype)
-    if id_code is None:
+    ld, one = table.stride()
+    if one != 1 and cols > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must be contiguous")
+    code = _DTYPE_CODES.get(table.dtype)
+    if code is None:
+        raise CameError(CAME_ERR_DTYPE, f"{name} must be fp32 or bf16, got {table.dtype}")
+    return rows, cols, ld if rows > 1 else cols, code, index       # (the stride of a single row says nothing)
+
+
+def _embed_ids(ids, index) -> int:
+    """The ids' type code."""
+    if ids.get_device() != index:
+        raise CameError(CAME_ERR_DEVICE, "ids must be on the table's GPU")
+    code = _ID_CODES.get(ids.dtype)
+    if code is None:
         raise CameError(CAME_ERR_DTYPE, f"ids must be int32 or int64, got {ids.dtype}")
-    table_code, data_code = _DTYPE_CODES.get(table.dtype), _DTYPE_CODES.get(data.dtype)
-    if table_code is None or data_code is None:
-        raise CameError(CAME_ERR_DTYPE, f"{table_name} and {data_name} must be fp32 or bf16, got {table.dtype} and {data.dtype}")
-    if data_shape[:-1] != ids_shape or data_shape[-1] != cols:
-        raise CameError(CAME_ERR_SHAPE, f"{data_name} must have the shape of ids and the columns of {table_name}")
     if not ids.is_contiguous():
         raise CameError(CAME_ERR_UNSUPPORTED, "ids must be contiguous")
-    if len(data_shape) != 2:
+    return code
+
+
+def _embed_data(data, name, ids, cols, index):
+    """(row stride, dtype code) of the tokens' rows."""
+    shape = data.shape
+    if shape[:-1] != ids.shape or shape[-1] != cols:
+        raise CameError(CAME_ERR_SHAPE, f"{name} must have the shape of ids and the columns of the table")
+    if data.get_device() != index:
+        raise CameError(CAME_ERR_DEVICE, f"{name} must be on the table's GPU")
+    code = _DTYPE_CODES.get(data.dtype)
+    if code is None:
+        raise CameError(CAME_ERR_DTYPE, f"{name} must be fp32 or bf16, got {data.dtype}")
+    if len(shape) != 2:
         data = data.view(-1, cols)
-    tokens = ids.numel()
-    table_ld, one = table.stride()
-    data_ld, two = data.stride()
-    if cols > 1 and (one != 1 or two != 1):
-        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {table_name} and of {data_name} must be contiguous")
-    if rows == 1:                       # the stride of a single row says nothing
-        table_ld = cols
-    if tokens <= 1:
-        data_ld = cols
-    return came_embed(table.data_ptr(), data.data_ptr(), ids.data_ptr(), rows, cols, tokens, table_ld, data_ld,
-                      padding_row, scale, table_code, data_code, id_code, flags, 0)
+    ld, one = data.stride()
+    if one != 1 and cols > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must be contiguous")
+    return ld if data.shape[0] > 1 else cols, code
 
 
 def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
@@ -593,14 +605,20 @@ def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
     ``table``: fp32 or bf16 CUDA matrix with contiguous rows; ``ids``: contiguous int32 or int64
     CUDA tensor of any shape; ``out``: tensor of shape ``(*ids.shape, cols)``, fp32 or bf16, made
     here when it is None (of type ``out_dtype``, the table's when that is None too)."""
+    rows, cols, table_ld, table_code, index = _embed_table(table, "table")
+    id_code = _embed_ids(ids, index)
     if out is None:
-        if table.dim() != 2:
-            raise CameError(CAME_ERR_SHAPE, "table must be a matrix")
-        out = table.new_empty((*ids.shape, table.shape[1]), dtype=out_dtype)
-    elif out_dtype is not None and out.dtype != out_dtype:
-        raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
-    e = _embed_args(table, "table", out, "out", ids, scale)
-    _call_on(table.device, came_embed_forward, e)
+        out = table.new_empty((*ids.shape, cols), dtype=out_dtype)
+        ld, code = cols, _DTYPE_CODES.get(out.dtype)
+        if code is None:
+            raise CameError(CAME_ERR_DTYPE, f"out must be fp32 or bf16, got {out.dtype}")
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
+        ld, code = _embed_data(out, "out", ids, cols, index)
+    e = came_embed(table.data_ptr(), out.data_ptr(), ids.data_ptr(), rows, cols, ids.numel(), table_ld, ld,
+                   0, scale, table_code, code, id_code, 0, 0)
+    _call_on(index, came_embed_forward, e)
     return out
 
 
@@ -612,14 +630,18 @@ def embed_backward(grad_out, ids, grad, scale: float = 1.0, padding_row: Optiona
     ``grad_out``: fp32 or bf16, shape ``(*ids.shape, cols)``; ``grad``: fp32 or bf16 matrix, every
     row of it written unless ``accumulate``; tokens of ``padding_row`` add nothing.  Returns
     ``grad``.  Bit-reproducible: a row's tokens are added in an order fixed by the ids."""
+    rows, cols, grad_ld, grad_code, index = _embed_table(grad, "grad")
+    id_code = _embed_ids(ids, index)
+    ld, code = _embed_data(grad_out, "grad_out", ids, cols, index)
     flags = CAME_EMBED_ACCUMULATE if accumulate else 0
     if padding_row is not None:
         flags |= CAME_EMBED_PADDING_ROW
-    e = _embed_args(grad, "grad", grad_out, "grad_out", ids, scale, flags, padding_row or 0)
+    e = came_embed(grad.data_ptr(), grad_out.data_ptr(), ids.data_ptr(), rows, cols, ids.numel(), grad_ld, ld,
+                   padding_row or 0, scale, grad_code, code, id_code, flags, 0)
     size = came_embed_workspace(e)
     # from torch's allocator, for the device's current stream: not reused before the call is done
-    ws = grad_out.new_empty((size + 3) // 4, dtype=_torch().float32)
-    _call_on(grad.device, came_embed_backward, e, ws.data_ptr(), size)
+    ws = grad.new_empty((size + 3) // 4, dtype=_torch().float32)
+    _call_on(index, came_embed_backward, e, ws.data_ptr(), size)
     return grad
 
 
