@@ -4,15 +4,18 @@
 //   backward   dW[v, :] (+)= rn(scale * sum over t with id_t = v of dY[t, :])
 //
 // The backward pass sorts the tokens by id (stable, so a row's tokens keep their order), then
-// adds each row's tokens in that order in fp32: no atomics on floating-point data, results are
-// bit-reproducible.
+// adds each row's tokens in an order fixed by the ids alone, in fp32.  No element is the target of
+// two additions whose order could differ: results are bit-reproducible.
+//
+// Both are bound by their bytes where there are many tokens (128k x 4096 bf16: lookup 223 us of
+// 202 at the measured copy rate; gradient into 32000 rows 229 us of 196, 13 of them the sort that nothing
+// overlaps), and by launches and dependent round trips where there are few.
 #include "came_ops.cuh"
 
 #include <cooperative_groups.h>
 
 #include <algorithm>
 #include <cmath>
-#include <cstdio>
 
 namespace cg = cooperative_groups;
 
@@ -128,7 +131,7 @@ __device__ __forceinline__ long long column(long long slice, int group, int lane
 
 // A warp copies S slices of one token's row: S rows' pieces in flight per lane.  Bound by the bytes:
 // 128k tokens of 4096 bf16 take 229 / 241 / 338 us with 4 / 2 / 1 slices per warp; rows of one slice, and rows that
-// go in accesses below 16 bytes, are faster with one (60000 rows of 1001 bf16: 62 against 145 us).
+// go in accesses below 16 bytes, are faster with one (60000 rows of 1001 bf16: 48 against 145 us).
 // stream: the output is larger than the L2 can hold for its reader anyway, so it leaves the
 // table's rows there (223 instead of 229 us).
 template <typename I, typename T, typename O, int EV, int S>
@@ -173,15 +176,23 @@ k_embed_forward(const T* __restrict__ table, long long rows, int cols, long long
 // the blocks' counts; over all digits: a scan), so every element's place is known and nothing
 // depends on the order in which atomics arrive.  Ids that are not rows (and the padding row) get the
 // key `rows` and end up behind all others.
+//
+// Four ways by the number of tokens, each launched alone: up to kTinyTokens (below) inside the
+// sums' grid; up to kFewTokens 2.0 us; up to kOneTokens one block, 7 us at 2048 and 10 at 4096 tokens; beyond
+// that three to five short grids, 14 us at 8192 and 16384 and 23 at 131072 tokens.  Bound by the
+// latency of their dependent steps.  (One cluster of eight blocks took 61 us at 131072 tokens: scattered
+// stores go one lane per cycle and SM.  Blocks that count all tokens themselves instead of the
+// counting grid: 44 instead of 36 us for the whole gradient at 16384 tokens.  kOneTokens 2048: 20.4
+// instead of 17.2 us for the whole gradient at 3000.)
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
 constexpr int kMaxDigitBits = 9;
 constexpr int kMaxBins = 1 << kMaxDigitBits;
 constexpr int kMaxPasses = 4;            // keys below 2^31 in digits of 8 bits
-constexpr int kFewTokens = 512;          // up to here every token counts the tokens before it
+constexpr int kFewTokens = 512;          // every token counts the tokens before it
 constexpr unsigned kFewRows = 1u << 22;  // (key and position then fit one word)
-constexpr int kOneTokens = 4096;         // up to here one block sorts in its shared memory
-constexpr int kMoveThreads = 512;        // beyond that a grid of blocks that leave room for others on their SM
+constexpr int kOneTokens = 4096;         // one block sorts in its shared memory
+constexpr int kMoveThreads = 512;        // a grid of blocks that leave room for the zeroing ones on their SM
 constexpr int kMoveWarps = kMoveThreads / 32;
 constexpr int kMoveTile = 512;           // tokens per block, or a multiple of it ...
 constexpr int kMoveBlocks = 148;         // ... so that there are no more blocks than SMs
@@ -466,8 +477,15 @@ k_embed_move(const I* __restrict__ ids, SortArgs a, int pass)
 //
 // The first zero_blocks blocks write the rows without tokens instead.  They need the ids only, so
 // they do not wait for the sort: the zeros are written while it runs.
+//
+// What bounds it: the bytes at 128k tokens (5.7 TB/s of them in the whole grid); a row of one token costs
+// a warp about 40 instructions per 512 bytes, so it needs the 32 warps per SM that 64 registers allow
+// (24 or 16 warps: 238 and 255 instead of 229 us).  Copies into a ring in shared memory instead of the two
+// batches in registers: 247 us, more instructions and fewer warps.
 constexpr int kSumWarps = 8;
-constexpr int kTinyTokens = 64;          // one block's: no run crosses blocks
+constexpr int kTinyTokens = 64;          // one block's: no run crosses blocks, and it sorts for itself
+// 64 clusters: with 32 the zeroing blocks were packed onto half of the SMs (128256 rows of 4096 fp32, 8192
+// tokens: 467 instead of 355 us), with 128 the marking shows (32000 rows, 131072 tokens: 286 instead of 229).
 constexpr int kClusterBlocks = 8, kZeroClusters = 64, kZeroBlocks = kClusterBlocks * kZeroClusters;
 constexpr int kZeroWords = 2048;         // of the bit map: 65536 of a cluster's rows per round
 enum : int { kLinkHead = 1, kLinkTail = 2, kLinkThrough = 4 };
