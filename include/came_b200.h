@@ -360,14 +360,15 @@ typedef struct {
 } came_clip_params;
 
 /* Plans the tiles and allocates the context's tables and workspace; `t`: HOST array of n
- * descriptors; `device` must be current.  Synchronises the device once.  Errors of these
- * functions are reported through came_last_error(NULL) on the calling thread. */
+ * descriptors; `device` must be current.  Copies the tables and waits for that copy.  Errors of
+ * these functions are reported through came_last_error(NULL) on the calling thread. */
 came_status came_clip_create(came_clip_ctx** out, const came_clip_tensor* t, int32_t n, int32_t device);
 
 /* One launch: `results` (DEVICE fp32 [2 + n], 4-byte aligned) receives N, coef, n_0 .. n_{n-1}.
  * `grads`: HOST array of n DEVICE pointers that replace the gradients given before (the outputs of
  * tensors clipped in place move with them), or NULL.  Asynchronous on `cuda_stream`; allocates
- * nothing.  One context serves one stream at a time. */
+ * nothing but, at the first replacement, the pinned host buffer through which the table moves
+ * (make that call outside a stream capture).  One context serves one stream at a time. */
 came_status came_clip_norm(came_clip_ctx* ctx, const came_clip_params* p, const void* const* grads,
                            float* results, void* cuda_stream);
 

@@ -11,6 +11,7 @@ that fails, or a call returns an error status, a ``CameError`` is raised.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import List, Optional, Sequence
 
 from . import build as _build
@@ -354,7 +355,7 @@ def came_debug_bounds(device: int = 0) -> dict:
 
 def came_clip_create(tensors: Sequence[came_clip_tensor], device: int = 0) -> ctypes.c_void_p:
     ctx = ctypes.c_void_p()
-    arr = (came_clip_tensor * len(tensors))(*tensors)
+    arr = tensors if isinstance(tensors, ctypes.Array) else (came_clip_tensor * len(tensors))(*tensors)
     _check(load().came_clip_create(ctypes.byref(ctx), arr, len(tensors), device))
     return ctx
 
@@ -467,30 +468,36 @@ class GradClip:
             raise CameError(CAME_ERR_SHAPE, "need at least one tensor")
         if self.outs is not None and len(self.outs) != len(self.grads):
             raise CameError(CAME_ERR_SHAPE, "outs must be as many as grads")
-        self.device = self.grads[0].device
-        descs = []
-        for i, g in enumerate(self.grads):
-            o = None if self.outs is None else self.outs[i]
-            self._check_tensor(g, f"grads[{i}]")
-            if o is not None:
-                self._check_tensor(o, f"outs[{i}]")
+        first = self.grads[0]
+        _cuda_tensor(first, "grads[0]")
+        self.device = first.device
+        self._codes = [self._check_tensor(g, "grads", i) for i, g in enumerate(self.grads)]
+        packed = []
+        if self.outs is None:
+            for g, code in zip(self.grads, self._codes):
+                packed += (g.data_ptr(), 0, g.numel(), code, 0)
+        else:
+            for i, (g, o, code) in enumerate(zip(self.grads, self.outs, self._codes)):
+                out_code = self._check_tensor(o, "outs", i)
                 if o.numel() != g.numel():
                     raise CameError(CAME_ERR_SHAPE, f"outs[{i}] has another size than grads[{i}]")
-            descs.append(came_clip_tensor(g.data_ptr(), None if o is None else o.data_ptr(), g.numel(),
-                                          _dtype_code(g, f"grads[{i}]"),
-                                          0 if o is None else _dtype_code(o, f"outs[{i}]")))
-        self._codes = [d.grad_dtype for d in descs]
-        self.results = torch.zeros(2 + len(descs), dtype=torch.float32, device=self.device)
+                packed += (g.data_ptr(), o.data_ptr(), g.numel(), code, out_code)
+        n = len(self.grads)
+        descs = (came_clip_tensor * n).from_buffer_copy(struct.pack("PPqii" * n, *packed))
+        self.results = torch.empty(2 + n, dtype=torch.float32, device=self.device)
         self.total_norm, self.coef, self.tensor_norms = self.results[0], self.results[1], self.results[2:]
         self._results_at = self.results.data_ptr()
         self._params = came_clip_params()
         with torch.cuda.device(self.device):
             self.ctx = came_clip_create(descs, self.device.index)
 
-    def _check_tensor(self, x, name):
-        _cuda_tensor(x, name, None, self.device)
+    def _check_tensor(self, x, name, i) -> int:
+        """The dtype code of a tensor that may be in the list."""
+        if x.device != self.device:
+            raise CameError(CAME_ERR_DEVICE, f"{name}[{i}] must be on {self.device}")
         if not x.is_contiguous():
-            raise CameError(CAME_ERR_UNSUPPORTED, f"{name} must be contiguous")
+            raise CameError(CAME_ERR_UNSUPPORTED, f"{name}[{i}] must be contiguous")
+        return _dtype_code(x, name)
 
     def _run(self, call, max_norm, eps, grad_scale, grads):
         at = None
@@ -499,8 +506,7 @@ class GradClip:
             if len(grads) != len(self.grads):
                 raise CameError(CAME_ERR_SHAPE, "grads must be as many as at creation")
             for i, (g, old) in enumerate(zip(grads, self.grads)):
-                self._check_tensor(g, f"grads[{i}]")
-                if g.numel() != old.numel() or _dtype_code(g, f"grads[{i}]") != self._codes[i]:
+                if self._check_tensor(g, "grads", i) != self._codes[i] or g.numel() != old.numel():
                     raise CameError(CAME_ERR_SHAPE, f"grads[{i}] must keep its size and dtype")
             at = [g.data_ptr() for g in grads]
         p = self._params

@@ -467,6 +467,16 @@ came_status rebind(came_clip_ctx* c, const void* const* grads, cudaStream_t stre
     }
     if (!moved) return CAME_OK;
     cudaError_t e;
+    if (!c->pinned) {                       // only contexts whose gradients move need it
+        if ((e = cudaEventCreateWithFlags(&c->pinned_free, cudaEventDisableTiming)) != cudaSuccess)
+            return report_cuda(e, "cudaEventCreate");
+        if ((e = cudaMallocHost(&c->pinned, sizeof(ClipTensor) * c->n)) != cudaSuccess) {
+            cudaEventDestroy(c->pinned_free);
+            c->pinned = nullptr;
+            c->pinned_free = nullptr;
+            return report_cuda(e, "cudaMallocHost(table)");
+        }
+    }
     if (c->pinned_used && (e = cudaEventSynchronize(c->pinned_free)) != cudaSuccess)
         return report_cuda(e, "cudaEventSynchronize(table)");
     for (int i = 0; i < c->n; ++i) {
@@ -580,12 +590,12 @@ came_status came_clip_create(came_clip_ctx** out, const came_clip_tensor* t, int
         c->work.tile_sum = reinterpret_cast<double*>(c->d_mem + at_tile_sum);
         c->work.tensor_sum = reinterpret_cast<double*>(c->d_mem + at_tensor_sum);
         c->work.arrived = reinterpret_cast<unsigned*>(c->d_mem + at_arrived);
-        CLIP_TRY(cudaMallocHost(&c->pinned, sizeof(ClipTensor) * n), "cudaMallocHost(table)");
-        CLIP_TRY(cudaEventCreateWithFlags(&c->pinned_free, cudaEventDisableTiming), "cudaEventCreate");
-        CLIP_TRY(cudaMemset(c->work.arrived, 0, sizeof(unsigned) * (static_cast<size_t>(n) + 1)), "cudaMemset(counters)");
-        CLIP_TRY(cudaMemcpy(c->d_table, c->table.data(), sizeof(ClipTensor) * n, cudaMemcpyHostToDevice), "cudaMemcpy(table)");
-        CLIP_TRY(cudaMemcpy(c->d_tiles, tiles.data(), sizeof(ClipTile) * tiles.size(), cudaMemcpyHostToDevice), "cudaMemcpy(tiles)");
-        CLIP_TRY(cudaDeviceSynchronize(), "cudaDeviceSynchronize");
+        // one copy: the table, the tiles and (zero) everything behind them
+        std::vector<char> host(bytes, 0);
+        std::memcpy(host.data() + at_table, c->table.data(), sizeof(ClipTensor) * n);
+        std::memcpy(host.data() + at_tiles, tiles.data(), sizeof(ClipTile) * tiles.size());
+        CLIP_TRY(cudaMemcpy(c->d_mem, host.data(), bytes, cudaMemcpyHostToDevice), "cudaMemcpy(clip workspace)");
+        CLIP_TRY(cudaStreamSynchronize(nullptr), "cudaStreamSynchronize");
 #undef CLIP_TRY
     } catch (const std::bad_alloc&) {
         free_clip(c);
