@@ -549,9 +549,16 @@ came_status check_current_device(came_ctx* ctx)
 // text goes where came_last_error(NULL) finds it.
 namespace came_ops {
 
-came_status report(came_status s, const char* msg) { return fail(nullptr, s, msg); }
+came_status report(came_status s, const char* msg)
+{
+    try { return fail(nullptr, s, msg); } catch (...) { return s; }      // no memory for the text
+}
 
-came_status report_cuda(cudaError_t e, const char* what) { return cuda_fail(nullptr, e, what); }
+came_status report_cuda(cudaError_t e, const char* what)
+{
+    try { return cuda_fail(nullptr, e, what); }
+    catch (...) { return e == cudaErrorMemoryAllocation ? CAME_ERR_OOM : CAME_ERR_CUDA; }
+}
 
 came_status require_current_device(int32_t device)
 {
@@ -559,12 +566,12 @@ came_status require_current_device(int32_t device)
     const cudaError_t e = cudaGetDevice(&cur);
     if (e != cudaSuccess) {
         cudaGetLastError();
-        return fail(nullptr, CAME_ERR_DEVICE, "no usable CUDA device");
+        return report(CAME_ERR_DEVICE, "no usable CUDA device");
     }
     if (came_device_status(device, cur) == CAME_OK) return CAME_OK;
     char buf[120];
     std::snprintf(buf, sizeof buf, "the tensors live on device %d but device %d is current", device, cur);
-    return fail(nullptr, CAME_ERR_DEVICE, buf);
+    return report(CAME_ERR_DEVICE, buf);
 }
 
 }  // namespace came_ops

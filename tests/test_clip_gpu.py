@@ -134,6 +134,18 @@ def test_large_small_and_non_finite_values(env, gdt):
     assert float(n) == 0 and float(c) == 1 and float(each[0]) == 0
 
 
+def test_more_than_two_to_the_31_elements(env):
+    torch, binding = env
+    n = (1 << 31) + 17
+    g = torch.full((n + 3,), 0.5, dtype=torch.bfloat16, device="cuda")[3:]
+    out = torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    norm, coef, _ = binding.GradClip([g], [out]).clip(0.25 * n ** 0.5)
+    assert abs(float(norm) - 0.5 * n ** 0.5) <= NORM_TOL * 0.5 * n ** 0.5
+    want = (0.5 * coef).bfloat16()
+    assert bool((out[:1000] == want).all()) and bool((out[-1000:] == want).all())
+    assert int((out == want).sum()) == n
+
+
 def test_results_do_not_depend_on_timing_or_stream(env):
     torch, binding = env
     g = [torch.randn(n, device="cuda") for n in (5_000_003, 17, 1_000_000)]
