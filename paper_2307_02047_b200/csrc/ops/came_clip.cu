@@ -9,10 +9,10 @@
 // without waiting: the last tile of a tensor to arrive adds that tensor's partials, the last
 // tensor adds the tensors', both in a fixed order, so results do not depend on timing.
 //
-// Bound by the bytes: 13.5 GB of bf16 in 1816 us (7.4 TB/s, 1.14 of the measured copy rate, which also
-// writes), 436 MB of fp32 in 72 us (6.1 TB/s); a set of 0.5 MB takes 4.5 us on the device, a
+// Bound by the bytes: 13.5 GB of bf16 in 1812 us (7.4 TB/s, 1.14 of the measured copy rate, which also
+// writes), 436 MB of fp32 in 70.4 us (6.2 TB/s); a set of 0.5 MB takes 4.5 us on the device, a
 // chain of dependent round trips.  Writing clipped copies reads a set larger than the L2 twice: 709 MB
-// bf16 to bf16 in 338 us, 6.1 TB/s of the 2.03 GB that move.
+// bf16 to bf16 in 337 us, 6.0 TB/s of the 2.03 GB that move.
 #include "came_ops.cuh"
 
 #include <algorithm>
@@ -170,9 +170,15 @@ __device__ __forceinline__ void store_total(double sum, const ClipConsts& hc, fl
 // A warp's sum of count values that other blocks have written.
 __device__ __forceinline__ double warp_sum_of(const double* p, int count, int lane)
 {
+    constexpr int B = 8;                                 // loads of one round trip
     double s = 0.0;
-#pragma unroll 4
-    for (int k = lane; k < count; k += 32) s += __ldcg(p + k);
+    for (int k = lane; k < count; k += B * 32) {
+        double v[B];
+#pragma unroll
+        for (int u = 0; u < B; ++u) v[u] = k + u * 32 < count ? __ldcg(p + k + u * 32) : 0.0;
+#pragma unroll
+        for (int u = 0; u < B; ++u) s += v[u];
+    }
     return warp_sum(s);
 }
 
@@ -180,8 +186,11 @@ __device__ __forceinline__ double warp_sum_of(const double* p, int count, int la
 // saves a round of store, fence and atomic (1.5 us of a small call), but one block reads
 // all partial sums: for lists of up to kFlatTiles tiles.  Else the last tile of each tensor adds the
 // tensor's sums, and the last tensor the tensors'.
+//
+// Resident blocks: sets of a thousand tiles want them in one wave (32 MB: 12.6 us with seven per SM, 14.0 with
+// six); larger ones are better off with five that need no spilled registers (436 MB: 70.7 against 74.2).
 template <bool kFlat, int kUnroll>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kUnroll == 4 ? 7 : 5)
 k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles, int n, ClipWork w,
             ClipConsts hc, float* __restrict__ results)
 {
@@ -225,17 +234,21 @@ k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles
     } else {
         if (warp > 0) return;
         // one warp: arrive, and finish the tensor / the whole list when last
-        unsigned last = 0;
+        unsigned last = 1;
         if (lane == 0) {
             s = 0.0;
             for (int k = 0; k < kThreads / 32; ++k) s += red[k];
-            w.tile_sum[blockIdx.x] = s;
-            publish();
-            last = atomicAdd(&w.arrived[t.tensor], 1u) == static_cast<unsigned>(d.ntiles - 1);
-            publish();
+            if (d.ntiles > 1) {
+                w.tile_sum[blockIdx.x] = s;
+                publish();
+                last = atomicAdd(&w.arrived[t.tensor], 1u) == static_cast<unsigned>(d.ntiles - 1);
+                publish();
+            }
         }
-        if (!__shfl_sync(0xffffffffu, last, 0)) return;
-        s = warp_sum_of(w.tile_sum + d.tile0, d.ntiles, lane);
+        if (d.ntiles > 1) {                              // (a tensor of one tile is finished)
+            if (!__shfl_sync(0xffffffffu, last, 0)) return;
+            s = warp_sum_of(w.tile_sum + d.tile0, d.ntiles, lane);
+        }
         if (lane == 0) {
             w.arrived[t.tensor] = 0u;
             w.tensor_sum[t.tensor] = s;
@@ -444,9 +457,9 @@ came_status validate_clip_params(const came_clip_params& p)
     return CAME_OK;
 }
 
-// Bytes of gradient per tile.  Up to 64 KB: about a thousand tiles, one wave of blocks (32 MB of fp32 take
-// 12.2 us, 14.6 with twice and 13.1 with half as many).  Above: about two thousand of up to 512 KB,
-// whose threads have eight loads in flight (436 MB: 72 us, against 76 with 64 KB tiles and four loads).
+// Bytes of gradient per tile.  Up to 64 KB: about a thousand tiles, one wave of blocks (32 MB of fp32 took
+// 12.2 us, against 14.6 with twice and 13.1 with half as many).  Above: about two thousand of up to
+// 512 KB, whose threads have eight loads in flight (436 MB: 70 us, against 76 with 64 KB tiles and four loads).
 int tile_bytes_for(double total_bytes)
 {
     long long bytes = 16 << 10;
