@@ -386,8 +386,8 @@ came_status came_clip_destroy(came_clip_ctx* ctx);
  * Backward:  dW[v, :] = rn(scale * sum over the tokens t with id_t = v of dY[t, :]), every row
  *            written (rows without tokens with 0); with CAME_EMBED_ACCUMULATE
  *            dW[v, :] = rn(dW[v, :] + scale * sum ...), rows without tokens untouched.
- * The sums are fp32, a row's tokens are added in an order fixed by the ids alone, and each result
- * is rounded once: results are bit-reproducible.  Lengths from zero tokens and one column up; rows
+ * The sums and their products with the scale are fp32, a row's tokens are added in an order fixed
+ * by the ids alone, and what is stored is rounded to its type once: results are bit-reproducible.  Lengths from zero tokens and one column up; rows
  * may have any stride >= cols and any element-aligned address (aligned ones are faster).  The
  * output shares no memory with an input (CAME_ERR_OVERLAP). */
 typedef enum { CAME_I32 = 0, CAME_I64 = 1 } came_id_dtype;
