@@ -367,8 +367,10 @@ came_status came_clip_create(came_clip_ctx** out, const came_clip_tensor* t, int
 /* One launch: `results` (DEVICE fp32 [2 + n], 4-byte aligned) receives N, coef, n_0 .. n_{n-1}.
  * `grads`: HOST array of n DEVICE pointers that replace the gradients given before (the outputs of
  * tensors clipped in place move with them), or NULL.  Asynchronous on `cuda_stream`; allocates
- * nothing but, at the first replacement, the pinned host buffer through which the table moves
- * (make that call outside a stream capture).  One context serves one stream at a time. */
+ * nothing but, at the first replacement, the pinned host buffer through which the table moves.
+ * Inside a stream capture the call may only be given the gradients that the context already has
+ * (CAME_ERR_UNSUPPORTED for others, and nothing changes); a captured call works, at each replay, on
+ * those that the context has then.  One context serves one stream at a time. */
 came_status came_clip_norm(came_clip_ctx* ctx, const came_clip_params* p, const void* const* grads,
                            float* results, void* cuda_stream);
 

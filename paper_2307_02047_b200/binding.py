@@ -526,7 +526,8 @@ class GradClip:
 
     def norm(self, max_norm: float = float("inf"), eps: float = 1e-6, grad_scale: float = 1.0,
              grads=None):
-        """``(total_norm, coef, tensor_norms)``; ``grads`` replaces the tensors of earlier calls."""
+        """``(total_norm, coef, tensor_norms)``; ``grads`` replaces the tensors of earlier calls
+        (not inside a stream capture)."""
         return self._run(self._norm_call, max_norm, eps, grad_scale, grads)
 
     def clip(self, max_norm: float, eps: float = 1e-6, grad_scale: float = 1.0, grads=None):

@@ -479,7 +479,15 @@ came_status rebind(came_clip_ctx* c, const void* const* grads, cudaStream_t stre
         moved |= d.g != grads[i];
     }
     if (!moved) return CAME_OK;
-    cudaError_t e;
+    // A captured copy would run at the graph's replay, out of the staging buffer as it is then, while
+    // the table here would count as copied from now on.
+    cudaStreamCaptureStatus capture;
+    cudaError_t e = cudaStreamIsCapturing(stream, &capture);
+    if (e == cudaErrorStreamCaptureImplicit || (e == cudaSuccess && capture != cudaStreamCaptureStatusNone)) {
+        cudaGetLastError();
+        return report(CAME_ERR_UNSUPPORTED, "gradients cannot be replaced while the stream captures");
+    }
+    if (e != cudaSuccess) return report_cuda(e, "cudaStreamIsCapturing");
     if (!c->pinned) {                       // only contexts whose gradients move need it
         if ((e = cudaEventCreateWithFlags(&c->pinned_free, cudaEventDisableTiming)) != cudaSuccess)
             return report_cuda(e, "cudaEventCreate");
