@@ -468,6 +468,26 @@ int tile_bytes_for(double total_bytes)
     return static_cast<int>(bytes);
 }
 
+// The rule of check_overlap for the list that replacing the gradients would make.
+came_status check_moved(const came_clip_ctx* c, const void* const* grads)
+{
+    if (!c->has_out) return CAME_OK;
+    try {
+        std::vector<came_clip_tensor> t(c->n);
+        for (int i = 0; i < c->n; ++i) {
+            const ClipTensor& d = c->table[i];
+            t[i].grad = grads[i];
+            t[i].out = d.in_place ? const_cast<void*>(grads[i]) : d.out;
+            t[i].numel = d.n;
+            t[i].grad_dtype = d.g_bf16 ? CAME_BF16 : CAME_F32;
+            t[i].out_dtype = d.out_bf16 ? CAME_BF16 : CAME_F32;
+        }
+        return check_overlap(t.data(), c->n);
+    } catch (const std::bad_alloc&) {
+        return report(CAME_ERR_OOM, "host allocation failed");
+    }
+}
+
 came_status rebind(came_clip_ctx* c, const void* const* grads, cudaStream_t stream)
 {
     bool moved = false;
@@ -479,6 +499,8 @@ came_status rebind(came_clip_ctx* c, const void* const* grads, cudaStream_t stre
         moved |= d.g != grads[i];
     }
     if (!moved) return CAME_OK;
+    const came_status s = check_moved(c, grads);
+    if (s != CAME_OK) return s;
     // A captured copy would run at the graph's replay, out of the staging buffer as it is then, while
     // the table here would count as copied from now on.
     cudaStreamCaptureStatus capture;

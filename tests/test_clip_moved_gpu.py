@@ -1,4 +1,4 @@
-"""Gradients that are replaced between calls of one GradClip: what a stream capture may hold."""
+"""Gradients that are replaced between calls of one GradClip: in a stream capture, and over outputs."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -64,3 +64,48 @@ def test_the_first_replacement_inside_a_capture_is_refused(env):
             refused = e.status
     assert refused == binding.CAME_ERR_UNSUPPORTED
     assert _is_norm_of(clip.norm(), a) and _is_norm_of(clip.norm(grads=b), b)
+
+
+def test_a_replacement_that_meets_an_output_is_refused(env):
+    """Blocks that write one tensor's output must not race with blocks that read another's gradient."""
+    torch, binding = env
+    buf = torch.zeros(4 * 8192, device="cuda")
+    g, fresh = _lists(torch, (1, 2), sizes=(5000, 5000))
+    outs = [buf[:5000], buf[8192:13192]]
+
+    def refused(clip, grads):
+        for call in (lambda: clip.clip(1.0, grads=grads), lambda: clip.norm(1.0, grads=grads)):
+            with pytest.raises(binding.CameError) as e:
+                call()
+            assert e.value.status == binding.CAME_ERR_OVERLAP
+            assert clip.grads[0] is g[0]
+
+    clip = binding.GradClip(g, outs)
+    refused(clip, [outs[1], outs[0]])                    # each over the other's output
+    refused(clip, [buf[8:5008], g[1]])                   # eight elements into its own output
+    refused(clip, [g[0], buf[13191:18191]])              # the last element of an output
+    assert bool((buf == 0).all())
+    _, coef, _ = clip.clip(1.0)                          # the context still works, on the gradients that it had
+    assert torch.equal(outs[0], g[0] * coef) and torch.equal(outs[1], g[1] * coef)
+    _, coef, _ = clip.clip(1.0, grads=fresh)
+    assert torch.equal(outs[0], fresh[0] * coef) and torch.equal(outs[1], fresh[1] * coef)
+    old = outs[0].clone()                                # exactly its own output: in place
+    _, coef, _ = clip.clip(0.5, grads=[outs[0], fresh[1]])
+    assert torch.equal(outs[0], old * coef) and torch.equal(outs[1], fresh[1] * coef)
+    _, coef, _ = clip.clip(1.0, grads=[g[0], buf[13192:18192]])          # right behind an output
+    assert torch.equal(outs[0], g[0] * coef) and bool((outs[1] == 0).all())
+
+    clip = binding.GradClip(g, g)                        # in place: the outputs move with the gradients
+    refused(clip, [buf[:5000], buf[3000:8000]])
+    halves = [buf[16384:21384], buf[21384:26384]]
+    for h in halves:
+        h.fill_(3.0)
+    _, coef, _ = clip.clip(1.0, grads=halves)
+    assert all(torch.equal(h, torch.full_like(h, 3.0) * coef) for h in halves)
+
+    wide = torch.ones(5000, device="cuda")               # in place, but another type
+    clip = binding.GradClip(g, [wide.view(torch.bfloat16)[:5000], torch.empty(5000, device="cuda", dtype=torch.bfloat16)])
+    refused(clip, [wide, g[1]])
+    assert bool((wide == 1).all())
+    clip = binding.GradClip(g)                           # without outputs nothing can meet
+    assert _is_norm_of(clip.norm(grads=[wide, wide]), [wide, wide])
