@@ -522,15 +522,21 @@ came_status rebind(came_clip_ctx* c, const void* const* grads, cudaStream_t stre
     }
     if (c->pinned_used && (e = cudaEventSynchronize(c->pinned_free)) != cudaSuccess)
         return report_cuda(e, "cudaEventSynchronize(table)");
+    std::copy(c->table.begin(), c->table.end(), c->pinned);
     for (int i = 0; i < c->n; ++i) {
-        c->table[i].g = grads[i];
-        if (c->table[i].in_place) c->table[i].out = const_cast<void*>(grads[i]);
-        c->table[i].vec_out = groups_agree(c->table[i]);
+        ClipTensor& d = c->pinned[i];
+        d.g = grads[i];
+        if (d.in_place) d.out = const_cast<void*>(grads[i]);
+        d.vec_out = groups_agree(d);
     }
-    std::memcpy(c->pinned, c->table.data(), sizeof(ClipTensor) * c->n);
     e = cudaMemcpyAsync(c->d_table, c->pinned, sizeof(ClipTensor) * c->n, cudaMemcpyHostToDevice, stream);
     if (e != cudaSuccess) return report_cuda(e, "cudaMemcpyAsync(table)");
-    if ((e = cudaEventRecord(c->pinned_free, stream)) != cudaSuccess) return report_cuda(e, "cudaEventRecord(table)");
+    // from here on the device has, or will have, these: what is kept here never runs ahead of it
+    std::copy(c->pinned, c->pinned + c->n, c->table.begin());
+    if ((e = cudaEventRecord(c->pinned_free, stream)) != cudaSuccess) {
+        cudaStreamSynchronize(stream);      // (nothing would tell when the buffer is free)
+        return report_cuda(e, "cudaEventRecord(table)");
+    }
     c->pinned_used = true;
     return CAME_OK;
 }
