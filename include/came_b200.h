@@ -368,6 +368,8 @@ came_status came_clip_create(came_clip_ctx** out, const came_clip_tensor* t, int
  * `grads`: HOST array of n DEVICE pointers that replace the gradients given before (the outputs of
  * tensors clipped in place move with them), or NULL.  Asynchronous on `cuda_stream`; allocates
  * nothing but, at the first replacement, the pinned host buffer through which the table moves.
+ * It has two slots: a call that replaces gradients waits on the host until the copy that the last
+ * but one such call queued has run, and for nothing else.
  * Inside a stream capture the call may only be given the gradients that the context already has
  * (CAME_ERR_UNSUPPORTED for others, and nothing changes); a captured call works, at each replay, on
  * those that the context has then.  One context serves one stream at a time. */

@@ -369,9 +369,12 @@ struct came_clip_ctx {
     ClipTensor* d_table = nullptr;
     ClipTile*   d_tiles = nullptr;
     ClipWork    work = {};
-    ClipTensor* pinned = nullptr;           // staging of the table when gradients move
-    cudaEvent_t pinned_free = nullptr;
-    bool        pinned_used = false;
+    // staging of the table when gradients move, made at the first move; two slots, taken in turn, so
+    // that a call does not wait for the copy of the call before it
+    ClipTensor* pinned[2] = {nullptr, nullptr};
+    cudaEvent_t pinned_free[2] = {nullptr, nullptr};
+    bool        pinned_used[2] = {false, false};
+    int         pinned_next = 0;
 };
 
 namespace {
@@ -380,8 +383,9 @@ void free_clip(came_clip_ctx* c)
 {
     if (!c) return;
     cudaFree(c->d_mem);
-    if (c->pinned) cudaFreeHost(c->pinned);
-    if (c->pinned_free) cudaEventDestroy(c->pinned_free);
+    if (c->pinned[0]) cudaFreeHost(c->pinned[0]);
+    for (cudaEvent_t e : c->pinned_free)
+        if (e) cudaEventDestroy(e);
     delete c;
 }
 
@@ -510,34 +514,36 @@ came_status rebind(came_clip_ctx* c, const void* const* grads, cudaStream_t stre
         return report(CAME_ERR_UNSUPPORTED, "gradients cannot be replaced while the stream captures");
     }
     if (e != cudaSuccess) return report_cuda(e, "cudaStreamIsCapturing");
-    if (!c->pinned) {                       // only contexts whose gradients move need it
-        if ((e = cudaEventCreateWithFlags(&c->pinned_free, cudaEventDisableTiming)) != cudaSuccess)
-            return report_cuda(e, "cudaEventCreate");
-        if ((e = cudaMallocHost(&c->pinned, sizeof(ClipTensor) * c->n)) != cudaSuccess) {
-            cudaEventDestroy(c->pinned_free);
-            c->pinned = nullptr;
-            c->pinned_free = nullptr;
+    if (!c->pinned[0]) {
+        for (cudaEvent_t& free : c->pinned_free)
+            if (!free && (e = cudaEventCreateWithFlags(&free, cudaEventDisableTiming)) != cudaSuccess)
+                return report_cuda(e, "cudaEventCreate");
+        if ((e = cudaMallocHost(&c->pinned[0], 2 * sizeof(ClipTensor) * c->n)) != cudaSuccess) {
+            c->pinned[0] = nullptr;
             return report_cuda(e, "cudaMallocHost(table)");
         }
+        c->pinned[1] = c->pinned[0] + c->n;
     }
-    if (c->pinned_used && (e = cudaEventSynchronize(c->pinned_free)) != cudaSuccess)
+    const int k = c->pinned_next;
+    if (c->pinned_used[k] && (e = cudaEventSynchronize(c->pinned_free[k])) != cudaSuccess)
         return report_cuda(e, "cudaEventSynchronize(table)");
-    std::copy(c->table.begin(), c->table.end(), c->pinned);
+    ClipTensor* const to = c->pinned[k];
+    std::copy(c->table.begin(), c->table.end(), to);
     for (int i = 0; i < c->n; ++i) {
-        ClipTensor& d = c->pinned[i];
-        d.g = grads[i];
-        if (d.in_place) d.out = const_cast<void*>(grads[i]);
-        d.vec_out = groups_agree(d);
+        to[i].g = grads[i];
+        if (to[i].in_place) to[i].out = const_cast<void*>(grads[i]);
+        to[i].vec_out = groups_agree(to[i]);
     }
-    e = cudaMemcpyAsync(c->d_table, c->pinned, sizeof(ClipTensor) * c->n, cudaMemcpyHostToDevice, stream);
+    e = cudaMemcpyAsync(c->d_table, to, sizeof(ClipTensor) * c->n, cudaMemcpyHostToDevice, stream);
     if (e != cudaSuccess) return report_cuda(e, "cudaMemcpyAsync(table)");
     // from here on the device has, or will have, these: what is kept here never runs ahead of it
-    std::copy(c->pinned, c->pinned + c->n, c->table.begin());
-    if ((e = cudaEventRecord(c->pinned_free, stream)) != cudaSuccess) {
-        cudaStreamSynchronize(stream);      // (nothing would tell when the buffer is free)
+    std::copy(to, to + c->n, c->table.begin());
+    if ((e = cudaEventRecord(c->pinned_free[k], stream)) != cudaSuccess) {
+        cudaStreamSynchronize(stream);      // (nothing would tell when the slot is free)
         return report_cuda(e, "cudaEventRecord(table)");
     }
-    c->pinned_used = true;
+    c->pinned_used[k] = true;
+    c->pinned_next = k ^ 1;
     return CAME_OK;
 }
 

@@ -1,4 +1,5 @@
-"""Gradients that are replaced between calls of one GradClip: in a stream capture, and over outputs."""
+"""Gradients that are replaced between calls of one GradClip: in a stream capture, over outputs, and while
+the GPU is busy."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +110,22 @@ def test_a_replacement_that_meets_an_output_is_refused(env):
     assert bool((wide == 1).all())
     clip = binding.GradClip(g)                           # without outputs nothing can meet
     assert _is_norm_of(clip.norm(grads=[wide, wide]), [wide, wide])
+
+
+def test_replacements_do_not_wait_for_the_gpu(env):
+    """Two calls whose gradients have moved return while the stream still works on what came before."""
+    torch, binding = env
+    a, b = _lists(torch, (1, 2))
+    clip = binding.GradClip(a)
+    clip.norm(grads=b)
+    clip.norm(grads=a)
+    torch.cuda.synchronize()
+    done = torch.cuda.Event()
+    torch.cuda._sleep(1_000_000_000)                     # half a second
+    done.record()
+    clip.norm(grads=b)
+    clip.norm(grads=a)
+    assert not done.query()
+    for k in range(9):                                   # every call finds the addresses that it was given
+        now = b if k % 2 else a
+        assert _is_norm_of(clip.norm(grads=now), now)
