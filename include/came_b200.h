@@ -335,8 +335,8 @@ came_status came_factor_update_static_plan(const void* grad, int32_t grad_dtype,
  *   coef = 1                               if N + eps <= max_norm
  *        = max_norm / (N + eps)            otherwise
  *   out_ij = g_ij * (s * coef)             rounded once, to nearest even (came_clip_grads only)
- * Squares are added in fp32 within a thread (a few hundred terms) and in double from there on, in
- * a fixed order: results are bit-reproducible.  A finite N is found even where squares overflow
+ * Squares are added in fp32 for up to 32 terms (and one of a tensor's ends) and in double from there
+ * on, in a fixed order: results are bit-reproducible.  A finite N is found even where squares overflow
  * fp32; gradients below 1e-19 in magnitude may count as zero.  Inf or NaN in a gradient gives
  * N = inf or NaN and coef = 0 or NaN, as the formulas do; nothing is skipped.
  *

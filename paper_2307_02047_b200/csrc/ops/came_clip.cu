@@ -5,7 +5,7 @@
 //   out_ij = rn(g_ij * (s * coef))
 //
 // One grid reads every gradient once: a block per tile of one tensor, the tile's sum of squares
-// in fp32 per thread (a few hundred terms) and in double from there on.  The sums are finished
+// in fp32 for up to 32 terms and in double from there on.  The sums are finished
 // without waiting: the last tile of a tensor to arrive adds that tensor's partials, the last
 // tensor adds the tensors', both in a fixed order, so results do not depend on timing.
 //
@@ -106,15 +106,22 @@ __device__ __forceinline__ Span span_of(const ClipTensor& d, const T* g, int ind
     return s;
 }
 
-// Sum of squares of this thread's share of the tile.
+// Sum of squares of this thread's share of the tile.  At most 32 squares (and one of the tile's ragged
+// ends) go into one fp32 accumulator: what follows is added in double.  Tiles of up to 64 KB have no more than
+// that; of larger ones (kUnroll 8) every batch starts anew.  Longer chains lose more than their length
+// suggests: the square of a bf16 has so few bits that roundings of one sign prevail (normal values:
+// the sum is low by 2.5e-7 at 256 squares, 2e-8 at 32), and squares below half a spacing vanish.
 template <int kUnroll, typename T>
 __device__ __forceinline__ double tile_squares(const ClipTensor& d, int index)
 {
     constexpr int N = Pack<T>::N;
+    constexpr bool kAnew = kUnroll == 8;
     const T* const g = static_cast<const T*>(d.g);
     const Span s = span_of<T>(d, g, index, N);
     const int tid = threadIdx.x;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    double sum = 0.0;                                    // of the batches before
+    auto joined = [&] { return static_cast<double>((acc[0] + acc[1]) + (acc[2] + acc[3])); };
     const int packs = static_cast<int>((s.b - s.a) / N);
     const T* const body = g + s.a;
     int k = tid;
@@ -124,6 +131,11 @@ __device__ __forceinline__ double tile_squares(const ClipTensor& d, int index)
         for (int u = 0; u < kUnroll; ++u) p[u].load(body + static_cast<long long>(k + u * kThreads) * N);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) p[u].add_squares(acc);
+        if constexpr (kAnew) {
+            sum += joined();
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = 0.f;
+        }
     }
     {
         Pack<T> p[kUnroll];
@@ -144,8 +156,8 @@ __device__ __forceinline__ double tile_squares(const ClipTensor& d, int index)
         const float x = to_float(g[rest]);
         acc[1] = fmaf(x, x, acc[1]);
     }
-    const float sum = (acc[0] + acc[1]) + (acc[2] + acc[3]);
-    if (sum <= 3.0e38f) return static_cast<double>(sum);
+    sum += joined();
+    if (isfinite(sum)) return sum;
     // An element beyond 1.8e19 overflows an fp32 square although the norm is finite: the
     // thread adds its share once more, in double.  (Inf and NaN come out as they are.)
     double wide = 0.0;
