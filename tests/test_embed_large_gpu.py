@@ -1,0 +1,59 @@
+"""The lookup's gradient where a warp has more than 32 sorted tokens, as training batches of wide models do.
+
+Whole numbers small enough that every sum is exact in fp32, whatever its order: the fp32 result equals
+the one in 64 bits, the bf16 result is that one rounded."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2307_02047_b200 import binding
+    assert torch.cuda.is_available()
+    return torch, binding
+
+
+def _ids(torch, kind, tokens, rows, gen):
+    if kind == "same":
+        return torch.full((tokens,), rows // 2, device="cuda")
+    if kind == "hot":                        # frequencies that fall as 1 / rank
+        u = torch.rand(tokens, generator=gen, device="cuda", dtype=torch.float64)
+        return (torch.exp(u * torch.log(torch.tensor(rows + 1.0, dtype=torch.float64))) - 1).long().clamp_(0, rows - 1)
+    ids = torch.randint(0, rows, (tokens,), generator=gen, device="cuda")
+    if kind == "padded":                     # three of four tokens are no rows: warps whose later groups are empty
+        ids[torch.rand(tokens, generator=gen, device="cuda") < 0.75] = -1
+    return ids
+
+
+@pytest.mark.parametrize("tokens,cols,gap,kind,rows", [
+    (70_001, 4096, 0, "hot", 32_000),        # 64 tokens per warp; 8 columns per access
+    (70_001, 4096, 0, "any", 300),           # runs of 233
+    (70_001, 4095, 0, "hot", 32_000),        # one column per access
+    (70_001, 4092, 4, "padded", 5_000),      # four
+    (65_600, 4096, 0, "any", 60_000),        # runs of one
+    (65_536, 4096, 0, "same", 7),            # one run across all blocks
+    (270_000, 4096, 0, "hot", 32_000),       # 128 per warp
+    (270_007, 4095, 1, "any", 1_000),
+    (270_007, 4096, 0, "padded", 200_000),
+])
+@pytest.mark.parametrize("ydt,gdt", [("bfloat16", "bfloat16"), ("bfloat16", "float32"), ("float32", "float32"), ("float32", "bfloat16")])
+def test_every_group_of_a_warp_is_added(env, tokens, cols, gap, kind, rows, ydt, gdt):
+    torch, binding = env
+    gen = torch.Generator(device="cuda").manual_seed(tokens + cols)
+    ids = _ids(torch, kind, tokens, rows, gen)
+    ids = ids.int() if rows % 2 else ids
+    draw = lambda n: torch.randint(-3, 4, (n, cols + gap), generator=gen, device="cuda", dtype=torch.int8)  # noqa: E731
+    dy = draw(tokens).to(getattr(torch, ydt))[:, :cols]
+    for accumulate in (False, True):
+        grad = draw(rows).to(getattr(torch, gdt))[:, :cols]
+        old = grad.clone()
+        binding.embed_backward(dy, ids, grad, 2.0, accumulate=accumulate)
+        ok = (ids >= 0).nonzero()[:, 0]
+        for a in range(0, cols, 1024):       # the reference in 64 bits, by columns
+            part = slice(a, min(cols, a + 1024))
+            want = old[:, part].double() if accumulate else torch.zeros_like(old[:, part], dtype=torch.float64)
+            want.index_add_(0, ids[ok].long(), 2.0 * dy[ok, part].double())
+            assert float(want.abs().max()) < 2 ** 24
+            assert torch.equal(grad[:, part], want.to(grad.dtype))
