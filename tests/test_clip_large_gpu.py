@@ -40,3 +40,80 @@ def test_no_one_sided_error_on_normal_values(env, dtype):
     got = float(binding.GradClip([g]).norm()[0])
     want = sum(float((p.double() ** 2).sum()) for p in g.split(1 << 26)) ** 0.5
     assert abs(got - want) <= (2.0 ** -24 + 1e-8) * want
+
+
+def _views(torch, sizes, offsets, dtype):
+    """Tensors of one flat buffer, each `offset` elements behind a 64-byte boundary."""
+    at, starts = 0, []
+    for n, o in zip(sizes, offsets):
+        starts.append(at + o)
+        at += -(-(n + o) // 32) * 32
+    flat = torch.zeros(at, dtype=getattr(torch, dtype), device="cuda")
+    return flat, [flat[s:s + n] for s, n in zip(starts, sizes)]
+
+
+SIZES = {   # elements; tiles of 128 KB and of 512 KB
+    "fp32, 128 KB": ("float32", [20_000_003, 5, 19_000_001, 1000, 3 * 32768 + 1, 0, 7_123_457]),
+    "bf16, 128 KB": ("bfloat16", [40_000_003, 5, 38_000_001, 1000, 3 * 65536 + 1, 0, 7_123_457]),
+    "fp32, 512 KB": ("float32", [90_000_003, 5, 60_000_001, 1000, 3 * 131072 + 1, 0, 7_123_457]),
+    "bf16, 512 KB": ("bfloat16", [190_000_003, 5, 120_000_001, 1000, 3 * 262144 + 1, 0, 7_123_457]),
+}
+OFFSETS = [3, 0, 17, 1, 31, 5, 8]
+
+
+@pytest.mark.parametrize("odt", ["float32", "bfloat16", "in place"])
+@pytest.mark.parametrize("case", list(SIZES))
+def test_large_lists_of_odd_tensors(env, case, odt):
+    """Norms against 64 bits; outputs bit for bit given the coefficient."""
+    torch, binding = env
+    dtype, sizes = SIZES[case]
+    flat, grads = _views(torch, sizes, OFFSETS, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(len(odt))
+    for i, g in enumerate(grads):
+        g.normal_(0, 10.0 ** (-1 - i % 3), generator=gen)
+    before = flat.clone()
+    if odt == "in place":
+        out_flat, outs = flat, grads
+    else:                                    # every other output at another offset than its gradient
+        out_flat, outs = _views(torch, sizes, [o + i % 2 for i, o in enumerate(OFFSETS)], odt)
+    old = [before[g.storage_offset():g.storage_offset() + g.numel()] for g in grads]
+    want = [sum(float((p.double() ** 2).sum()) for p in g.split(1 << 26)) ** 0.5 if g.numel() else 0.0 for g in grads]
+    N = sum(w * w for w in want) ** 0.5
+    total, coef, each = binding.GradClip(grads, outs).clip(0.5, 0.0)
+    assert abs(float(total) - N) <= NORM_TOL * N
+    assert abs(float(coef) - 0.5 / N) <= NORM_TOL * 0.5 / N
+    for got, w in zip(each.tolist(), want):
+        assert abs(got - w) <= NORM_TOL * w
+    for o, g in zip(outs, old):
+        for p, q in zip(o.split(1 << 26), g.split(1 << 26)):
+            assert torch.equal(p, (q.float() * coef).to(o.dtype))
+    if odt != "in place":
+        assert torch.equal(flat, before)
+    gaps = torch.ones(out_flat.numel(), dtype=torch.bool, device="cuda")
+    for o in outs:
+        gaps[o.storage_offset():o.storage_offset() + o.numel()] = False
+    assert bool((out_flat[gaps] == 0).all())
+
+
+@pytest.mark.parametrize("case", list(SIZES))
+def test_every_element_counts_once(env, case):
+    """Tensors of zeros with a few ones, at their ends, around the borders of tiles and anywhere: a norm is
+    the square root of their number, exactly, and one that is missed or counted twice changes it."""
+    torch, binding = env
+    dtype, sizes = SIZES[case]
+    flat, grads = _views(torch, sizes, OFFSETS, dtype)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    counts = []
+    for g in grads:
+        if g.numel():
+            at = [torch.tensor([0, g.numel() - 1], device="cuda")]
+            tile = 16 * 1024                 # borders of tiles are among its multiples, counted from the start or the first aligned element
+            border = torch.randint(0, g.numel() // tile + 1, (40,), generator=gen, device="cuda") * tile
+            at += [border + k for k in range(-33, 34)] + [torch.randint(0, g.numel(), (200,), generator=gen, device="cuda")]
+            at = torch.cat(at)
+            g[at[(at >= 0) & (at < g.numel())]] = 1
+        counts.append(int(g.count_nonzero()))
+    total, coef, each = binding.GradClip(grads).norm()
+    assert each.tolist() == torch.tensor(counts, dtype=torch.float64).sqrt().float().tolist()
+    assert float(total) == float(torch.tensor(float(sum(counts)), dtype=torch.float64).sqrt().float())
+    assert float(coef) == 1

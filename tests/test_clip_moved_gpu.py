@@ -129,3 +129,30 @@ def test_replacements_do_not_wait_for_the_gpu(env):
     for k in range(9):                                   # every call finds the addresses that it was given
         now = b if k % 2 else a
         assert _is_norm_of(clip.norm(grads=now), now)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("count", [1, 600])
+def test_outputs_of_moved_gradients(env, dtype, count):
+    """Gradients that move to other alignments than their outputs and back: written wide, one by one, wide.
+    count tensors: the list's sums are finished in one stage, or in two."""
+    torch, binding = env
+    dtype = getattr(torch, dtype)
+    sizes = [4097, 300, 8192][:max(1, min(3, count))] * max(1, count // 3)
+    flat = torch.empty(sum(sizes) + 16 * len(sizes), device="cuda", dtype=dtype)
+
+    def views(flat, shift):
+        at, got = 0, []
+        for n in sizes:
+            got.append(flat[at + shift:at + shift + n])
+            at += n // 8 * 8 + 16
+        return got
+
+    outs = views(torch.empty_like(flat), 0)
+    clip = binding.GradClip([g.normal_() for g in views(flat, 0)], outs)
+    for shift in (0, 1, 7, 8, 2, 0):
+        grads = views(torch.randn(flat.numel(), device="cuda").to(dtype), shift)
+        total, coef, _ = clip.clip(0.25, grads=grads)
+        want = sum(float((g.double() ** 2).sum()) for g in grads) ** 0.5
+        assert abs(float(total) - want) <= 2.5e-6 * want                 # 64 * 2^-24 / 2 of a sum of squares, and its rounding
+        assert all(torch.equal(o, (g.float() * coef).to(dtype)) for o, g in zip(outs, grads))
