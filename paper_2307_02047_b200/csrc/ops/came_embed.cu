@@ -563,13 +563,18 @@ __device__ __forceinline__ void join_blocks(const SumArgs& a, O* grad, unsigned 
         last += found ? __ffs(found) : 32;
         ends = found != 0;
     }
-    publish();
+    // The warp's parts are ordered before lane 0's fence, and with it before its arrival; what the others
+    // have published, behind it, before the warp's reads.  (A shuffle orders no memory.)
     __syncwarp();
     unsigned final = 0;
-    if (lane == 0)
+    if (lane == 0) {
+        publish();
         final = atomicAdd(&a.arrived[static_cast<long long>(first) * a.slices + slice], 1u) == static_cast<unsigned>(last - first);
-    if (!__shfl_sync(0xffffffffu, final, 0)) return;
-    publish();
+        publish();
+    }
+    final = __shfl_sync(0xffffffffu, final, 0);
+    __syncwarp();
+    if (!final) return;
     float total[8];
     {
         const float* const p = at(first, 1);

@@ -57,3 +57,21 @@ def test_every_group_of_a_warp_is_added(env, tokens, cols, gap, kind, rows, ydt,
             want.index_add_(0, ids[ok].long(), 2.0 * dy[ok, part].double())
             assert float(want.abs().max()) < 2 ** 24
             assert torch.equal(grad[:, part], want.to(grad.dtype))
+
+
+def test_runs_across_many_blocks_are_joined_alike_every_time(env):
+    """Three rows that share all blocks, many times over: the block that arrives last always finds
+    the others' parts."""
+    torch, binding = env
+    tokens, rows, cols = 40_000, 3, 4096
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    ids = torch.randint(0, rows, (tokens,), generator=gen, device="cuda")
+    grad = torch.empty(rows, cols, device="cuda")
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for k in range(10):
+        dy = torch.randint(-3, 4, (tokens, cols), generator=gen, device="cuda", dtype=torch.int8)
+        want = torch.stack([dy[ids == v].sum(0) for v in range(rows)]).float()
+        dy = dy.bfloat16()
+        for _ in range(30):
+            wrong += (binding.embed_backward(dy, ids, grad) != want).sum()
+    assert int(wrong) == 0
