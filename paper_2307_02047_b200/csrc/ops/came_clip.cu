@@ -258,7 +258,9 @@ k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles
             }
         }
         if (d.ntiles > 1) {                              // (a tensor of one tile is finished)
-            if (!__shfl_sync(0xffffffffu, last, 0)) return;
+            last = __shfl_sync(0xffffffffu, last, 0);
+            __syncwarp();                                // lane 0's fence holds for the warp's reads (a shuffle orders no memory)
+            if (!last) return;
             s = warp_sum_of(w.tile_sum + d.tile0, d.ntiles, lane);
         }
         if (lane == 0) {
@@ -269,7 +271,9 @@ k_clip_norm(const ClipTensor* __restrict__ T, const ClipTile* __restrict__ tiles
             last = atomicAdd(&w.arrived[n], 1u) == static_cast<unsigned>(n - 1);
             publish();
         }
-        if (!__shfl_sync(0xffffffffu, last, 0)) return;
+        last = __shfl_sync(0xffffffffu, last, 0);
+        __syncwarp();
+        if (!last) return;
         s = warp_sum_of(w.tensor_sum, n, lane);
         if (lane == 0) {
             w.arrived[n] = 0u;

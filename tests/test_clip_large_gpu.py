@@ -117,3 +117,21 @@ def test_every_element_counts_once(env, case):
     assert each.tolist() == torch.tensor(counts, dtype=torch.float64).sqrt().float().tolist()
     assert float(total) == float(torch.tensor(float(sum(counts)), dtype=torch.float64).sqrt().float())
     assert float(coef) == 1
+
+
+def test_sums_of_many_tiles_and_tensors_are_finished_alike_every_time(env):
+    """Whole numbers, so sums are exact: the tile and the tensor that arrive last always find the others'."""
+    torch, binding = env
+    sizes = [3_000_001, 17, 1_000_000] * 40  # two stages: above 64 tensors
+    flat = torch.empty(sum(sizes), device="cuda")
+    grads = list(flat.split(sizes))
+    clip = binding.GradClip(grads)
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for k in range(10):
+        flat.copy_(torch.randint(-2, 3, flat.shape, device="cuda", dtype=torch.int8))
+        want = torch.stack([(g.double() ** 2).sum() for g in grads]).sqrt().float()
+        all_ = (flat.double() ** 2).sum().sqrt().float()
+        for _ in range(100):
+            total, _, each = clip.norm()
+            wrong += (each != want).sum() + (total != all_)
+    assert int(wrong) == 0
