@@ -606,12 +606,47 @@ def _embed_data(data, name, ids, cols, index):
     return ld if data.shape[0] > 1 else cols, code
 
 
+_lookup_class = None
+
+
+def _lookup_function():
+    """The lookup as an autograd function."""
+    global _lookup_class
+    if _lookup_class is None:
+        torch = _torch()
+
+        class Lookup(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, table, ids, scale, out_dtype):
+                ctx.save_for_backward(ids)
+                ctx.shape, ctx.dtype, ctx.scale = table.shape, table.dtype, scale
+                return embed_forward(table, ids, scale, out_dtype=out_dtype)      # (grad mode is off here)
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, grad_out):
+                (ids,) = ctx.saved_tensors
+                grad = grad_out.new_empty(ctx.shape, dtype=ctx.dtype)
+                return embed_backward(grad_out.contiguous(), ids, grad, ctx.scale), None, None, None
+
+        _lookup_class = Lookup
+    return _lookup_class
+
+
 def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
     """``out[t] = scale * table[ids[t]]``, zero where an id is not a row of the table.
 
     ``table``: fp32 or bf16 CUDA matrix with contiguous rows; ``ids``: contiguous int32 or int64
     CUDA tensor of any shape; ``out``: tensor of shape ``(*ids.shape, cols)``, fp32 or bf16, made
-    here when it is None (of type ``out_dtype``, the table's when that is None too)."""
+    here when it is None (of type ``out_dtype``, the table's when that is None too).
+
+    When autograd records and the table requires grad, the result carries the graph: the table's
+    gradient is ``embed_backward``'s, a whole matrix of its type (once differentiable).  ``out``
+    must be None then; ``embed_backward`` itself adds to a buffer of the caller's."""
+    if table.requires_grad and _torch().is_grad_enabled():
+        if out is not None:
+            raise CameError(CAME_ERR_UNSUPPORTED, "a table that requires grad takes no out: detach it, or disable grad mode")
+        return _lookup_function().apply(table, ids, scale, out_dtype)
     rows, cols, table_ld, table_code, index = _embed_table(table, "table")
     id_code = _embed_ids(ids, index)
     if out is None:
