@@ -591,7 +591,7 @@ def _embed_ids(ids, index) -> int:
 def _embed_data(data, name, ids, cols, index):
     """(row stride, dtype code) of the tokens' rows."""
     shape = data.shape
-    if shape[:-1] != ids.shape or shape[-1] != cols:
+    if not shape or shape[:-1] != ids.shape or shape[-1] != cols:
         raise CameError(CAME_ERR_SHAPE, f"{name} must have the shape of ids and the columns of the table")
     if data.get_device() != index:
         raise CameError(CAME_ERR_DEVICE, f"{name} must be on the table's GPU")
@@ -599,7 +599,10 @@ def _embed_data(data, name, ids, cols, index):
     if code is None:
         raise CameError(CAME_ERR_DTYPE, f"{name} must be fp32 or bf16, got {data.dtype}")
     if len(shape) != 2:
-        data = data.view(-1, cols)
+        try:
+            data = data.view(ids.numel(), cols)
+        except RuntimeError:
+            raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must lie at one stride") from None
     ld, one = data.stride()
     if one != 1 and cols > 1:
         raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must be contiguous")

@@ -1,4 +1,4 @@
-"""The lookup on a table that requires grad."""
+"""The lookup on a table that requires grad, and shapes that do not fit."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -50,3 +50,24 @@ def test_what_has_no_gradient_is_refused(env):
     (g,) = torch.autograd.grad(binding.embed_forward(table, ids).square().sum(), table, create_graph=True)
     with pytest.raises(RuntimeError):                    # once differentiable
         g.sum().backward()
+
+
+def test_shapes_that_do_not_fit_are_refused_as_errors_of_the_library(env):
+    torch, binding = env
+    t, ids = torch.ones(10, 8, device="cuda"), torch.zeros(4, 3, device="cuda", dtype=torch.int64)
+    crossed = torch.ones(3, 4, 8, device="cuda").transpose(0, 1)         # rows at two strides
+
+    def refused(status, call):
+        with pytest.raises(binding.CameError) as e:
+            call()
+        assert e.value.status == status
+
+    refused(binding.CAME_ERR_UNSUPPORTED, lambda: binding.embed_forward(t, ids, out=crossed))
+    refused(binding.CAME_ERR_UNSUPPORTED, lambda: binding.embed_backward(crossed, ids, t))
+    one = torch.ones((), device="cuda")
+    refused(binding.CAME_ERR_SHAPE, lambda: binding.embed_forward(t, ids[0, 0], out=one))
+    refused(binding.CAME_ERR_SHAPE, lambda: binding.embed_backward(one, ids[0, 0], t))
+    refused(binding.CAME_ERR_SHAPE, lambda: binding.embed_backward(torch.ones(4, 3, 0, device="cuda"), ids, torch.ones(10, 0, device="cuda")))
+    none = torch.ones(0, 3, 8, device="cuda")            # no tokens: any strides
+    assert bool((binding.embed_backward(none, ids[:0], t.clone()) == 0).all())
+    assert bool((t == 1).all())
