@@ -409,7 +409,7 @@ typedef struct {
     int64_t     tokens;       /* 0 (data and ids may then be NULL) .. 2^31 - 1               */
     int64_t     table_ld, data_ld;      /* elements from row to row, cols .. 2^29            */
     int64_t     padding_row;  /* used with CAME_EMBED_PADDING_ROW                            */
-    double      scale;        /* finite                                                      */
+    double      scale;        /* taken as fp32: finite there, and 0 only if it is 0          */
     int32_t     table_dtype, data_dtype;   /* came_dtype                                     */
     int32_t     id_dtype;     /* came_id_dtype                                               */
     uint32_t    flags;        /* CAME_EMBED_*; forward: 0                                    */

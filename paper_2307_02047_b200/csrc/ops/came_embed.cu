@@ -15,7 +15,6 @@
 #include <cooperative_groups.h>
 
 #include <algorithm>
-#include <cmath>
 
 namespace cg = cooperative_groups;
 
@@ -916,7 +915,7 @@ came_status validate_embed(const came_embed* e, bool backward)
     if (e->flags & ~static_cast<uint32_t>(CAME_EMBED_ACCUMULATE | CAME_EMBED_PADDING_ROW))
         return report(CAME_ERR_UNSUPPORTED, "unknown flag");
     if (e->reserved != 0) return report(CAME_ERR_SHAPE, "reserved must be 0");
-    if (!std::isfinite(e->scale)) return report(CAME_ERR_HPARAM, "scale must be finite");
+    if (!holds_in_fp32(e->scale)) return report(CAME_ERR_HPARAM, "scale must be finite, and not vanish, in fp32");
     if (!e->table || (e->tokens && (!e->data || !e->ids))) return report(CAME_ERR_NULL, "table, data and ids are required");
     if (!aligned_to(e->table, dtype_bytes(e->table_dtype)) || !aligned_to(e->data, dtype_bytes(e->data_dtype)) ||
         !aligned_to(e->ids, e->id_dtype == CAME_I64 ? 8 : 4))

@@ -8,6 +8,8 @@
 #include <stdint.h>
 
 #include <atomic>
+#include <cfloat>
+#include <cmath>
 
 namespace came_ops {
 
@@ -19,6 +21,8 @@ came_status require_current_device(int32_t device);
 
 inline bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 inline size_t dtype_bytes(int32_t dt) { return dt == CAME_BF16 ? 2 : 4; }
+// A factor that kernels take as fp32: neither infinite there nor, unless it is zero, zero.  (No NaN passes.)
+inline bool holds_in_fp32(double x) { return x == 0.0 || (std::fabs(x) <= FLT_MAX && std::fabs(x) >= FLT_TRUE_MIN); }
 inline bool known_dtype(int32_t dt) { return dt == CAME_F32 || dt == CAME_BF16; }
 
 // Lets `kernel` use `bytes` of dynamic shared memory; the runtime is asked once per device.

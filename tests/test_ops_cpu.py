@@ -91,3 +91,17 @@ def test_embed_without_gpu_reports_device_error():
         with pytest.raises(binding.CameError) as e:
             call(_embed())
         assert e.value.status == 7
+
+
+@pytest.mark.parametrize("scale", [1e39, -3.5e38, 1.7976931348623157e308, 1e-46, -1e-300, float("inf")])
+def test_a_scale_that_fp32_does_not_hold_is_refused(scale):
+    """The kernels multiply by the fp32 value: infinity would make NaN of zeros, and zero would drop the data."""
+    for call in (binding.came_embed_workspace, lambda e: binding.came_embed_forward(e), lambda e: binding.came_embed_backward(e, 0x40000, 1 << 20)):
+        with pytest.raises(binding.CameError) as e:
+            call(_embed(scale=scale))
+        assert e.value.status == binding.CAME_ERR_HPARAM
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-40, -1.5e-45, 3.4028234663852886e38, -3.4e38])
+def test_a_scale_that_fp32_holds_is_taken(scale):
+    assert binding.came_embed_workspace(_embed(scale=scale)) > 0
