@@ -356,7 +356,8 @@ typedef struct {
 typedef struct {
     double max_norm;          /* > 0; infinity = never clip       */
     double eps;               /* >= 0, finite                     */
-    double grad_scale;        /* s > 0, as in came_hparams; 0 = 1 */
+    double grad_scale;        /* s > 0, as in came_hparams; 0 = 1; came_clip_grads takes it as fp32,
+                                 where it must be finite and not 0 */
 } came_clip_params;
 
 /* Plans the tiles and allocates the context's tables and workspace; `t`: HOST array of n

@@ -570,6 +570,8 @@ came_status run_clip(came_clip_ctx* c, const came_clip_params* p, const void* co
     if (!aligned_to(results, 4)) return report(CAME_ERR_ALIGN, "results not 4-byte aligned");
     came_status s = validate_clip_params(*p);
     if (s != CAME_OK) return s;
+    if (apply && !holds_in_fp32(p->grad_scale))
+        return report(CAME_ERR_HPARAM, "grad_scale must be finite, and not vanish, in fp32 where outputs are written");
     if (apply && !c->has_out) return report(CAME_ERR_UNSUPPORTED, "the context was created without outputs");
     if ((s = require_current_device(c->device)) != CAME_OK) return s;
     if (grads && (s = rebind(c, grads, stream)) != CAME_OK) return s;
