@@ -334,7 +334,9 @@ came_status came_factor_update_static_plan(const void* grad, int32_t grad_dtype,
  *   n_i  = s sqrt(sum_j g_ij^2)            N = sqrt(sum_i n_i^2)
  *   coef = 1                               if N + eps <= max_norm
  *        = max_norm / (N + eps)            otherwise
- *   out_ij = g_ij * (s * coef)             rounded once, to nearest even (came_clip_grads only)
+ *   out_ij = rn(fl(g_ij * fl(fl(s) * coef)))      (came_clip_grads only)
+ * where coef is the fp32 value in `results`, fl rounds to fp32 and rn to the output's type, both to
+ * nearest even.
  * Squares are added in fp32 for up to 32 terms (and one of a tensor's ends) and in double from there
  * on, in a fixed order: results are bit-reproducible.  A finite N is found even where squares overflow
  * fp32; gradients below 1e-19 in magnitude may count as zero.  Inf or NaN in a gradient gives
@@ -386,15 +388,19 @@ came_status came_clip_destroy(came_clip_ctx* ctx);
 
 /* ---- Embedding lookup and its gradient -------------------------------------------------------
  *
- * Forward:   out[t, :] = rn(scale * W[id_t, :]) for 0 <= id_t < rows, and 0 for any other id
+ * Forward:   out[t, :] = rn(fl(scale * W[id_t, :])) for 0 <= id_t < rows, and 0 for any other id
  *            (masked or padding tokens are often -1).
- * Backward:  dW[v, :] = rn(scale * sum over the tokens t with id_t = v of dY[t, :]), every row
- *            written (rows without tokens with 0); with CAME_EMBED_ACCUMULATE
- *            dW[v, :] = rn(dW[v, :] + scale * sum ...), rows without tokens untouched.
- * The sums and their products with the scale are fp32, a row's tokens are added in an order fixed
- * by the ids alone, and what is stored is rounded to its type once: results are bit-reproducible.  Lengths from zero tokens and one column up; rows
- * may have any stride >= cols and any element-aligned address (aligned ones are faster).  The
- * output shares no memory with an input (CAME_ERR_OVERLAP). */
+ * Backward:  dW[v, :] = rn(fl(scale * S_v)), S_v = sum over the tokens t with id_t = v of dY[t, :], every
+ *            row written (rows without tokens with 0); with CAME_EMBED_ACCUMULATE
+ *            dW[v, :] = rn(fl(dW[v, :] + scale * S_v)), the product rounded to fp32 first where dW
+ *            is fp32; rows without tokens untouched.
+ * scale is its fp32 value, fl rounds to fp32 and rn to the stored type, both to nearest even.  S_v is
+ * added in fp32 in an order fixed by the ids alone: results are bit-reproducible.  Adding to an fp32 dW
+ * takes subnormal old values, addends and results as zero (the memory's own addition does); nothing else
+ * does.  Lengths from zero tokens and one column up; rows may have any stride >= cols and
+ * any element-aligned address (aligned ones are faster).  The output shares no memory with an
+ * input (CAME_ERR_OVERLAP); for this the ranges from a buffer's first to its last element count, so
+ * interleaved columns of one buffer are refused too. */
 typedef enum { CAME_I32 = 0, CAME_I64 = 1 } came_id_dtype;
 
 enum {

@@ -2,7 +2,7 @@
 //
 //   n_i  = |s| sqrt(sum_j g_ij^2),   N = sqrt(sum_i n_i^2)
 //   coef = 1 if N + eps <= max_norm, else max_norm / (N + eps)
-//   out_ij = rn(g_ij * (s * coef))
+//   out_ij = rn(fl(g_ij * fl(fl(s) * coef)))      fl: rounded to fp32, rn: to the output's type
 //
 // One grid reads every gradient once: a block per tile of one tensor, the tile's sum of squares
 // in fp32 for up to 32 terms and in double from there on.  The sums are finished

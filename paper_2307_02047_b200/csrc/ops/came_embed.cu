@@ -1,7 +1,9 @@
 // Embedding lookup with scaling, and its gradient by sorted tokens.
 //
-//   forward    out[t, :] = rn(scale * W[id_t, :])            0 where id_t is not in [0, rows)
-//   backward   dW[v, :] (+)= rn(scale * sum over t with id_t = v of dY[t, :])
+//   forward    out[t, :] = rn(fl(scale * W[id_t, :]))        0 where id_t is not in [0, rows)
+//   backward   dW[v, :] = rn(fl([dW[v, :] +] scale * sum over t with id_t = v of dY[t, :]))
+//
+// fl rounds to fp32, rn to the stored type.
 //
 // The backward pass sorts the tokens by id (stable, so a row's tokens keep their order), then
 // adds each row's tokens in an order fixed by the ids alone, in fp32.  No element is the target of
@@ -519,7 +521,8 @@ __device__ __forceinline__ void store_row(const SumArgs& a, O* grad, unsigned ro
         if (a.accumulate) {
             if constexpr (sizeof(O) == 4) {
                 // The only addition to these elements in the whole call, so its order cannot matter;
-                // done in the L2, it keeps the warp from waiting for the old value.
+                // done in the L2, it keeps the warp from waiting for the old value.  (That addition takes
+                // subnormal inputs and results as zero.)
                 reduce_ev<EV>(dst + c, y);
                 continue;
             } else {

@@ -35,3 +35,22 @@ def test_gradient_equals_differences_exactly(env, tokens, rows, cols):
         # the same sum from the formula, and what any one token gives to it
         each = scale * (c[ok].double() * E[ids[ok]].double()).sum(1)
         assert left == float(each.sum()) and float(each.min()) > 0
+
+
+@pytest.mark.parametrize("cols", [1, 2, 4, 8, 72])
+def test_subnormal_values_when_adding(env, cols):
+    """Adding in fp32 takes subnormal old values, addends and results as zero (each below 2^-126): three of
+    those at most, so the result is within 3 * 2^-126; what is overwritten, or bf16, keeps them.  Rows without
+    tokens are not touched at all."""
+    torch, binding = env
+    values = [0.0, 1e-40, -1e-39, 1.1e-38, -1.2e-38, 1.5e-38, -1.4e-38, 1e-30]
+    pairs = [(a, b) for a in values for b in values]
+    old, new = (torch.tensor([p[k] for p in pairs] + [1e-40], device="cuda")[:, None].expand(-1, cols).contiguous() for k in (0, 1))
+    ids = torch.arange(len(pairs), device="cuda")
+    got = binding.embed_backward(new[:-1], ids, old.clone(), accumulate=True)
+    assert float((got.double() - old.double() - new.double())[:-1].abs().max()) <= 3 * 2.0 ** -126
+    assert torch.equal(got[-1], old[-1])
+    assert torch.equal(binding.embed_backward(new[:-1], ids, old.clone())[:-1], new[:-1])
+    narrow = old.bfloat16()
+    got = binding.embed_backward(new[:-1], ids, narrow.clone(), accumulate=True)
+    assert torch.equal(got[:-1], (narrow.float() + new).bfloat16()[:-1]) and torch.equal(got[-1], narrow[-1])
