@@ -183,7 +183,9 @@ came_status came_create(came_ctx** out, const came_tensor* t, int32_t n, int32_t
  * the replacement must be 32-byte aligned too (came_required_grad_alignment);
  * everywhere else 16 bytes.  A pointer that is not gives CAME_ERR_ALIGN and
  * nothing is launched.  `cuda_stream`: the caller's cudaStream_t (NULL = default
- * stream).  Asynchronous; allocates nothing. */
+ * stream).  Asynchronous; allocates nothing.  Do not replace gradients in a call that
+ * is captured: the context takes them as replaced at once, the device only when
+ * the graph runs. */
 came_status came_step(came_ctx* ctx, const came_hparams* hp, const void* const* grads,
                       void* cuda_stream);
 

@@ -451,10 +451,11 @@ def _dtype_code(x, name) -> int:
 
 
 class GradClip:
-    """The global norm of a list of gradients, and clipping by it.
+    """The global norm of a list of gradients, and clipping by it.  To be made once for a list and
+    kept: creation plans the tiles, allocates, and waits for a copy.
 
     ``grads``: contiguous fp32 or bf16 CUDA tensors of any shape, read by every call (their
-    storage may be refilled).  ``outs``: where ``clip`` writes, tensors of the same sizes (``grads``
+    storage may be refilled; tensors with new memory are handed to a call).  ``outs``: where ``clip`` writes, tensors of the same sizes (``grads``
     itself clips in place), fp32 or bf16; None: norm only.  After a call ``total_norm``, ``coef``
     (CUDA scalars) and ``tensor_norms`` (one per tensor) hold its results, until the next call.
     """

@@ -10,7 +10,7 @@
 // tensor adds the tensors', both in a fixed order, so results do not depend on timing.
 //
 // Bound by the bytes: 13.5 GB of bf16 in 1812 us (7.4 TB/s, 1.14 of the measured copy rate, which also
-// writes), 436 MB of fp32 in 70.4 us (6.2 TB/s); a set of 0.5 MB takes 4.5 us on the device, a
+// writes), 436 MB of fp32 in 71 us (6.1 TB/s); a set of 0.5 MB takes 4.5 us on the device, a
 // chain of dependent round trips.  Writing clipped copies reads a set larger than the L2 twice: 709 MB
 // bf16 to bf16 in 337 us, 6.0 TB/s of the 2.03 GB that move.
 #include "came_ops.cuh"
