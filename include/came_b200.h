@@ -435,6 +435,83 @@ came_status came_embed_workspace(const came_embed* e, int64_t* out_bytes);
 came_status came_embed_backward(const came_embed* e, void* workspace, int64_t workspace_bytes,
                                 int32_t device, void* cuda_stream);
 
+/* ---- AdamW over many tensors, states in 32 or 8 bits -------------------------------------------
+ *
+ * For every tensor, with fp32 parameters p and states m, v (fl: rounded to fp32, in this order):
+ *   g = fl(grad * fl(fl(s) * device_scale))
+ *   m = fl(fl(beta1 m) + fl((1-beta1) g))         v = fl(fl(beta2 v) + fl((1-beta2) fl(g g)))
+ *   p = p - (lr wd p + lr m / (1-beta1^t) / (sqrt(v / (1-beta2^t)) + eps))
+ * beta, 1-beta are rounded to fp32 once (1-beta formed in double).  The update uses m and v as they are
+ * here, whatever they are stored in; the root and the quotient are approximations good to 2^-22 each.
+ * A root, or a sum of root and eps, below 2^-126 counts as zero: with eps = 0 that divides by zero.
+ *
+ * States of 8 bits (state_bits = 8): every 256 consecutive elements of a tensor (the last block may be
+ * shorter) share one byte e_m and one byte e_v, and
+ *   m = sign/4-bit exponent/3-bit fraction ("e4m3") * 2^(e_m - 127)
+ *   v = 5-bit exponent/2-bit fraction ("e5m2") * 2^(e_v - 127)
+ * With E the biased fp32 exponent of the block's largest finite |m| (v), e_m = max(E - 7, 0) and
+ * e_v = max(E - 14, 0).  A value between two neighbouring codes is stored as one of them at random, the
+ * upper with the probability (to 2^-16, centred) of how far it lies between them, so that the mean over many
+ * steps is the exact moving average: to the nearest, v would never leave a code with beta2 = 0.999, whose
+ * steps are a hundredth of the codes' spacing.  A v that is not zero is never stored as zero.  An
+ * infinite or NaN value is stored as NaN (v: infinity as infinity) and leaves its block's scale alone.
+ * The random bits are a hash of (seed, t, tensor and element): the same call gives the same bits.
+ * All in 32-bit wrapping arithmetic, with
+ *   mix(x): x ^= x >> 16; x *= 0xBB67AE85; x ^= x >> 15; x *= 0xA54FF53B; x ^= x >> 16
+ *   k = 0;  k = mix((k ^ w) + 0x3C6EF373) for w = low, high word of seed, low, high word of t
+ *   b = number of the block, counted through the whole list of tensors (each has ceil(numel / 256))
+ *   r = mix(mix(k + b * 0x9E3779B9) + (element in the block) * 0x9E3779B9)
+ * m takes the low 16 bits of r, v the high ones.
+ *
+ * Buffers may have any length (0 included) and any element-aligned address (rows of 256 elements that start
+ * 32-byte aligned are faster); they are contiguous and, but for gradients, share no memory
+ * (CAME_ERR_OVERLAP). */
+typedef struct came_adamw_ctx came_adamw_ctx;   /* opaque */
+
+typedef struct {
+    float*      param;        /* DEVICE fp32 [numel], updated in place                          */
+    const void* grad;         /* DEVICE grad_dtype [numel], read only                           */
+    void*       m;            /* DEVICE [numel] fp32, or bytes with state_bits 8                 */
+    void*       v;            /* DEVICE [numel] likewise                                         */
+    uint8_t*    m_scale;      /* DEVICE [ceil(numel / 256)] bytes e_m; state_bits 32: ignored    */
+    uint8_t*    v_scale;      /* DEVICE [ceil(numel / 256)] bytes e_v                            */
+    void*       param_bf16;   /* DEVICE bf16 [numel] or NULL: receives the updated parameters, to nearest even */
+    int64_t     numel;        /* 0 (all pointers may then be NULL); all tensors together 2^39                      */
+    int32_t     grad_dtype;   /* came_dtype                                                      */
+    int32_t     state_bits;   /* 32 or 8                                                         */
+    uint32_t    flags;        /* CAME_T_NO_WEIGHT_DECAY or 0                                     */
+    uint32_t    reserved;     /* must be 0                                                       */
+} came_adamw_tensor;
+
+typedef struct {
+    double   lr;              /* >= 0                                                            */
+    double   beta1, beta2;    /* in [0, 1)                                                       */
+    double   eps;             /* >= 0                                                            */
+    double   weight_decay;    /* >= 0                                                            */
+    double   grad_scale;      /* s > 0, as in came_hparams, taken as fp32; 0 = 1                 */
+    int64_t  step;            /* t >= 1                                                          */
+    uint64_t seed;            /* of the random bits of 8-bit states                              */
+} came_adamw_hparams;
+
+/* Plans the tiles and allocates the context's tables; `t`: HOST array of n descriptors; `device` must be
+ * current.  Zero-fills the states unless flags has CAME_CREATE_KEEP_STATE.  Synchronises the
+ * device's default stream once.  Errors of these functions are reported through came_last_error(NULL). */
+came_status came_adamw_create(came_adamw_ctx** out, const came_adamw_tensor* t, int32_t n, int32_t device,
+                              uint32_t flags);
+
+/* One step.  `grads`: HOST array of n DEVICE pointers that this call reads in place of the ones given at
+ * create, or NULL; they travel with the launch, so a captured call keeps the ones that it was given (they must
+ * not share memory with what the step writes: not checked).  `device_scale`: as in came_step_scaled, or
+ * NULL.  `device_step` (DEVICE int64 [1], 8-byte aligned, or NULL): t is read from there by the step's kernels
+ * and hp->step is ignored, so that a captured step goes on counting when the graph's caller adds one to it before
+ * each replay; a value below 1 there counts as 1.  Asynchronous on `cuda_stream`; allocates nothing.  One context
+ * serves one stream at a time. */
+came_status came_adamw_step(came_adamw_ctx* ctx, const came_adamw_hparams* hp, const void* const* grads,
+                            const float* device_scale, const int64_t* device_step, void* cuda_stream);
+
+/* Frees the context; the caller has synchronised the streams it used. */
+came_status came_adamw_destroy(came_adamw_ctx* ctx);
+
 /* Process-wide tuning knobs, read by later came_create calls (each knob is an atomic, so any
  * thread may set one; a context takes the values in force while it is being created, so set
  * them before the contexts they are meant for).  CAME_TUNE_TILE_ELEMS:

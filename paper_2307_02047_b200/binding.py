@@ -53,7 +53,8 @@ EXPORTED = ["came_create", "came_step", "came_step_host", "came_destroy", "came_
             "came_device_status", "came_lr_warmup", "came_clear_device_error",
             "came_selftest_wait_timeout", "came_debug_bounds", "came_step_scaled",
             "came_clip_create", "came_clip_norm", "came_clip_grads", "came_clip_destroy",
-            "came_embed_forward", "came_embed_workspace", "came_embed_backward"]
+            "came_embed_forward", "came_embed_workspace", "came_embed_backward",
+            "came_adamw_create", "came_adamw_step", "came_adamw_destroy"]
 
 
 class CameError(RuntimeError):
@@ -95,6 +96,19 @@ class came_embed(ctypes.Structure):
                 ("padding_row", ctypes.c_int64), ("scale", ctypes.c_double),
                 ("table_dtype", ctypes.c_int32), ("data_dtype", ctypes.c_int32),
                 ("id_dtype", ctypes.c_int32), ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class came_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("param_bf16", ctypes.c_void_p), ("numel", ctypes.c_int64), ("grad_dtype", ctypes.c_int32),
+                ("state_bits", ctypes.c_int32), ("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class came_adamw_hparams(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("grad_scale", ctypes.c_double),
+                ("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
 
 
 _lib = None
@@ -200,6 +214,12 @@ def _bind(L):
     L.came_embed_workspace.restype = i32
     L.came_embed_backward.argtypes = [ctypes.POINTER(came_embed), vp, i64, i32, vp]
     L.came_embed_backward.restype = i32
+    L.came_adamw_create.argtypes = [ctypes.POINTER(vp), ctypes.POINTER(came_adamw_tensor), i32, i32, u32]
+    L.came_adamw_create.restype = i32
+    L.came_adamw_step.argtypes = [vp, ctypes.POINTER(came_adamw_hparams), ctypes.POINTER(vp), vp, vp, vp]
+    L.came_adamw_step.restype = i32
+    L.came_adamw_destroy.argtypes = [vp]
+    L.came_adamw_destroy.restype = i32
     return L
 
 
@@ -395,6 +415,25 @@ def came_embed_backward(e: came_embed, workspace: int, workspace_bytes: int, dev
     status = (_lib or load()).came_embed_backward(e, workspace, workspace_bytes, device, stream)
     if status:
         _check(status)
+
+
+def came_adamw_create(tensors: Sequence[came_adamw_tensor], device: int = 0, flags: int = 0) -> ctypes.c_void_p:
+    ctx = ctypes.c_void_p()
+    arr = (came_adamw_tensor * len(tensors))(*tensors)
+    _check(load().came_adamw_create(ctypes.byref(ctx), arr, len(tensors), device, flags))
+    return ctx
+
+
+def came_adamw_step(ctx, hp: came_adamw_hparams, grads: Optional[Sequence[int]] = None, device_scale: int = 0,
+                    device_step: int = 0, stream: int = 0) -> None:
+    garr = None if grads is None else (ctypes.c_void_p * len(grads))(*grads)
+    status = (_lib or load()).came_adamw_step(ctx, hp, garr, device_scale, device_step, stream)
+    if status:
+        _check(status)
+
+
+def came_adamw_destroy(ctx) -> None:
+    _check(load().came_adamw_destroy(ctx))
 
 
 def make_hparams(step: int, **kw) -> came_hparams:
@@ -754,6 +793,149 @@ class CameOptimizer:
         if self.ctx is not None:
             self.torch.cuda.synchronize()
             came_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# --- AdamW ---------------------------------------------------------------------------------------
+
+CAME_ADAMW_BLOCK = 256      # consecutive elements that share a scale where states have 8 bits
+
+
+class AdamWOptimizer:
+    """AdamW over a list of torch CUDA parameter tensors: one launch steps them all (one for each type
+    of state and gradient in the list).
+
+    ``params``: fp32 CUDA tensors of any shape, contiguous, updated in place.  ``grads``: tensors of the same
+    shapes, fp32 or bf16, read by every step (their storage may be refilled; tensors with new memory are
+    handed to ``step``).  ``state_bits``: 32 (fp32 states) or 8, one for all or one per tensor.  With 8, ``m[i]``
+    is ``torch.float8_e4m3fn``, ``v[i]`` is ``torch.float8_e5m2``, both in the shape of the parameter, and each 256
+    consecutive elements share a power of two in ``m_scale[i]``, ``v_scale[i]`` (``torch.float8_e8m0fnu``):
+    the state's value is code times scale.  States are rounded up or down at random, with bits that
+    ``seed`` and the number of the step determine (see ``include/came_b200.h``).
+
+    ``m``, ``v``, ``m_scale``, ``v_scale``: lists of the states to go on with (None: new ones, zero);
+    ``step_count`` goes with them.  ``flags``: one per tensor, ``CAME_T_NO_WEIGHT_DECAY`` or 0.  ``bf16_copy``: True,
+    or the list of bf16 tensors that every step fills with the new parameters (``p_bf16``)."""
+
+    def __init__(self, params, grads, state_bits=32, flags: Optional[Sequence[int]] = None, bf16_copy=False,
+                 m=None, v=None, m_scale=None, v_scale=None, seed: int = 0, step_count: int = 0):
+        torch = _torch()
+        self.ctx = None
+        self.params, self.grads = list(params), list(grads)
+        n = len(self.params)
+        if not n or len(self.grads) != n:
+            raise CameError(CAME_ERR_SHAPE, "need at least one parameter, and as many grads")
+        self.state_bits = [state_bits] * n if isinstance(state_bits, int) else list(state_bits)
+        if not 0 <= seed < 1 << 64:
+            raise CameError(CAME_ERR_HPARAM, "seed must lie in [0, 2^64)")
+        given = {"state_bits": self.state_bits, "m": m, "v": v, "m_scale": m_scale, "v_scale": v_scale, "flags": flags,
+                 "bf16_copy": None if isinstance(bf16_copy, bool) or bf16_copy is None else bf16_copy}
+        for name, x in given.items():
+            if x is not None and len(x) != n:
+                raise CameError(CAME_ERR_SHAPE, f"{name} must be as many as params")
+        if (m is None) != (v is None):
+            raise CameError(CAME_ERR_NULL, "m and v belong together")
+        first = self.params[0]
+        _cuda_tensor(first, "params[0]")
+        self.device, self.seed, self.step_count = first.device, seed, step_count
+        self.m, self.v, self.m_scale, self.v_scale, self.p_bf16 = [], [], [], [], []
+        descs, self._codes = [], []
+        at = lambda x: 0 if x is None else x.data_ptr()  # noqa: E731
+        for i, (p, g, bits) in enumerate(zip(self.params, self.grads, self.state_bits)):
+            self._check_tensor(p, f"params[{i}]", (torch.float32,), p.numel())
+            self._codes.append(_dtype_code(g, f"grads[{i}]"))
+            self._check_tensor(g, f"grads[{i}]", None, p.numel())
+            if bits not in (32, 8):
+                raise CameError(CAME_ERR_DTYPE, f"state_bits of tensor {i} must be 32 or 8")
+            blocks = -(-p.numel() // CAME_ADAMW_BLOCK)
+            e8m0 = torch.float8_e8m0fnu
+            for name, mine, theirs, dtype, shape in (
+                    ("m", self.m, m, torch.float32 if bits == 32 else torch.float8_e4m3fn, p.shape),
+                    ("v", self.v, v, torch.float32 if bits == 32 else torch.float8_e5m2, p.shape),
+                    ("m_scale", self.m_scale, m_scale, e8m0 if bits == 8 else None, (blocks,)),
+                    ("v_scale", self.v_scale, v_scale, e8m0 if bits == 8 else None, (blocks,))):
+                if dtype is None:
+                    mine.append(None)
+                elif m is None:
+                    zeros = torch.zeros(shape, dtype=torch.float32 if dtype == torch.float32 else torch.uint8, device=self.device)
+                    mine.append(zeros if dtype == torch.float32 else zeros.view(dtype))
+                else:
+                    if theirs is None or theirs[i] is None:
+                        raise CameError(CAME_ERR_NULL, f"{name}[{i}] is required with 8-bit states")
+                    self._check_tensor(theirs[i], f"{name}[{i}]", (dtype,), p.numel() if len(shape) != 1 or name in "mv" else blocks)
+                    mine.append(theirs[i])
+            if given["bf16_copy"] is not None:
+                self._check_tensor(bf16_copy[i], f"bf16_copy[{i}]", (torch.bfloat16,), p.numel())
+                self.p_bf16.append(bf16_copy[i])
+            else:
+                self.p_bf16.append(torch.empty_like(p, dtype=torch.bfloat16, requires_grad=False) if bf16_copy else None)
+            descs.append(came_adamw_tensor(at(p), at(g), at(self.m[i]), at(self.v[i]), at(self.m_scale[i]), at(self.v_scale[i]),
+                                           at(self.p_bf16[i]), p.numel(), self._codes[i], bits, 0 if flags is None else int(flags[i]), 0))
+        self._hp = came_adamw_hparams()
+        with torch.cuda.device(self.device):
+            self.ctx = came_adamw_create(descs, self.device.index, CAME_CREATE_KEEP_STATE)
+
+    def _check_tensor(self, x, name, dtypes, numel) -> None:
+        if x.device != self.device:
+            raise CameError(CAME_ERR_DEVICE, f"{name} must be on {self.device}")
+        if dtypes is not None and x.dtype not in dtypes:
+            raise CameError(CAME_ERR_DTYPE, f"{name} must be {dtypes[0]}, got {x.dtype}")
+        if x.numel() != numel:
+            raise CameError(CAME_ERR_SHAPE, f"{name} must have {numel} elements")
+        if not x.is_contiguous():
+            raise CameError(CAME_ERR_UNSUPPORTED, f"{name} must be contiguous")
+
+    def step(self, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, weight_decay: float = 0.0,
+             grad_scale: float = 1.0, device_scale=None, device_step=None, grads=None) -> None:
+        """One step on the current stream.
+
+        ``device_scale``: an fp32 CUDA scalar that multiplies every gradient (``GradClip.coef``).  ``device_step``: an
+        int64 CUDA scalar that holds the number of the step, counted by the caller: for steps that are captured
+        into a graph (``step_count`` is not used then).  ``grads``: tensors that this call reads in place
+        of the ones given at creation."""
+        torch = _torch()
+        scale_at = step_at = 0
+        if device_scale is not None:
+            _cuda_tensor(device_scale, "device_scale", torch.float32, self.device)
+            if device_scale.numel() != 1:
+                raise CameError(CAME_ERR_SHAPE, "device_scale must hold one value")
+            scale_at = device_scale.data_ptr()
+        if device_step is not None:
+            _cuda_tensor(device_step, "device_step", torch.int64, self.device)
+            if device_step.numel() != 1:
+                raise CameError(CAME_ERR_SHAPE, "device_step must hold one value")
+            step_at = device_step.data_ptr()
+        moved = None
+        if grads is not None:
+            grads = list(grads)
+            if len(grads) != len(self.params):
+                raise CameError(CAME_ERR_SHAPE, "grads must be as many as params")
+            for i, (g, p) in enumerate(zip(grads, self.params)):
+                self._check_tensor(g, f"grads[{i}]", None, p.numel())
+                if _dtype_code(g, f"grads[{i}]") != self._codes[i]:
+                    raise CameError(CAME_ERR_DTYPE, f"grads[{i}] must keep its dtype")
+            moved = [g.data_ptr() for g in grads]
+        hp = self._hp
+        hp.lr, hp.beta1, hp.beta2, hp.eps, hp.weight_decay, hp.grad_scale = lr, beta1, beta2, eps, weight_decay, grad_scale
+        hp.step, hp.seed = self.step_count + 1, self.seed
+        _call_on(self.device.index, self._step_call, self.ctx, hp, moved, scale_at, step_at)
+        if device_step is None:
+            self.step_count += 1
+
+    @staticmethod
+    def _step_call(ctx, hp, grads, scale_at, step_at, index, stream):
+        came_adamw_step(ctx, hp, grads, scale_at, step_at, stream)
+
+    def close(self) -> None:
+        if self.ctx is not None:
+            _torch().cuda.synchronize(self.device)
+            came_adamw_destroy(self.ctx)
             self.ctx = None
 
     def __del__(self):

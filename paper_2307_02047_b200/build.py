@@ -5,9 +5,11 @@ import os
 import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(_HERE, "csrc", s) for s in ("came_api.cu", "ops/came_clip.cu", "ops/came_embed.cu")]
+SRCS = [os.path.join(_HERE, "csrc", s) for s in ("came_api.cu", "ops/came_clip.cu", "ops/came_embed.cu",
+                                                "ops/came_adamw.cu")]
 DEPS = SRCS + [os.path.join(_HERE, "csrc", h) for h in
-               ("came_kernels.cuh", "came_pipelined.cuh", "came_stream.cuh", "ops/came_ops.cuh")] + \
+               ("came_kernels.cuh", "came_pipelined.cuh", "came_stream.cuh", "ops/came_ops.cuh",
+                "ops/came_vec.cuh")] + \
        [os.path.join(os.path.dirname(_HERE), "include", "came_b200.h")]
 LIB = os.path.join(_HERE, "libcame_b200.so")
 LIB_DEBUG = os.path.join(_HERE, "libcame_b200_debug.so")     # -DCAME_DEBUG_BOUNDS (see the header)
