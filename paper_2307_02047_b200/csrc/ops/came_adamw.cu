@@ -6,6 +6,11 @@
 // A warp takes 256 consecutive elements of a tensor, eight per lane: the elements that share a scale
 // where states have 8 bits.  Nothing crosses from one such block to the next, so there is one pass, one
 // launch for each type of state and gradient in the list, and no order that could change a result.
+//
+// Bound by the bytes: 355 M elements with fp32 states and gradients move 9.9 GB; 256 M with 8-bit states, bf16
+// gradients and bf16 copies 4.1 GB in 626 us (6.5 TB/s, the measured copy rate).  The 8-bit form computes about 70
+// instructions for an element, three quarters of what the SMs can issue in that time, a third of them for the random bits
+// and the rounding; one hash serves both states.
 #include "came_vec.cuh"
 
 #include <cuda_fp16.h>
@@ -38,13 +43,13 @@ struct AdamwTensor {
     int            decay;
 };
 
-struct AdamwTile { int tensor; unsigned block; };       // blocks [block, block + per_tile) of a tensor
+struct AdamwTile { int tensor; unsigned block; };       // blocks of a tensor from `block` on, per_warp for each warp
 
 struct AdamwConsts {
     float b1, c1, b2, c2, eps, decay, scale;
     float step, root;                    // lr / (1 - b1^t), 1 / sqrt(1 - b2^t); not used with a step on the device
     unsigned key;
-    int per_tile;
+    unsigned per_warp;
     double lr, log_b1, log_b2;           // used with a step on the device
     unsigned key_seed;
     const float* device_scale;
@@ -76,47 +81,43 @@ __device__ __forceinline__ float power_of_two(int e) { return e > 0 ? __uint_as_
 // values included, so that adding a random number below the bits that are dropped and cutting these
 // off rounds up with the right probability.
 struct E4M3 {
-    static constexpr int kTop = 7, kDrop = 20;
-    static constexpr float kLow = 0x1p-120f;
-    static __device__ __forceinline__ unsigned random(unsigned r) { return ((r & 0xffffu) << 4) + 8u; }
-    static __device__ __forceinline__ void decode(uint32_t two, float& a, float& b)      // bytes 0 and 1
+    static constexpr bool kSigned = true;
+    static constexpr int kTop = 7, kDrop = 20, kLow = 120;
+    static __device__ __forceinline__ unsigned random(unsigned r) { return ((r << 4) & 0xffff0u) | 8u; }
+    template <int K> static __device__ __forceinline__ uint32_t halves(uint32_t w)       // bytes K and K + 1
     {
         uint32_t h;
-        asm("{ .reg .b16 t; cvt.u16.u32 t, %1; cvt.rn.f16x2.e4m3x2 %0, t; }" : "=r"(h) : "r"(two));
-        const __half2 x = *reinterpret_cast<const __half2*>(&h);
-        a = __low2float(x);
-        b = __high2float(x);
+        if constexpr (K == 0) asm("{ .reg .b16 l, u; mov.b32 {l, u}, %1; cvt.rn.f16x2.e4m3x2 %0, l; }" : "=r"(h) : "r"(w));
+        else asm("{ .reg .b16 l, u; mov.b32 {l, u}, %1; cvt.rn.f16x2.e4m3x2 %0, u; }" : "=r"(h) : "r"(w));
+        return h;
     }
 };
 struct E5M2 {
-    static constexpr int kTop = 14, kDrop = 21;
-    static constexpr float kLow = 0x1p-112f;
-    static __device__ __forceinline__ unsigned random(unsigned r) { return ((r >> 16) << 5) + 16u; }
-    static __device__ __forceinline__ void decode(uint32_t two, float& a, float& b)
+    static constexpr bool kSigned = false;
+    static constexpr int kTop = 14, kDrop = 21, kLow = 112;
+    static __device__ __forceinline__ unsigned random(unsigned r) { return ((r >> 11) & 0x1fffe0u) | 16u; }
+    template <int K> static __device__ __forceinline__ uint32_t halves(uint32_t w)       // an e5m2 is the upper byte of a half
     {
-        const uint32_t h = __byte_perm(two, 0, 0x1404);              // an e5m2 is the upper byte of a half
-        const __half2 x = *reinterpret_cast<const __half2*>(&h);
-        a = __low2float(x);
-        b = __high2float(x);
+        return __byte_perm(w, 0, K == 0 ? 0x1404 : 0x3424);
     }
 };
 
 template <typename F>
-__device__ __forceinline__ void decode8(const uint32_t (&w)[2], uint8_t e, float (&x)[8])
+__device__ __forceinline__ void decode8(const uint32_t (&w)[2], unsigned e, float (&x)[8])
 {
-    const float scale = power_of_two(e);
+    const float scale = power_of_two(static_cast<int>(e));
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
-        F::decode(w[k >> 2] >> (k & 2 ? 16 : 0), x[k], x[k + 1]);
-        x[k] *= scale;
-        x[k + 1] *= scale;
+        const uint32_t h = k & 2 ? F::template halves<2>(w[k >> 2]) : F::template halves<0>(w[k >> 2]);
+        const __half2 two = *reinterpret_cast<const __half2*>(&h);
+        x[k] = __low2float(two) * scale;
+        x[k + 1] = __high2float(two) * scale;
     }
 }
 
-// Codes of a block's values (x: this lane's eight), and the byte of its scale.  The order of a lane's elements does
-// not matter here: r are their random bits.
-template <typename F, bool kSigned>
-__device__ __forceinline__ uint8_t encode8(const float (&x)[8], const unsigned (&r)[8], uint32_t (&w)[2])
+// Codes of a block's values (x: this lane's eight; r: their random bits), and the byte of its scale.
+template <typename F>
+__device__ __forceinline__ unsigned encode8(const float (&x)[8], const unsigned (&r)[8], uint32_t (&w)[2])
 {
     float most = 0.f;
 #pragma unroll
@@ -130,22 +131,38 @@ __device__ __forceinline__ uint8_t encode8(const float (&x)[8], const unsigned (
         top = __reduce_max_sync(0xffffffffu, __float_as_uint(most));
     }
     const int e = max(static_cast<int>(top >> 23) - F::kTop, 0);
-    const float inverse = power_of_two(254 - e);
-    w[0] = w[1] = 0u;
+    // One factor scales and lowers the exponent: 2^(127 - e - kLow), also where it is subnormal.  Of blocks whose values are
+    // so large that it would vanish, a part of it is taken first (what that loses is far below every code).
+    int power = 254 - e - F::kLow;
+    float first = 1.f;
+    if (power < -22) {
+        first = 0x1p-64f;
+        power += 64;
+    }
+    const float factor = power_of_two(power);
+    uint32_t c[8];                                       // codes in the upper byte
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float y = __fmul_rn(__fmul_rn(fabsf(x[k]), inverse), F::kLow);
-        unsigned code = (__float_as_uint(y) + F::random(r[k])) >> F::kDrop;
-        if constexpr (kSigned) {
-            if (special && !(fabsf(x[k]) < INFINITY)) code = 0x7fu;
-            code |= (__float_as_uint(x[k]) >> 24) & 0x80u;
+        const float z = first == 1.f ? fabsf(x[k]) : fabsf(x[k]) * first;
+        unsigned s = __float_as_uint(z * factor) + F::random(r[k]);
+        if constexpr (F::kSigned) {
+            c[k] = ((s << (24 - F::kDrop)) & 0x7f000000u) | (__float_as_uint(x[k]) & 0x80ffffffu);
         } else {
-            code = max(code, min(__float_as_uint(x[k]), 1u));       // not zero: not stored as zero
-            if (special && !(x[k] < INFINITY)) code = x[k] == INFINITY ? 0x7cu : 0x7fu;
+            s = max(s, min(__float_as_uint(x[k]), 1u << F::kDrop));      // not zero: not stored as zero
+            c[k] = s << (24 - F::kDrop);
         }
-        w[k >> 2] |= code << (8 * (k & 3));
     }
-    return static_cast<uint8_t>(e);
+    if (special) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (fabsf(x[k]) < INFINITY) continue;
+            c[k] = !F::kSigned && x[k] == INFINITY ? 0x7c000000u : 0x7f000000u;
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; k += 4)
+        w[k >> 2] = __byte_perm(__byte_perm(c[k], c[k + 1], 0x73), __byte_perm(c[k + 2], c[k + 3], 0x73), 0x5410);
+    return static_cast<unsigned>(e);
 }
 
 // One element's new p, from its old p, its gradient and its states, which become the new ones.
@@ -161,58 +178,64 @@ struct Update {
     }
 };
 
-// 256 elements from `i0` on, `left` of them in the tensor.  kWide: all there, and 8 per lane lie side by side and
-// aligned; else lane l takes the elements l, l + 32, ... one by one.
-template <int BITS, typename G, bool kWide>
-__device__ __forceinline__ void adamw_block(const AdamwTensor& d, const G* grad, unsigned block, int left, const Update& f, unsigned key)
-{
+// A block as it is stored, eight elements per lane side by side: what a warp has in flight.
+template <int BITS, typename G>
+struct Stored {
     using S = typename std::conditional<BITS == 32, float, uint8_t>::type;
-    const int lane = threadIdx.x & 31;
-    const long long i0 = static_cast<long long>(block) * kBlock;
-    float p[8], g[8], m[8], v[8];
-    const int first = kWide ? 8 * lane : lane, next = kWide ? 1 : 32;
-    const long long at = i0 + first;
+    Vec<G, 8> g;
+    Vec<S, 8> m, v;
+    Vec<float, 8> p;
+    __device__ __forceinline__ void load(const AdamwTensor& d, const G* grad, unsigned block)
+    {
+        const long long at = static_cast<long long>(block) * kBlock + 8 * (threadIdx.x & 31);
+        g.load(grad + at);
+        m.load(static_cast<const S*>(d.m) + at);
+        v.load(static_cast<const S*>(d.v) + at);
+        p.load(d.p + at);
+    }
+};
+
+// Updates one block.  kWide: all 256 elements are there, aligned, and loaded; else lane l takes the elements
+// l, l + 32, ... of the `left` ones one by one.  `scales`: the bytes of m (low) and v, which become the new ones.
+template <int BITS, typename G, bool kWide>
+__device__ __forceinline__ void adamw_block(const AdamwTensor& d, const G* grad, const Stored<BITS, G>& in, unsigned block, int left,
+                                            const Update& f, unsigned key, unsigned& scales)
+{
+    using S = typename Stored<BITS, G>::S;
+    const int lane = threadIdx.x & 31, first = kWide ? 8 * lane : lane, next = kWide ? 1 : 32;
+    const long long at = static_cast<long long>(block) * kBlock + first;
     float* const pp = d.p + at;
     S* const pm = static_cast<S*>(d.m) + at;
     S* const pv = static_cast<S*>(d.v) + at;
-    Vec<float, 8> vp;
+    float p[8], g[8], m[8], v[8];
+    uint32_t wm[2] = {0u, 0u}, wv[2] = {0u, 0u};
     if constexpr (kWide) {
-        Vec<G, 8> vg;
-        Vec<S, 8> vm, vv;
-        uint8_t em = 0, ev = 0;
-        vg.load(grad + at);
-        vm.load(pm);
-        vv.load(pv);
-        vp.load(pp);
-        if constexpr (BITS == 8) em = d.ms[block], ev = d.vs[block];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) g[k] = vg.value(k), p[k] = vp.value(k);
+        for (int k = 0; k < 8; ++k) g[k] = in.g.value(k), p[k] = in.p.value(k);
         if constexpr (BITS == 32) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) m[k] = vm.value(k), v[k] = vv.value(k);
+            for (int k = 0; k < 8; ++k) m[k] = in.m.value(k), v[k] = in.v.value(k);
         } else {
-            decode8<E4M3>(vm.w, em, m);
-            decode8<E5M2>(vv.w, ev, v);
+            wm[0] = in.m.w[0], wm[1] = in.m.w[1], wv[0] = in.v.w[0], wv[1] = in.v.w[1];
         }
     } else {
-        uint32_t wm[2] = {0u, 0u}, wv[2] = {0u, 0u};
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const bool in = first + 32 * k < left;
-            p[k] = in ? pp[32 * k] : 0.f;
-            g[k] = in ? to_float(grad[at + 32 * k]) : 0.f;
+            const bool there = first + 32 * k < left;
+            p[k] = there ? pp[32 * k] : 0.f;
+            g[k] = there ? to_float(grad[at + 32 * k]) : 0.f;
             if constexpr (BITS == 32) {
-                m[k] = in ? pm[32 * k] : 0.f;
-                v[k] = in ? pv[32 * k] : 0.f;
-            } else if (in) {
+                m[k] = there ? pm[32 * k] : 0.f;
+                v[k] = there ? pv[32 * k] : 0.f;
+            } else if (there) {
                 wm[k >> 2] |= static_cast<uint32_t>(pm[32 * k]) << (8 * (k & 3));
                 wv[k >> 2] |= static_cast<uint32_t>(pv[32 * k]) << (8 * (k & 3));
             }
         }
-        if constexpr (BITS == 8) {
-            decode8<E4M3>(wm, d.ms[block], m);
-            decode8<E5M2>(wv, d.vs[block], v);
-        }
+    }
+    if constexpr (BITS == 8) {
+        decode8<E4M3>(wm, scales & 255u, m);
+        decode8<E5M2>(wv, scales >> 8, v);
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) p[k] = f(p[k], g[k], m[k], v[k]);
@@ -221,15 +244,13 @@ __device__ __forceinline__ void adamw_block(const AdamwTensor& d, const G* grad,
         const unsigned base = mix(key + (d.block0 + block) * kGolden) + static_cast<unsigned>(first) * kGolden;
 #pragma unroll
         for (int k = 0; k < 8; ++k) r[k] = mix(base + static_cast<unsigned>(k * next) * kGolden);
-        if constexpr (!kWide) {          // elements behind the end are zero and stay out of the scales
+        if constexpr (!kWide) {          // elements behind the end stay out of the scales
 #pragma unroll
             for (int k = 0; k < 8; ++k)
                 if (first + 32 * k >= left) m[k] = v[k] = 0.f;
         }
-        uint32_t wm[2], wv[2];
-        const uint8_t em = encode8<E4M3, true>(m, r, wm), ev = encode8<E5M2, false>(v, r, wv);
-        __syncwarp();                    // every lane has read the old scales
-        if (lane == 0) d.ms[block] = em, d.vs[block] = ev;
+        scales = encode8<E4M3>(m, r, wm);
+        scales |= encode8<E5M2>(v, r, wv) << 8;
         if constexpr (kWide) {
             *reinterpret_cast<uint2*>(pm) = make_uint2(wm[0], wm[1]);
             *reinterpret_cast<uint2*>(pv) = make_uint2(wv[0], wv[1]);
@@ -242,18 +263,20 @@ __device__ __forceinline__ void adamw_block(const AdamwTensor& d, const G* grad,
                 }
         }
     } else if constexpr (kWide) {
-        vp.set(m);
-        vp.store(pm);
-        vp.set(v);
-        vp.store(pv);
+        Vec<float, 8> x;
+        x.set(m);
+        x.store(pm);
+        x.set(v);
+        x.store(pv);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k)
             if (first + 32 * k < left) pm[32 * k] = m[k], pv[32 * k] = v[k];
     }
     if constexpr (kWide) {
-        vp.set(p);
-        vp.store(pp);
+        Vec<float, 8> x;
+        x.set(p);
+        x.store(pp);
         if (d.copy) {
             Vec<__nv_bfloat16, 8> c;
             c.set(p);
@@ -269,8 +292,10 @@ __device__ __forceinline__ void adamw_block(const AdamwTensor& d, const G* grad,
     }
 }
 
+// 8 bits: registers for three blocks per SM (256 M elements: 583 us, against 645 with two and 649 with four, whose
+// registers do not hold the block that is on its way).
 template <int BITS, typename G>
-__global__ void __launch_bounds__(kWarps * 32)
+__global__ void __launch_bounds__(kWarps * 32, BITS == 8 ? 3 : 1)
 k_adamw(const AdamwTensor* __restrict__ table, const void* const* __restrict__ grads, const AdamwTile* __restrict__ tiles,
         const __grid_constant__ AdamwConsts c)
 {
@@ -294,15 +319,47 @@ k_adamw(const AdamwTensor* __restrict__ table, const void* const* __restrict__ g
         f.root = s_root;
         key = s_key;
     }
+    // The block's warps take turns: neighbouring blocks at the same time (64 M elements: 181 us, against 198 with
+    // each warp's blocks side by side).
+    const int lane = threadIdx.x & 31;
     const unsigned blocks = static_cast<unsigned>((d.n + kBlock - 1) / kBlock);
-    const unsigned end = min(blocks, tile.block + static_cast<unsigned>(c.per_tile));
-    const uintptr_t states = reinterpret_cast<uintptr_t>(d.m) | reinterpret_cast<uintptr_t>(d.v);
+    const unsigned begin = tile.block + (threadIdx.x >> 5), end = min(blocks, tile.block + kWarps * c.per_warp);
     const bool aligned = ((reinterpret_cast<uintptr_t>(d.p) & 31) | (reinterpret_cast<uintptr_t>(grad) & (8 * sizeof(G) - 1)) |
-                          (states & (BITS == 32 ? 31 : 7)) | (reinterpret_cast<uintptr_t>(d.copy) & 15)) == 0;
-    for (unsigned b = tile.block + (threadIdx.x >> 5); b < end; b += kWarps) {
-        const long long left = d.n - static_cast<long long>(b) * kBlock;
-        if (aligned && left >= kBlock) adamw_block<BITS, G, true>(d, grad, b, kBlock, f, key);
-        else adamw_block<BITS, G, false>(d, grad, b, static_cast<int>(min(left, static_cast<long long>(kBlock))), f, key);
+                          ((reinterpret_cast<uintptr_t>(d.m) | reinterpret_cast<uintptr_t>(d.v)) & (BITS == 32 ? 31 : 7)) |
+                          (reinterpret_cast<uintptr_t>(d.copy) & 15)) == 0;
+    const unsigned wide = aligned ? min(end, static_cast<unsigned>(d.n / kBlock)) : 0u;          // the last block may be short
+    // The scales of the warp's blocks are read at the start and written at the end, lane j those of its block j: a load
+    // from a sector to which neighbours have just written takes the time of several others (64 M elements: 374 us block
+    // by block, 181 with the loads at the start).
+    const unsigned mine = begin + lane * kWarps;
+    unsigned scales = 0;
+    if (BITS == 8 && mine < end) scales = d.ms[mine] | d.vs[mine] << 8;
+    Stored<BITS, G> now, ahead;
+    unsigned b = begin;
+    auto turn = [&](auto is_wide) {
+        const unsigned j = (b - begin) / kWarps;
+        unsigned e = BITS == 8 ? __shfl_sync(0xffffffffu, scales, j) : 0u;
+        const int left = static_cast<int>(min(d.n - static_cast<long long>(b) * kBlock, static_cast<long long>(kBlock)));
+        adamw_block<BITS, G, decltype(is_wide)::value>(d, grad, now, b, left, f, key, e);
+        if (lane == j) scales = e;
+    };
+    // 8 bits: the next block is on its way while this one is computed (256 M elements: 642 us, 738 without); fp32 states
+    // compute so little that it only costs registers (64 M: 276 and 273 us).
+    constexpr bool kAhead = BITS == 8;
+    if (kAhead && b < wide) ahead.load(d, grad, b);
+    for (; b < wide; b += kWarps) {
+        if constexpr (kAhead) {
+            now = ahead;
+            if (b + kWarps < wide) ahead.load(d, grad, b + kWarps);
+        } else {
+            now.load(d, grad, b);
+        }
+        turn(std::true_type{});
+    }
+    for (; b < end; b += kWarps) turn(std::false_type{});
+    if (BITS == 8 && mine < end) {
+        d.ms[mine] = static_cast<uint8_t>(scales);
+        d.vs[mine] = static_cast<uint8_t>(scales >> 8);
     }
 }
 
@@ -317,7 +374,8 @@ __global__ void k_adamw_pointers(const __grid_constant__ MovedPointers from, con
 }  // namespace
 
 struct came_adamw_ctx {
-    int device = 0, n = 0, per_tile = 0;
+    int device = 0, n = 0;
+    unsigned per_warp[2] = {1, 1};       // blocks of a tile for each warp: fp32, 8-bit states
     int first[5] = {0, 0, 0, 0, 0};      // where the tiles of each (state, gradient) type begin
     std::vector<int64_t> numel;
     std::vector<int>     grad_bytes;
@@ -402,8 +460,9 @@ came_status validate_hparams(const came_adamw_hparams& h, bool device_step)
 }
 
 template <int BITS, typename G>
-cudaError_t launch(const came_adamw_ctx* c, int kind, const void* const* grads, const AdamwConsts& k, cudaStream_t stream)
+cudaError_t launch(const came_adamw_ctx* c, int kind, const void* const* grads, AdamwConsts k, cudaStream_t stream)
 {
+    k.per_warp = c->per_warp[BITS == 8];
     const int tiles = c->first[kind + 1] - c->first[kind];
     if (!tiles) return cudaSuccess;
     k_adamw<BITS, G><<<tiles, kWarps * 32, 0, stream>>>(c->d_table, grads, c->d_tiles + c->first[kind], k);
@@ -440,8 +499,9 @@ came_status came_adamw_create(came_adamw_ctx** out, const came_adamw_tensor* t, 
         long long blocks = 0;
         for (int i = 0; i < n; ++i) blocks += (t[i].numel + kBlock - 1) / kBlock;
         if (blocks > (1ll << 31)) { free_adamw(c); return report(CAME_ERR_SHAPE, "more than 2^39 elements in all"); }
-        // a block per warp in small lists, four in large ones
-        c->per_tile = kWarps * (blocks > 148 * 8 * kWarps * 4 ? 4 : 1);
+        // 8 bits: up to eight, so that a tile writes whole sectors of scales and loads ahead (64 M elements: 161 us,
+        // 230 with one), as long as there are tiles for every SM.  fp32: one (261 us, 272 with eight).
+        while (c->per_warp[1] < 8 && blocks >= 148ll * kWarps * c->per_warp[1]) c->per_warp[1] *= 2;
         std::vector<AdamwTensor> table(n);
         std::vector<AdamwTile> tiles;
         long long block0 = 0;
@@ -455,14 +515,15 @@ came_status came_adamw_create(came_adamw_ctx** out, const came_adamw_tensor* t, 
         }
         for (int kind = 0; kind < 4; ++kind) {
             c->first[kind] = static_cast<int>(tiles.size());
+            const unsigned per_tile = kWarps * c->per_warp[kind >> 1];
             for (int i = 0; i < n; ++i) {
                 if (kind_of(t[i]) != kind) continue;
                 const long long have = (t[i].numel + kBlock - 1) / kBlock;
-                if (static_cast<long long>(tiles.size()) + have / c->per_tile + 1 > (1 << 28)) {
+                if (static_cast<long long>(tiles.size()) + have / per_tile + 1 > (1 << 28)) {
                     free_adamw(c);
                     return report(CAME_ERR_SHAPE, "too many tiles");
                 }
-                for (long long b = 0; b < have; b += c->per_tile) tiles.push_back(AdamwTile{i, static_cast<unsigned>(b)});
+                for (long long b = 0; b < have; b += per_tile) tiles.push_back(AdamwTile{i, static_cast<unsigned>(b)});
             }
         }
         c->first[4] = static_cast<int>(tiles.size());
@@ -536,7 +597,6 @@ came_status came_adamw_step(came_adamw_ctx* ctx, const came_adamw_hparams* hp, c
     k.root = static_cast<float>(1.0 / std::sqrt(-std::expm1(t * k.log_b2)));
     k.key_seed = mix_word(0u, hp->seed);
     k.key = mix_word(k.key_seed, static_cast<uint64_t>(device_step ? 1 : hp->step));
-    k.per_tile = ctx->per_tile;
     k.device_scale = device_scale;
     k.device_step = device_step;
     cudaError_t e = cudaSuccess;
