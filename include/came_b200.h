@@ -512,6 +512,50 @@ came_status came_adamw_step(came_adamw_ctx* ctx, const came_adamw_hparams* hp, c
 /* Frees the context; the caller has synchronised the streams it used. */
 came_status came_adamw_destroy(came_adamw_ctx* ctx);
 
+/* ---- Layer norm and its backward pass ----------------------------------------------------------
+ *
+ * Over rows x of cols elements, with weight w and bias b (each optional):
+ *   forward   mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps)
+ *             y = rn((x - mean) rstd w + b)
+ *   backward  h = (x - mean) rstd,  d = dy w,  dx = rn(rstd (d - sum d / cols - h sum (d h) / cols))
+ *             dweight = rn([dweight +] sum over rows of dy h),  dbias = rn([dbias +] sum over rows of dy)
+ *             the terms in brackets with CAME_LAYERNORM_ACCUMULATE
+ * Everything is computed in fp32 and rounded once to the stored type, to nearest even.  The variance is that of
+ * the differences from the mean.  Sums are added in an order that depends on the sizes alone: results are
+ * bit-reproducible.  Rows may have any stride >= cols and any element-aligned address (strides, lengths and
+ * addresses that are multiples of 8 elements, 16 bytes at least, are faster); weight, bias and their gradients are
+ * contiguous.  What is written shares memory with nothing else (CAME_ERR_OVERLAP; the ranges from a buffer's
+ * first to its last element count). */
+enum { CAME_LAYERNORM_ACCUMULATE = 1u << 0 };   /* backward: add to dweight and dbias */
+
+typedef struct {
+    const void*  x;           /* DEVICE x_dtype [rows][x_ld]                                      */
+    const void*  weight;      /* DEVICE weight_dtype [cols] or NULL (ones)                        */
+    const void*  bias;        /* forward: DEVICE weight_dtype [cols] or NULL; backward: not used  */
+    void*        y;           /* forward: DEVICE y_dtype [rows][y_ld]                             */
+    const void*  dy;          /* backward: DEVICE y_dtype [rows][y_ld]                            */
+    void*        dx;          /* backward: DEVICE dx_dtype [rows][dx_ld] or NULL                  */
+    void*        dweight;     /* backward: DEVICE weight_dtype [cols] or NULL                     */
+    void*        dbias;       /* backward: DEVICE weight_dtype [cols] or NULL                     */
+    float*       mean;        /* DEVICE fp32 [rows]: forward: written, or NULL; backward: read    */
+    float*       rstd;        /* DEVICE fp32 [rows] likewise (both or none)                       */
+    int64_t      rows, cols;  /* rows 0 .. 2^30, cols 1 .. 2^27                                   */
+    int64_t      x_ld, y_ld, dx_ld;   /* elements from row to row, cols .. 2^29 (unused ones: 0)  */
+    double       eps;         /* forward: >= 0, taken as fp32                                     */
+    int32_t      x_dtype, y_dtype, dx_dtype, weight_dtype;   /* came_dtype                        */
+    uint32_t     flags;       /* CAME_LAYERNORM_*; forward: 0                                     */
+    uint32_t     reserved;    /* must be 0                                                        */
+} came_layernorm;
+
+/* Asynchronous on `cuda_stream`; allocate nothing; `device` must be current and hold every buffer.  Errors
+ * through came_last_error(NULL).  The backward pass needs `workspace` (DEVICE, 16-byte aligned, at least the
+ * bytes that came_layernorm_workspace answers for the same descriptor; no CUDA call there); its contents need not
+ * be kept between calls, and calls that may run at the same time need one each. */
+came_status came_layernorm_forward(const came_layernorm* l, int32_t device, void* cuda_stream);
+came_status came_layernorm_workspace(const came_layernorm* l, int64_t* out_bytes);
+came_status came_layernorm_backward(const came_layernorm* l, void* workspace, int64_t workspace_bytes,
+                                    int32_t device, void* cuda_stream);
+
 /* Process-wide tuning knobs, read by later came_create calls (each knob is an atomic, so any
  * thread may set one; a context takes the values in force while it is being created, so set
  * them before the contexts they are meant for).  CAME_TUNE_TILE_ELEMS:

@@ -23,6 +23,7 @@ CAME_OK = 0
 CAME_F32, CAME_BF16 = 0, 1
 CAME_I32, CAME_I64 = 0, 1
 CAME_EMBED_ACCUMULATE, CAME_EMBED_PADDING_ROW = 1, 2
+CAME_LAYERNORM_ACCUMULATE = 1
 CAME_T_NO_WEIGHT_DECAY = 1
 CAME_T_VEC_NO_CONFIDENCE = 2
 CAME_CREATE_KEEP_STATE = 1
@@ -54,7 +55,8 @@ EXPORTED = ["came_create", "came_step", "came_step_host", "came_destroy", "came_
             "came_selftest_wait_timeout", "came_debug_bounds", "came_step_scaled",
             "came_clip_create", "came_clip_norm", "came_clip_grads", "came_clip_destroy",
             "came_embed_forward", "came_embed_workspace", "came_embed_backward",
-            "came_adamw_create", "came_adamw_step", "came_adamw_destroy"]
+            "came_adamw_create", "came_adamw_step", "came_adamw_destroy",
+            "came_layernorm_forward", "came_layernorm_workspace", "came_layernorm_backward"]
 
 
 class CameError(RuntimeError):
@@ -109,6 +111,13 @@ class came_adamw_hparams(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
                 ("eps", ctypes.c_double), ("weight_decay", ctypes.c_double), ("grad_scale", ctypes.c_double),
                 ("step", ctypes.c_int64), ("seed", ctypes.c_uint64)]
+
+
+class came_layernorm(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("x", "weight", "bias", "y", "dy", "dx", "dweight", "dbias", "mean", "rstd")] + \
+               [(k, ctypes.c_int64) for k in ("rows", "cols", "x_ld", "y_ld", "dx_ld")] + [("eps", ctypes.c_double)] + \
+               [(k, ctypes.c_int32) for k in ("x_dtype", "y_dtype", "dx_dtype", "weight_dtype")] + \
+               [("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 _lib = None
@@ -220,6 +229,12 @@ def _bind(L):
     L.came_adamw_step.restype = i32
     L.came_adamw_destroy.argtypes = [vp]
     L.came_adamw_destroy.restype = i32
+    L.came_layernorm_forward.argtypes = [ctypes.POINTER(came_layernorm), i32, vp]
+    L.came_layernorm_forward.restype = i32
+    L.came_layernorm_workspace.argtypes = [ctypes.POINTER(came_layernorm), ctypes.POINTER(i64)]
+    L.came_layernorm_workspace.restype = i32
+    L.came_layernorm_backward.argtypes = [ctypes.POINTER(came_layernorm), vp, i64, i32, vp]
+    L.came_layernorm_backward.restype = i32
     return L
 
 
@@ -434,6 +449,27 @@ def came_adamw_step(ctx, hp: came_adamw_hparams, grads: Optional[Sequence[int]] 
 
 def came_adamw_destroy(ctx) -> None:
     _check(load().came_adamw_destroy(ctx))
+
+
+def came_layernorm_forward(l: came_layernorm, device: int = 0, stream: int = 0) -> None:
+    status = (_lib or load()).came_layernorm_forward(l, device, stream)
+    if status:
+        _check(status)
+
+
+def came_layernorm_workspace(l: came_layernorm) -> int:
+    out = ctypes.c_int64()
+    status = (_lib or load()).came_layernorm_workspace(l, out)
+    if status:
+        _check(status)
+    return out.value
+
+
+def came_layernorm_backward(l: came_layernorm, workspace: int, workspace_bytes: int, device: int = 0,
+                            stream: int = 0) -> None:
+    status = (_lib or load()).came_layernorm_backward(l, workspace, workspace_bytes, device, stream)
+    if status:
+        _check(status)
 
 
 def make_hparams(step: int, **kw) -> came_hparams:
@@ -943,3 +979,170 @@ class AdamWOptimizer:
             self.close()
         except Exception:
             pass
+
+
+# --- layer norm ----------------------------------------------------------------------------------
+
+
+def _rows_of(x, name, shape, index):
+    """(rows, columns, row stride, dtype code) of a tensor whose last dimension is normalised."""
+    if x.get_device() != index:
+        raise CameError(CAME_ERR_DEVICE, f"{name} must be on the GPU of x" if index >= 0 and name != "x" else f"{name} must be a CUDA tensor")
+    code = _dtype_code(x, name)
+    if shape is not None and x.shape != shape:
+        raise CameError(CAME_ERR_SHAPE, f"{name} must have the shape of x")
+    cols = x.shape[-1]
+    if x.dim() != 2:
+        rows = x.numel() // cols if cols else 0
+        if x.is_contiguous():
+            return rows, cols, cols, code
+        try:
+            x = x.view(rows, cols)
+        except RuntimeError:
+            raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must lie at one stride") from None
+    rows = x.shape[0]
+    ld, one = x.stride()
+    if one != 1 and cols > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, f"the rows of {name} must be contiguous")
+    return rows, cols, ld if rows > 1 else cols, code           # (the stride of a single row says nothing)
+
+
+def _norm_param(p, name, cols, index, code):
+    """Address of a parameter (or gradient) of a row's length, and its dtype code; `code`: the one that it must have."""
+    if p is None:
+        return 0, code
+    if p.get_device() != index:
+        raise CameError(CAME_ERR_DEVICE, f"{name} must be on the GPU of x")
+    mine = _dtype_code(p, name)
+    if code is not None and mine != code:
+        raise CameError(CAME_ERR_DTYPE, f"{name} must have the weight's dtype")
+    if p.dim() != 1 or p.shape[0] != cols:
+        raise CameError(CAME_ERR_SHAPE, f"{name} must have {cols} elements")
+    if not p.is_contiguous():
+        raise CameError(CAME_ERR_UNSUPPORTED, f"{name} must be contiguous")
+    return p.data_ptr(), mine
+
+
+def _norm_stats(mean, rstd, rows, index):
+    torch = _torch()
+    for s, name in ((mean, "mean"), (rstd, "rstd")):
+        if s.get_device() != index:
+            raise CameError(CAME_ERR_DEVICE, f"{name} must be on the GPU of x")
+        if s.dtype != torch.float32:
+            raise CameError(CAME_ERR_DTYPE, f"{name} must be fp32")
+        if s.numel() != rows or not s.is_contiguous():
+            raise CameError(CAME_ERR_SHAPE, f"{name} must be contiguous and have one element per row")
+
+
+def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, out=None, out_dtype=None, stats: bool = True):
+    """``(y, mean, rstd)`` with ``y = (x - mean) * rstd * weight + bias`` over the last dimension, ``rstd`` =
+    1 / sqrt(variance + eps).
+
+    ``x``: fp32 or bf16 CUDA tensor of any shape whose rows (the last dimension) are contiguous and lie at one stride;
+    ``weight``, ``bias``: contiguous, as long as a row, fp32 or bf16, or None.  ``out``: tensor of x's shape, made here
+    (of type ``out_dtype``, x's when that is None too) when it is None.  ``mean`` and ``rstd`` are fp32, one for
+    each row, in the shape of x without its last dimension; with ``stats`` false they are neither computed for the
+    caller nor returned: ``y`` alone is (inference).  No autograd: see ``layer_norm``."""
+    torch = _torch()
+    if not x.dim() or not x.shape[-1]:
+        raise CameError(CAME_ERR_SHAPE, "x must have a last dimension of at least one element")
+    index = x.get_device()
+    if index < 0:
+        raise CameError(CAME_ERR_DEVICE, "x must be a CUDA tensor")
+    rows, cols, x_ld, x_code = _rows_of(x, "x", None, index)
+    w_at, w_code = _norm_param(weight, "weight", cols, index, None)
+    b_at, w_code = _norm_param(bias, "bias", cols, index, w_code)
+    if out is None:
+        out = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
+        y_ld, y_code = cols, _dtype_code(out, "out")
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
+        _, _, y_ld, y_code = _rows_of(out, "out", x.shape, index)
+    mean = rstd = None
+    mean_at = rstd_at = 0
+    if stats:
+        both = torch.empty((2, *x.shape[:-1]), dtype=torch.float32, device=x.device)
+        mean, rstd = both.unbind(0)
+        mean_at = both.data_ptr()
+        rstd_at = mean_at + 4 * rows
+    l = came_layernorm(x.data_ptr(), w_at, b_at, out.data_ptr(), 0, 0, 0, 0, mean_at, rstd_at, rows, cols, x_ld, y_ld, 0, eps,
+                       x_code, y_code, 0, w_code or 0, 0, 0)
+    _call_on(index, came_layernorm_forward, l)
+    return (out, mean, rstd) if stats else out
+
+
+def layer_norm_backward(grad_out, x, mean, rstd, weight=None, grad_x=None, grad_weight=None, grad_bias=None,
+                        accumulate: bool = False, need_x: bool = True):
+    """The gradient of x, in ``grad_x`` (made here, of x's type, when it is None; nothing with ``need_x`` false).
+
+    ``grad_out``, ``x``: fp32 or bf16, of the same shape; ``mean``, ``rstd``: as ``layer_norm_forward`` gave
+    them.  ``grad_weight``, ``grad_bias``: buffers of a row's length, in the weight's type (fp32 or bf16, both the same,
+    without a weight), which receive the sums over all rows, or to which these are added with ``accumulate``; None: not
+    wanted.  Returns ``grad_x``.  Bit-reproducible."""
+    torch = _torch()
+    if not x.dim() or not x.shape[-1]:
+        raise CameError(CAME_ERR_SHAPE, "x must have a last dimension of at least one element")
+    index = x.get_device()
+    if index < 0:
+        raise CameError(CAME_ERR_DEVICE, "x must be a CUDA tensor")
+    rows, cols, x_ld, x_code = _rows_of(x, "x", None, index)
+    _, _, y_ld, y_code = _rows_of(grad_out, "grad_out", x.shape, index)
+    _norm_stats(mean, rstd, rows, index)
+    w_at, w_code = _norm_param(weight, "weight", cols, index, None)
+    dw_at, w_code = _norm_param(grad_weight, "grad_weight", cols, index, w_code)
+    db_at, w_code = _norm_param(grad_bias, "grad_bias", cols, index, w_code)
+    dx_at = dx_ld = dx_code = 0
+    if grad_x is not None:
+        _, _, dx_ld, dx_code = _rows_of(grad_x, "grad_x", x.shape, index)
+        dx_at = grad_x.data_ptr()
+    elif need_x:
+        grad_x = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx_at, dx_ld, dx_code = grad_x.data_ptr(), cols, x_code
+    l = came_layernorm(x.data_ptr(), w_at, 0, 0, grad_out.data_ptr(), dx_at, dw_at, db_at, mean.data_ptr(), rstd.data_ptr(), rows, cols,
+                       x_ld, y_ld, dx_ld, 0.0, x_code, y_code, dx_code, w_code or 0, CAME_LAYERNORM_ACCUMULATE if accumulate else 0, 0)
+    size = came_layernorm_workspace(l)
+    # from torch's allocator, for the device's current stream: not reused before the call is done
+    ws = torch.empty((size + 3) // 4, dtype=torch.float32, device=x.device)
+    _call_on(index, came_layernorm_backward, l, ws.data_ptr(), size)
+    return grad_x
+
+
+_layer_norm_class = None
+
+
+def _layer_norm_function():
+    """Layer norm as an autograd function."""
+    global _layer_norm_class
+    if _layer_norm_class is None:
+        torch = _torch()
+
+        class LayerNorm(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, x, weight, bias, eps, out_dtype):
+                y, mean, rstd = layer_norm_forward(x, weight, bias, eps, out_dtype=out_dtype)
+                ctx.save_for_backward(x, weight, mean, rstd)
+                ctx.bias_like = None if bias is None else (bias.shape, bias.dtype)
+                return y
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, grad_out):
+                x, weight, mean, rstd = ctx.saved_tensors
+                need_x, need_w, need_b = ctx.needs_input_grad[:3]
+                new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=x.device)  # noqa: E731
+                dw = new(weight.shape, weight.dtype) if need_w else None
+                db = new(*ctx.bias_like) if need_b else None
+                dx = layer_norm_backward(grad_out.contiguous(), x, mean, rstd, weight, grad_weight=dw, grad_bias=db, need_x=need_x)
+                return dx, dw, db, None, None
+
+        _layer_norm_class = LayerNorm
+    return _layer_norm_class
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out_dtype=None):
+    """``layer_norm_forward``'s y as part of autograd's graph (once differentiable): gradients of ``x``, ``weight`` and
+    ``bias``, each in its own type.  When nothing requires grad, or grad mode is off, y alone is computed."""
+    if _torch().is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad)):
+        return _layer_norm_function().apply(x, weight, bias, eps, out_dtype)
+    return layer_norm_forward(x, weight, bias, eps, out_dtype=out_dtype, stats=False)

@@ -1,0 +1,661 @@
+// Layer norm over the rows of a matrix, and its backward pass.
+//
+//   y = (x - mean) rstd w + b
+//   dx = rstd (d - mean(d) - h mean(d h)),  d = dy w,  h = (x - mean) rstd
+//   dw = sum over rows of dy h,  db = sum over rows of dy
+//
+// A group of 32 to 1024 threads takes a row: it is read once and stays in registers, as stored, while its sums are
+// formed.  In the backward pass a group goes from row to row and keeps, for its columns, the sums over its
+// rows in registers; blocks write those to the workspace, and a second, short grid adds them.
+#include "came_vec.cuh"
+
+#include <algorithm>
+
+namespace {
+
+using namespace came_ops;
+
+constexpr int kSMs = 148;
+constexpr int kBlockThreads = 512;       // threads of a block whose groups are smaller than that
+constexpr int kHeld = 8;                 // backward: elements per thread that a group holds of a row
+
+struct LnArgs {
+    const void* x;
+    const void* w;
+    const void* b;
+    void*       y;                       // backward: dx
+    const void* dy;
+    float*      mean;
+    float*      rstd;
+    float*      part;                    // backward: [blocks][2][cols]
+    int         rows, cols;
+    long long   x_ld, y_ld, dy_ld;
+    float       eps, inv_cols;
+    int         tpr;                     // threads per row
+    int         w_bf16, y_bf16;
+};
+
+template <int V>
+__device__ __forceinline__ void load_param(const void* p, int is_bf16, int at, float (&out)[V])
+{
+    if (is_bf16) {
+        Vec<__nv_bfloat16, V> v;
+        v.load(static_cast<const __nv_bfloat16*>(p) + at);
+#pragma unroll
+        for (int k = 0; k < V; ++k) out[k] = v.value(k);
+    } else {
+        Vec<float, V> v;
+        v.load(static_cast<const float*>(p) + at);
+#pragma unroll
+        for (int k = 0; k < V; ++k) out[k] = v.value(k);
+    }
+}
+
+template <int V>
+__device__ __forceinline__ void store_as(void* p, int is_bf16, long long at, const float (&x)[V])
+{
+    if (is_bf16) {
+        Vec<__nv_bfloat16, V> v;
+        v.set(x);
+        v.store(static_cast<__nv_bfloat16*>(p) + at);
+    } else {
+        Vec<float, V> v;
+        v.set(x);
+        v.store(static_cast<float*>(p) + at);
+    }
+}
+
+__device__ __forceinline__ void group_barrier(int group, int tpr)
+{
+    asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(tpr) : "memory");
+}
+
+// Sum over a group's threads, the same in all of them.  `room`: shared memory of the group, 32 entries; a caller
+// that comes back before the group's next barrier takes another one.
+template <int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], int group, int tpr, float (*room)[N])
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+    if (tpr == 32) return;
+    const int lane = threadIdx.x & 31, warps = tpr >> 5, warp = (threadIdx.x & (tpr - 1)) >> 5;
+    if (lane == 0)
+#pragma unroll
+        for (int n = 0; n < N; ++n) room[warp][n] = v[n];
+    group_barrier(group, tpr);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = lane < warps ? room[lane][n] : 0.f;
+    for (int o = warps >> 1; o > 0; o >>= 1)
+#pragma unroll
+        for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+#pragma unroll
+    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, v[n], 0);
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+
+// C accesses of V elements per thread: the row's column (c tpr + thread) V.
+template <typename X, int V, int C>
+__global__ void __launch_bounds__(1024)
+k_ln_forward(const __grid_constant__ LnArgs a)
+{
+    __shared__ float room[2][32][1];     // 32 warps at most, of all groups together; one set for each sum
+    const int tpr = a.tpr, group = threadIdx.x / tpr, t = threadIdx.x & (tpr - 1);
+    const int row = blockIdx.x * (blockDim.x / tpr) + group;
+    if (row >= a.rows) return;           // (the whole group)
+    const int warp0 = group * (tpr >> 5);
+    const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
+    Vec<X, V> raw[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * tpr + t) * V;
+        if (col < a.cols) raw[c].load(x + col);
+    }
+    float sum[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if ((c * tpr + t) * V < a.cols)
+#pragma unroll
+            for (int k = 0; k < V; ++k) sum[0] += raw[c].value(k);
+    group_sum<1>(sum, group, tpr, room[0] + warp0);
+    const float mean = sum[0] * a.inv_cols;
+    float sq[1] = {0.f};
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+        if ((c * tpr + t) * V < a.cols)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float d = raw[c].value(k) - mean;
+                sq[0] = fmaf(d, d, sq[0]);
+            }
+    group_sum<1>(sq, group, tpr, room[1] + warp0);
+    const float rstd = __frsqrt_rn(fmaf(sq[0], a.inv_cols, a.eps));
+    if (t == 0 && a.mean) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * tpr + t) * V;
+        if (col >= a.cols) continue;
+        float y[V], p[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) y[k] = (raw[c].value(k) - mean) * rstd;
+        if (a.w) {
+            load_param<V>(a.w, a.w_bf16, col, p);
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] *= p[k];
+        }
+        if (a.b) {
+            load_param<V>(a.b, a.w_bf16, col, p);
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] += p[k];
+        }
+        store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, y);
+    }
+}
+
+// Rows that do not fit a block's registers: three passes over a row.
+template <typename X, int V>
+__global__ void __launch_bounds__(1024)
+k_ln_forward_long(const __grid_constant__ LnArgs a)
+{
+    __shared__ float room[2][32][1];
+    const int row = blockIdx.x, t = threadIdx.x;
+    const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
+    float sum[1] = {0.f}, sq[1] = {0.f};
+    for (int col = t * V; col < a.cols; col += 1024 * V) {
+        Vec<X, V> v;
+        v.load(x + col);
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) s += v.value(k);
+        sum[0] += s;
+    }
+    group_sum<1>(sum, 0, 1024, room[0]);
+    const float mean = sum[0] * a.inv_cols;
+    for (int col = t * V; col < a.cols; col += 1024 * V) {
+        Vec<X, V> v;
+        v.load(x + col);
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float d = v.value(k) - mean;
+            s = fmaf(d, d, s);
+        }
+        sq[0] += s;
+    }
+    group_sum<1>(sq, 0, 1024, room[1]);
+    const float rstd = __frsqrt_rn(fmaf(sq[0], a.inv_cols, a.eps));
+    if (t == 0 && a.mean) {
+        a.mean[row] = mean;
+        a.rstd[row] = rstd;
+    }
+    for (int col = t * V; col < a.cols; col += 1024 * V) {
+        Vec<X, V> v;
+        v.load(x + col);
+        float y[V], p[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) y[k] = (v.value(k) - mean) * rstd;
+        if (a.w) {
+            load_param<V>(a.w, a.w_bf16, col, p);
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] *= p[k];
+        }
+        if (a.b) {
+            load_param<V>(a.b, a.w_bf16, col, p);
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] += p[k];
+        }
+        store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, y);
+    }
+}
+
+// ---- backward -----------------------------------------------------------------------------------
+
+template <typename X, typename G, int V, int C>
+struct RowPair {
+    Vec<X, V> x[C];
+    Vec<G, V> dy[C];
+    float mean, rstd;
+    __device__ __forceinline__ void load(const LnArgs& a, long long row, int t)
+    {
+        mean = a.mean[row];
+        rstd = a.rstd[row];
+        const X* const px = static_cast<const X*>(a.x) + row * a.x_ld;
+        const G* const pg = static_cast<const G*>(a.dy) + row * a.dy_ld;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * a.tpr + t) * V;
+            if (col < a.cols) {
+                x[c].load(px + col);
+                dy[c].load(pg + col);
+            }
+        }
+    }
+};
+
+template <typename X, typename G, int V, int C>
+__global__ void __launch_bounds__(1024)
+k_ln_backward(const __grid_constant__ LnArgs a)
+{
+    extern __shared__ float sums[];      // the groups' sums at the end: [2][cols]
+    __shared__ float room[2][32][2];
+    const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x & (tpr - 1);
+    const int warp0 = group * (tpr >> 5);
+    const long long step = static_cast<long long>(gridDim.x) * groups;
+    float w[C][V], dw[C][V], db[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * tpr + t) * V;
+#pragma unroll
+        for (int k = 0; k < V; ++k) w[c][k] = 1.f, dw[c][k] = db[c][k] = 0.f;
+        if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
+    }
+    RowPair<X, G, V, C> next;
+    long long row = static_cast<long long>(blockIdx.x) * groups + group;
+    int turn = 0;
+    if (row < a.rows) next.load(a, row, t);
+    for (; row < a.rows; row += step, turn ^= 1) {
+        const RowPair<X, G, V, C> now = next;
+        if (row + step < a.rows) next.load(a, row + step, t);
+        float s[2] = {0.f, 0.f};         // sums of d and of d h
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+            if ((c * tpr + t) * V < a.cols)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float h = (now.x[c].value(k) - now.mean) * now.rstd, g = now.dy[c].value(k), d = g * w[c][k];
+                    dw[c][k] = fmaf(g, h, dw[c][k]);
+                    db[c][k] += g;
+                    s[0] += d;
+                    s[1] = fmaf(d, h, s[1]);
+                }
+        if (!a.y) continue;
+        group_sum<2>(s, group, tpr, room[turn] + warp0);
+        const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * tpr + t) * V;
+            if (col >= a.cols) continue;
+            float o[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float h = (now.x[c].value(k) - now.mean) * now.rstd;
+                o[k] = now.rstd * (fmaf(now.dy[c].value(k), w[c][k], -c1) - h * c2);
+            }
+            store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, o);
+        }
+    }
+    if (!a.part) return;
+    // the groups one after another, so that the order is theirs
+    float* const part = a.part + 2ll * blockIdx.x * a.cols;
+    for (int g = 0; g < groups; ++g) {
+        const bool last = g == groups - 1;
+        if (group == g)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * tpr + t) * V;
+                if (col >= a.cols) continue;
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    float p = dw[c][k], q = db[c][k];
+                    if (g > 0) p += sums[col + k], q += sums[a.cols + col + k];
+                    if (last) part[col + k] = p, part[a.cols + col + k] = q;
+                    else sums[col + k] = p, sums[a.cols + col + k] = q;
+                }
+            }
+        if (!last) __syncthreads();
+    }
+}
+
+// Rows that do not fit a group: first each row's two sums ...
+template <typename X, typename G, int V>
+__global__ void __launch_bounds__(1024)
+k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
+{
+    __shared__ float room[1][32][2];
+    const int row = blockIdx.x;
+    const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
+    const G* const dy = static_cast<const G*>(a.dy) + row * a.dy_ld;
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    float s[2] = {0.f, 0.f};
+    for (int col = threadIdx.x * V; col < a.cols; col += 1024 * V) {
+        Vec<X, V> vx;
+        Vec<G, V> vg;
+        vx.load(x + col);
+        vg.load(dy + col);
+        float w[V], p = 0.f, q = 0.f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) w[k] = 1.f;
+        if (a.w) load_param<V>(a.w, a.w_bf16, col, w);
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float d = vg.value(k) * w[k];
+            p += d;
+            q = fmaf(d, (vx.value(k) - mean) * rstd, q);
+        }
+        s[0] += p;
+        s[1] += q;
+    }
+    group_sum<2>(s, 0, 1024, room[0]);
+    if (threadIdx.x == 0) out[row] = make_float2(s[0] * a.inv_cols, s[1] * a.inv_cols);
+}
+
+// ... then everything else by columns: a block of 8 warps has 32 V columns and every gridDim.y-th group of 8 rows.
+template <typename X, typename G, int V>
+__global__ void __launch_bounds__(256)
+k_ln_backward_columns(const __grid_constant__ LnArgs a, const float2* means)
+{
+    __shared__ float sums[8][2][32 * V];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int col = (blockIdx.x * 32 + lane) * V;
+    const bool in = col < a.cols;
+    float w[V], dw[V], db[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) w[k] = 1.f, dw[k] = db[k] = 0.f;
+    if (a.w && in) load_param<V>(a.w, a.w_bf16, col, w);
+    for (long long row = blockIdx.y * 8 + warp; in && row < a.rows; row += 8 * gridDim.y) {
+        Vec<X, V> vx;
+        Vec<G, V> vg;
+        vx.load(static_cast<const X*>(a.x) + row * a.x_ld + col);
+        vg.load(static_cast<const G*>(a.dy) + row * a.dy_ld + col);
+        const float mean = a.mean[row], rstd = a.rstd[row];
+        float o[V];
+        float2 c = make_float2(0.f, 0.f);
+        if (a.y) c = means[row];
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float h = (vx.value(k) - mean) * rstd, g = vg.value(k);
+            dw[k] = fmaf(g, h, dw[k]);
+            db[k] += g;
+            o[k] = rstd * (fmaf(g, w[k], -c.x) - h * c.y);
+        }
+        if (a.y) store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, o);
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int k = 0; k < V; ++k) sums[warp][0][lane * V + k] = dw[k], sums[warp][1][lane * V + k] = db[k];
+    __syncthreads();
+    float* const part = a.part + 2ll * blockIdx.y * a.cols;
+    for (int i = threadIdx.x; i < 64 * V; i += 256) {
+        const int which = i / (32 * V), at = i % (32 * V), column = blockIdx.x * 32 * V + at;
+        float s = 0.f;
+        for (int g = 0; g < 8; ++g) s += sums[g][which][at];
+        if (column < a.cols) part[static_cast<long long>(which) * a.cols + column] = s;
+    }
+}
+
+// Adds the blocks' sums: 32 columns for each block, 32 warps that take every 32nd partial sum.
+struct LnFinish {
+    const float* part;
+    void*        dw;
+    void*        db;
+    int          parts, cols, bf16, accumulate;
+};
+
+__global__ void __launch_bounds__(1024)
+k_ln_finish(const __grid_constant__ LnFinish f)
+{
+    __shared__ float s[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 32 + lane, which = blockIdx.y;
+    void* const out = which ? f.db : f.dw;
+    if (!out) return;
+    wait_for_previous_grid();
+    float v = 0.f;
+    if (col < f.cols)
+        for (int p = warp; p < f.parts; p += 32) v += f.part[(2ll * p + which) * f.cols + col];
+    s[warp][lane] = v;
+    __syncthreads();
+    if (warp != 0 || col >= f.cols) return;
+    float t = 0.f;
+    for (int g = 0; g < 32; ++g) t += s[g][lane];
+    if (f.bf16) {
+        __nv_bfloat16* const o = static_cast<__nv_bfloat16*>(out) + col;
+        *o = __float2bfloat16_rn(f.accumulate ? to_float(*o) + t : t);
+    } else {
+        float* const o = static_cast<float*>(out) + col;
+        *o = f.accumulate ? *o + t : t;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+int round_up_power(long long x)
+{
+    int p = 1;
+    while (p < x) p <<= 1;
+    return p;
+}
+
+came_status validate_ln(const came_layernorm* l, bool backward)
+{
+    if (!l) return report(CAME_ERR_NULL, "descriptor is NULL");
+    if (l->rows < 0 || l->rows > (1ll << 30) || l->cols < 1 || l->cols > (1ll << 27))
+        return report(CAME_ERR_SHAPE, "rows must lie in [0, 2^30], cols in [1, 2^27]");
+    const bool dx = backward && l->dx;
+    auto ld_ok = [&](int64_t ld) { return ld >= l->cols && ld <= (1ll << 29) && ld <= (1ll << 40) / std::max<int64_t>(1, l->rows); };
+    if (!ld_ok(l->x_ld) || !ld_ok(l->y_ld) || (dx && !ld_ok(l->dx_ld)))
+        return report(CAME_ERR_SHAPE, "a row stride is below cols, or too large");
+    if (!known_dtype(l->x_dtype) || !known_dtype(l->y_dtype) || !known_dtype(l->weight_dtype) || (dx && !known_dtype(l->dx_dtype)))
+        return report(CAME_ERR_DTYPE, "unknown dtype");
+    if (l->flags & ~static_cast<uint32_t>(CAME_LAYERNORM_ACCUMULATE)) return report(CAME_ERR_UNSUPPORTED, "unknown flag");
+    if (l->flags && !backward) return report(CAME_ERR_UNSUPPORTED, "the flags apply to the backward pass only");
+    if (l->reserved) return report(CAME_ERR_SHAPE, "reserved must be 0");
+    if (!backward && !(l->eps >= 0 && l->eps <= FLT_MAX)) return report(CAME_ERR_HPARAM, "eps must be finite and >= 0");
+    if (l->rows) {
+        if (!l->x || (backward ? !l->dy || !l->mean || !l->rstd : !l->y)) return report(CAME_ERR_NULL, "a required buffer is NULL");
+        if (!l->mean != !l->rstd) return report(CAME_ERR_NULL, "mean and rstd belong together");
+    }
+    const size_t xs = dtype_bytes(l->x_dtype), ys = dtype_bytes(l->y_dtype), ws = dtype_bytes(l->weight_dtype), ds = dtype_bytes(l->dx_dtype);
+    const void* const y = backward ? l->dy : l->y;
+    if (!aligned_to(l->x, xs) || !aligned_to(y, ys) || !aligned_to(l->weight, ws) || !aligned_to(l->mean, 4) || !aligned_to(l->rstd, 4) ||
+        (backward ? (dx && !aligned_to(l->dx, ds)) || !aligned_to(l->dweight, ws) || !aligned_to(l->dbias, ws) : !aligned_to(l->bias, ws)))
+        return report(CAME_ERR_ALIGN, "a pointer is not aligned to its element size");
+    struct Range { uintptr_t lo, hi; bool out; } r[9];
+    int n = 0;
+    auto add = [&](const void* p, unsigned long long bytes, bool out) {
+        const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+        if (p && bytes) r[n++] = Range{lo, lo + bytes, out};
+    };
+    auto span = [&](int64_t ld, size_t b) { return l->rows ? ((l->rows - 1) * ld + l->cols) * static_cast<unsigned long long>(b) : 0ull; };
+    add(l->x, span(l->x_ld, xs), false);
+    add(y, span(l->y_ld, ys), !backward);
+    add(l->weight, l->cols * ws, false);
+    add(l->mean, l->rows * 4ull, !backward);
+    add(l->rstd, l->rows * 4ull, !backward);
+    if (backward) {
+        if (dx) add(l->dx, span(l->dx_ld, ds), true);
+        add(l->dweight, l->cols * ws, true);
+        add(l->dbias, l->cols * ws, true);
+    } else {
+        add(l->bias, l->cols * ws, false);
+    }
+    for (int i = 0; i < n; ++i)
+        for (int j = 0; j < i; ++j)
+            if ((r[i].out || r[j].out) && r[i].lo < r[j].hi && r[j].lo < r[i].hi)
+                return report(CAME_ERR_OVERLAP, "a buffer that is written shares memory with another");
+    return CAME_OK;
+}
+
+// Elements per access: 8 where every row of every tensor starts at a multiple of 8 elements (and 16 bytes, or 32), then 2, then 1.
+int access_of(const came_layernorm& l, bool backward)
+{
+    for (int v : {8, 2}) {
+        bool ok = l.cols % v == 0 && l.x_ld % v == 0 && l.y_ld % v == 0;
+        auto fits = [&](const void* p, int32_t dt) { ok = ok && aligned_to(p, v * dtype_bytes(dt)); };
+        fits(l.x, l.x_dtype);
+        fits(backward ? l.dy : l.y, l.y_dtype);
+        fits(l.weight, l.weight_dtype);
+        if (!backward) fits(l.bias, l.weight_dtype);
+        if (backward && l.dx) {
+            ok = ok && l.dx_ld % v == 0;
+            fits(l.dx, l.dx_dtype);
+        }
+        if (ok) return v;
+    }
+    return 1;
+}
+
+struct BackwardPlan { int v, tpr, threads, blocks, column_blocks; bool is_long; size_t means, part, bytes; };
+
+BackwardPlan plan_backward(const came_layernorm& l)
+{
+    BackwardPlan p = {};
+    p.v = access_of(l, true);
+    p.is_long = l.cols > 1024 * kHeld;
+    const bool sums = l.dweight || l.dbias;
+    if (!p.is_long) {
+        p.tpr = std::max(32, round_up_power((l.cols + kHeld - 1) / kHeld));
+        p.threads = std::max(p.tpr, kBlockThreads);
+        const int groups = p.threads / p.tpr;
+        const long long want = (l.rows + groups - 1) / groups;
+        p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, kSMs * (1024 / p.threads))));
+    } else {
+        p.column_blocks = static_cast<int>((l.cols + 32 * p.v - 1) / (32 * p.v));
+        const long long want = (l.rows + 7) / 8;
+        p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, std::max(1, kSMs * 8 / p.column_blocks))));
+    }
+    size_t at = 0;
+    auto take = [&](size_t b) { const size_t here = at; at += (b + 255) / 256 * 256; return here; };
+    p.means = take(p.is_long && l.dx ? sizeof(float2) * l.rows : 0);
+    p.part = take(sums ? 8ull * p.blocks * l.cols : 0);
+    p.bytes = std::max<size_t>(at, 256);
+    return p;
+}
+
+template <typename X, int V>
+void launch_forward(const LnArgs& a0, cudaStream_t stream)
+{
+    LnArgs a = a0;
+    constexpr int kMost = 32;            // elements that a thread may hold
+    if (a.cols > 1024 * kMost) {
+        k_ln_forward_long<X, V><<<a.rows, 1024, 0, stream>>>(a);
+        return;
+    }
+    // Few rows: as many threads for each as there are accesses.  Many rows: more elements for a thread.
+    constexpr int kFew = 8 / V, kMany = kMost / V;
+    const long long units = (a.cols + V - 1) / V;
+    const bool few = a.rows <= 2 * kSMs && (units + kFew - 1) / kFew <= 1024;
+    a.tpr = std::max(32, round_up_power((units + (few ? kFew : kMany) - 1) / (few ? kFew : kMany)));
+    const int threads = std::max(a.tpr, few ? a.tpr : 256), groups = threads / a.tpr;
+    const unsigned blocks = static_cast<unsigned>((a.rows + groups - 1) / groups);
+    if (units <= static_cast<long long>(a.tpr) * kFew) k_ln_forward<X, V, kFew><<<blocks, threads, 0, stream>>>(a);
+    else k_ln_forward<X, V, kMany><<<blocks, threads, 0, stream>>>(a);
+}
+
+template <typename X>
+void launch_forward_v(const LnArgs& a, int v, cudaStream_t stream)
+{
+    if (v == 8) launch_forward<X, 8>(a, stream);
+    else if (v == 2) launch_forward<X, 2>(a, stream);
+    else launch_forward<X, 1>(a, stream);
+}
+
+template <typename X, typename G, int V>
+cudaError_t launch_backward(LnArgs a, const BackwardPlan& p, float2* means, cudaStream_t stream)
+{
+    if (p.is_long) {
+        if (a.y) k_ln_backward_rows<X, G, V><<<a.rows, 1024, 0, stream>>>(a, means);
+        k_ln_backward_columns<X, G, V><<<dim3(p.column_blocks, p.blocks), 256, 0, stream>>>(a, means);
+        return cudaGetLastError();
+    }
+    a.tpr = p.tpr;
+    const size_t smem = p.threads > p.tpr && a.part ? sizeof(float) * 2 * a.cols : 0;      // (at most 2 * 4096 floats)
+    k_ln_backward<X, G, V, kHeld / V><<<p.blocks, p.threads, smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename X, typename G>
+cudaError_t launch_backward_v(const LnArgs& a, const BackwardPlan& p, float2* means, cudaStream_t stream)
+{
+    if (p.v == 8) return launch_backward<X, G, 8>(a, p, means, stream);
+    if (p.v == 2) return launch_backward<X, G, 2>(a, p, means, stream);
+    return launch_backward<X, G, 1>(a, p, means, stream);
+}
+
+LnArgs args_of(const came_layernorm& l, bool backward)
+{
+    LnArgs a = {};
+    a.x = l.x;
+    a.w = l.weight;
+    a.b = backward ? nullptr : l.bias;
+    a.y = backward ? l.dx : l.y;
+    a.dy = backward ? l.dy : nullptr;
+    a.mean = l.mean;
+    a.rstd = l.rstd;
+    a.rows = static_cast<int>(l.rows);
+    a.cols = static_cast<int>(l.cols);
+    a.x_ld = l.x_ld;
+    a.y_ld = backward ? l.dx_ld : l.y_ld;
+    a.dy_ld = l.y_ld;
+    a.eps = static_cast<float>(l.eps);
+    a.inv_cols = static_cast<float>(1.0 / static_cast<double>(l.cols));
+    a.w_bf16 = l.weight_dtype == CAME_BF16;
+    a.y_bf16 = (backward ? l.dx_dtype : l.y_dtype) == CAME_BF16;
+    return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+came_status came_layernorm_forward(const came_layernorm* l, int32_t device, void* cuda_stream)
+{
+    came_status s = validate_ln(l, false);
+    if (s != CAME_OK) return s;
+    if ((s = require_current_device(device)) != CAME_OK) return s;
+    if (l->rows == 0) return CAME_OK;
+    const LnArgs a = args_of(*l, false);
+    const int v = access_of(*l, false);
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (l->x_dtype == CAME_BF16) launch_forward_v<__nv_bfloat16>(a, v, stream);
+    else                         launch_forward_v<float>(a, v, stream);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
+}
+
+came_status came_layernorm_workspace(const came_layernorm* l, int64_t* out_bytes)
+{
+    if (!out_bytes) return report(CAME_ERR_NULL, "out_bytes is NULL");
+    const came_status s = validate_ln(l, true);
+    if (s != CAME_OK) return s;
+    *out_bytes = static_cast<int64_t>(plan_backward(*l).bytes);
+    return CAME_OK;
+}
+
+came_status came_layernorm_backward(const came_layernorm* l, void* workspace, int64_t workspace_bytes, int32_t device, void* cuda_stream)
+{
+    came_status s = validate_ln(l, true);
+    if (s != CAME_OK) return s;
+    const BackwardPlan p = plan_backward(*l);
+    if (!workspace) return report(CAME_ERR_NULL, "workspace is NULL");
+    if (!aligned_to(workspace, 16)) return report(CAME_ERR_ALIGN, "workspace not 16-byte aligned");
+    if (workspace_bytes < static_cast<int64_t>(p.bytes)) return report(CAME_ERR_SHAPE, "workspace smaller than came_layernorm_workspace says");
+    if ((s = require_current_device(device)) != CAME_OK) return s;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    char* const ws = static_cast<char*>(workspace);
+    const bool sums = l->dweight || l->dbias;
+    LnArgs a = args_of(*l, true);
+    if (sums) a.part = reinterpret_cast<float*>(ws + p.part);
+    float2* const means = reinterpret_cast<float2*>(ws + p.means);
+    cudaError_t e = cudaSuccess;
+    if (l->rows && (a.y || sums)) {
+        if (l->x_dtype == CAME_BF16)
+            e = l->y_dtype == CAME_BF16 ? launch_backward_v<__nv_bfloat16, __nv_bfloat16>(a, p, means, stream)
+                                        : launch_backward_v<__nv_bfloat16, float>(a, p, means, stream);
+        else
+            e = l->y_dtype == CAME_BF16 ? launch_backward_v<float, __nv_bfloat16>(a, p, means, stream)
+                                        : launch_backward_v<float, float>(a, p, means, stream);
+    }
+    if (e == cudaSuccess && sums && (l->rows || !(l->flags & CAME_LAYERNORM_ACCUMULATE))) {
+        LnFinish f{a.part, l->dweight, l->dbias, l->rows ? p.blocks : 0, a.cols, a.w_bf16, (l->flags & CAME_LAYERNORM_ACCUMULATE) ? 1 : 0};
+        k_ln_finish<<<dim3(static_cast<unsigned>((l->cols + 31) / 32), 2), 1024, 0, stream>>>(f);
+        e = cudaGetLastError();
+    }
+    return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
+}
+
+}  // extern "C"
