@@ -10,14 +10,16 @@
 #include "came_vec.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace {
 
 using namespace came_ops;
 
 constexpr int kSMs = 148;
-constexpr int kBlockThreads = 512;       // threads of a block whose groups are smaller than that
-constexpr int kHeld = 8;                 // backward: elements per thread that a group holds of a row
+constexpr int kBlockThreads = 512;       // backward: threads of a block at most
+constexpr int kRingBytes = 200 << 10;    // backward: shared memory for rows on their way
+constexpr int kMaxStages = 6;
 
 struct LnArgs {
     const void* x;
@@ -32,6 +34,7 @@ struct LnArgs {
     long long   x_ld, y_ld, dy_ld;
     float       eps, inv_cols;
     int         tpr;                     // threads per row
+    int         stages;                  // backward: rows in the ring, 2 to kMaxStages
     int         w_bf16, y_bf16;
 };
 
@@ -70,26 +73,28 @@ __device__ __forceinline__ void group_barrier(int group, int tpr)
     asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(tpr) : "memory");
 }
 
-// Sum over a group's threads, the same in all of them.  `room`: shared memory of the group, 32 entries; a caller
-// that comes back before the group's next barrier takes another one.
+// Sum over a group's threads, the same in all of them.  `room`: shared memory of the group, an entry per warp; a
+// caller that comes back before the group's next barrier takes another one.
 template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], int group, int tpr, float (*room)[N])
+__device__ __forceinline__ void group_sum(float (&v)[N], int group, int tpr, int warp, float (*room)[N])
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1)
 #pragma unroll
         for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
     if (tpr == 32) return;
-    const int lane = threadIdx.x & 31, warps = tpr >> 5, warp = (threadIdx.x & (tpr - 1)) >> 5;
+    const int lane = threadIdx.x & 31, warps = tpr >> 5;
     if (lane == 0)
 #pragma unroll
         for (int n = 0; n < N; ++n) room[warp][n] = v[n];
     group_barrier(group, tpr);
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = lane < warps ? room[lane][n] : 0.f;
-    for (int o = warps >> 1; o > 0; o >>= 1)
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
+    for (int o = 16; o > 0; o >>= 1)
+        if (o < warps)                   // (the lanes at `warps` and above hold zeros)
+#pragma unroll
+            for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
 #pragma unroll
     for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, v[n], 0);
 }
@@ -102,7 +107,7 @@ __global__ void __launch_bounds__(1024)
 k_ln_forward(const __grid_constant__ LnArgs a)
 {
     __shared__ float room[2][32][1];     // 32 warps at most, of all groups together; one set for each sum
-    const int tpr = a.tpr, group = threadIdx.x / tpr, t = threadIdx.x & (tpr - 1);
+    const int tpr = a.tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
     const int row = blockIdx.x * (blockDim.x / tpr) + group;
     if (row >= a.rows) return;           // (the whole group)
     const int warp0 = group * (tpr >> 5);
@@ -119,7 +124,7 @@ k_ln_forward(const __grid_constant__ LnArgs a)
         if ((c * tpr + t) * V < a.cols)
 #pragma unroll
             for (int k = 0; k < V; ++k) sum[0] += raw[c].value(k);
-    group_sum<1>(sum, group, tpr, room[0] + warp0);
+    group_sum<1>(sum, group, tpr, t >> 5, room[0] + warp0);
     const float mean = sum[0] * a.inv_cols;
     float sq[1] = {0.f};
 #pragma unroll
@@ -130,7 +135,7 @@ k_ln_forward(const __grid_constant__ LnArgs a)
                 const float d = raw[c].value(k) - mean;
                 sq[0] = fmaf(d, d, sq[0]);
             }
-    group_sum<1>(sq, group, tpr, room[1] + warp0);
+    group_sum<1>(sq, group, tpr, t >> 5, room[1] + warp0);
     const float rstd = __frsqrt_rn(fmaf(sq[0], a.inv_cols, a.eps));
     if (t == 0 && a.mean) {
         a.mean[row] = mean;
@@ -174,7 +179,7 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
         for (int k = 0; k < V; ++k) s += v.value(k);
         sum[0] += s;
     }
-    group_sum<1>(sum, 0, 1024, room[0]);
+    group_sum<1>(sum, 0, 1024, t >> 5, room[0]);
     const float mean = sum[0] * a.inv_cols;
     for (int col = t * V; col < a.cols; col += 1024 * V) {
         Vec<X, V> v;
@@ -187,7 +192,7 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
         }
         sq[0] += s;
     }
-    group_sum<1>(sq, 0, 1024, room[1]);
+    group_sum<1>(sq, 0, 1024, t >> 5, room[1]);
     const float rstd = __frsqrt_rn(fmaf(sq[0], a.inv_cols, a.eps));
     if (t == 0 && a.mean) {
         a.mean[row] = mean;
@@ -215,82 +220,194 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
 
 // ---- backward -----------------------------------------------------------------------------------
 
+// One access of `B` bytes (4, 8, 16 or 32) from global to shared memory, asynchronously.
+template <int B>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from)
+{
+    if constexpr (B >= 16) {
+#pragma unroll
+        for (int k = 0; k < B; k += 16)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + k), "l"(static_cast<const char*>(from) + k) : "memory");
+    } else {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(B) : "memory");
+    }
+}
+
+// What a thread has of the rows that are on their way.  Every thread copies, and later reads, its own columns
+// only, so nothing but its own copies has to be waited for.  bf16 that is not aligned to 4 bytes cannot be copied so:
+// there one row ahead is loaded into registers.
 template <typename X, typename G, int V, int C>
-struct RowPair {
+struct Ring {
+    static constexpr bool kAsync = V * sizeof(X) >= 4 && V * sizeof(G) >= 4;
+    static constexpr int  kX = V * static_cast<int>(sizeof(X)), kG = V * static_cast<int>(sizeof(G));
+    static constexpr int  kStage = C * (kX + kG);        // bytes per thread and stage
+
+    uint32_t base;
     Vec<X, V> x[C];
     Vec<G, V> dy[C];
-    float mean, rstd;
-    __device__ __forceinline__ void load(const LnArgs& a, long long row, int t)
+
+    // (accesses of a warp lie side by side: stage, then access, then thread)
+    __device__ __forceinline__ uint32_t x_at(int stage, int c) const { return base + stage * kStage * blockDim.x + (c * blockDim.x + threadIdx.x) * kX; }
+    __device__ __forceinline__ uint32_t g_at(int stage, int c) const { return base + (stage * kStage + C * kX) * blockDim.x + (c * blockDim.x + threadIdx.x) * kG; }
+
+    __device__ __forceinline__ void start(const LnArgs& a, long long row, int t, int stage)
     {
-        mean = a.mean[row];
-        rstd = a.rstd[row];
         const X* const px = static_cast<const X*>(a.x) + row * a.x_ld;
         const G* const pg = static_cast<const G*>(a.dy) + row * a.dy_ld;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int col = (c * a.tpr + t) * V;
-            if (col < a.cols) {
+            if (col >= a.cols) continue;
+            if constexpr (kAsync) {
+                copy_async<kX>(x_at(stage, c), px + col);
+                copy_async<kG>(g_at(stage, c), pg + col);
+            } else {
                 x[c].load(px + col);
                 dy[c].load(pg + col);
             }
         }
     }
+    template <int B, int W>
+    static __device__ __forceinline__ void read(uint32_t at, uint32_t (&w)[W])
+    {
+        if constexpr (B >= 16) {
+#pragma unroll
+            for (int k = 0; k < W; k += 4)
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "r"(at + 4 * k));
+        } else if constexpr (B == 8) {
+            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+        } else {
+            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+        }
+    }
+    __device__ __forceinline__ void take(int stage, int c, Vec<X, V>& vx, Vec<G, V>& vg) const
+    {
+        if constexpr (kAsync) {
+            read<kX>(x_at(stage, c), vx.w);
+            read<kG>(g_at(stage, c), vg.w);
+        } else {
+            vx = x[c];
+            vg = dy[c];
+        }
+    }
 };
 
-template <typename X, typename G, int V, int C>
-__global__ void __launch_bounds__(1024)
+template <int N>
+__device__ __forceinline__ void wait_all_but(int n)      // N at most: the youngest n of the copies committed may be on their way
+{
+    if constexpr (N > 0)
+        if (n < N) return wait_all_but<N - 1>(n);
+    asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory");
+}
+
+// C accesses of V elements per thread.  kHold: what the second half needs stays in registers; else it is read from the ring
+// (and the weight from memory) again.
+template <typename X, typename G, int V, int C, bool kHold>
+__global__ void __launch_bounds__(kBlockThreads, 1)
 k_ln_backward(const __grid_constant__ LnArgs a)
 {
-    extern __shared__ float sums[];      // the groups' sums at the end: [2][cols]
-    __shared__ float room[2][32][2];
-    const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x & (tpr - 1);
-    const int warp0 = group * (tpr >> 5);
+    using R = Ring<X, G, V, C>;
+    extern __shared__ __align__(16) char dynamic[];      // the ring; at the end the groups' sums: [2][cols]
+    __shared__ float room[2][kBlockThreads / 32][2];
+    release_dependents();
+    const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
+    const int warp0 = group * (tpr >> 5), stages = R::kAsync ? a.stages : 1;
     const long long step = static_cast<long long>(gridDim.x) * groups;
-    float w[C][V], dw[C][V], db[C][V];
+    float w[kHold ? C : 1][V], dw[C][V], db[C][V];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int col = (c * tpr + t) * V;
 #pragma unroll
-        for (int k = 0; k < V; ++k) w[c][k] = 1.f, dw[c][k] = db[c][k] = 0.f;
-        if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
+        for (int k = 0; k < V; ++k) dw[c][k] = db[c][k] = 0.f;
+        if constexpr (kHold) {
+#pragma unroll
+            for (int k = 0; k < V; ++k) w[c][k] = 1.f;
+            if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
+        }
     }
-    RowPair<X, G, V, C> next;
-    long long row = static_cast<long long>(blockIdx.x) * groups + group;
-    int turn = 0;
-    if (row < a.rows) next.load(a, row, t);
-    for (; row < a.rows; row += step, turn ^= 1) {
-        const RowPair<X, G, V, C> now = next;
-        if (row + step < a.rows) next.load(a, row + step, t);
+    R ring;
+    ring.base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
+    const long long first = static_cast<long long>(blockIdx.x) * groups + group;
+    // stages - 1 rows are on their way while one is computed
+    for (int k = 0; k < (R::kAsync ? stages - 1 : 1); ++k) {
+        if (first + k * step < a.rows) ring.start(a, first + k * step, t, k);
+        if constexpr (R::kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    float mean = 0.f, rstd = 0.f;
+    if (first < a.rows) mean = a.mean[first], rstd = a.rstd[first];
+    int stage = 0, turn = 0;
+    for (long long row = first; row < a.rows; row += step, turn ^= 1) {
+        float h[kHold ? C : 1][V], d[kHold ? C : 1][V];
         float s[2] = {0.f, 0.f};         // sums of d and of d h
+        const float now_mean = mean, now_rstd = rstd;
+        const int now = stage;
+        Vec<X, V> vx[R::kAsync ? 1 : C];
+        Vec<G, V> vg[R::kAsync ? 1 : C];
+        if constexpr (!R::kAsync) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-            if ((c * tpr + t) * V < a.cols)
+            for (int c = 0; c < C; ++c) vx[c] = ring.x[c], vg[c] = ring.dy[c];
+        } else {
+            wait_all_but<kMaxStages - 2>(stages - 2);
+        }
+        {
+            // the row after the ones on their way takes the place of the one before this (which has been read)
+            const long long ahead = row + (R::kAsync ? stages - 1 : 1) * step;
+            const int to = stage == 0 ? stages - 1 : stage - 1;
+            if (ahead < a.rows) ring.start(a, ahead, t, to);
+            if constexpr (R::kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+            if (row + step < a.rows) mean = a.mean[row + step], rstd = a.rstd[row + step];
+        }
+        stage = stage + 1 == stages ? 0 : stage + 1;
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    const float h = (now.x[c].value(k) - now.mean) * now.rstd, g = now.dy[c].value(k), d = g * w[c][k];
-                    dw[c][k] = fmaf(g, h, dw[c][k]);
-                    db[c][k] += g;
-                    s[0] += d;
-                    s[1] = fmaf(d, h, s[1]);
-                }
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * tpr + t) * V, at = kHold ? c : 0, from = R::kAsync ? 0 : c;
+            if (col >= a.cols) continue;
+            if constexpr (R::kAsync) ring.take(now, c, vx[0], vg[0]);
+            if constexpr (!kHold) {
+#pragma unroll
+                for (int k = 0; k < V; ++k) w[0][k] = 1.f;
+                if (a.w) load_param<V>(a.w, a.w_bf16, col, w[0]);
+            }
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float g = vg[from].value(k);
+                h[at][k] = (vx[from].value(k) - now_mean) * now_rstd;
+                d[at][k] = g * w[at][k];
+                dw[c][k] = fmaf(g, h[at][k], dw[c][k]);
+                db[c][k] += g;
+                s[0] += d[at][k];
+                s[1] = fmaf(d[at][k], h[at][k], s[1]);
+            }
+        }
         if (!a.y) continue;
-        group_sum<2>(s, group, tpr, room[turn] + warp0);
+        group_sum<2>(s, group, tpr, t >> 5, room[turn] + warp0);
         const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * tpr + t) * V;
+            const int col = (c * tpr + t) * V, at = kHold ? c : 0;
             if (col >= a.cols) continue;
             float o[V];
+            if constexpr (!kHold) {
+                ring.take(now, c, vx[0], vg[0]);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float h = (now.x[c].value(k) - now.mean) * now.rstd;
-                o[k] = now.rstd * (fmaf(now.dy[c].value(k), w[c][k], -c1) - h * c2);
+                for (int k = 0; k < V; ++k) w[0][k] = 1.f;
+                if (a.w) load_param<V>(a.w, a.w_bf16, col, w[0]);
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    h[0][k] = (vx[0].value(k) - now_mean) * now_rstd;
+                    d[0][k] = vg[0].value(k) * w[0][k];
+                }
             }
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[k] = now_rstd * fmaf(-h[at][k], c2, d[at][k] - c1);
             store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, o);
         }
     }
     if (!a.part) return;
     // the groups one after another, so that the order is theirs
+    if constexpr (R::kAsync) wait_all_but<0>(0);
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(dynamic);
     float* const part = a.part + 2ll * blockIdx.x * a.cols;
     for (int g = 0; g < groups; ++g) {
         const bool last = g == groups - 1;
@@ -340,7 +457,7 @@ k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
         s[0] += p;
         s[1] += q;
     }
-    group_sum<2>(s, 0, 1024, room[0]);
+    group_sum<2>(s, 0, 1024, threadIdx.x >> 5, room[0]);
     if (threadIdx.x == 0) out[row] = make_float2(s[0] * a.inv_cols, s[1] * a.inv_cols);
 }
 
@@ -423,13 +540,6 @@ k_ln_finish(const __grid_constant__ LnFinish f)
 
 // ---- host ---------------------------------------------------------------------------------------
 
-int round_up_power(long long x)
-{
-    int p = 1;
-    while (p < x) p <<= 1;
-    return p;
-}
-
 came_status validate_ln(const came_layernorm* l, bool backward)
 {
     if (!l) return report(CAME_ERR_NULL, "descriptor is NULL");
@@ -499,28 +609,38 @@ int access_of(const came_layernorm& l, bool backward)
     return 1;
 }
 
-struct BackwardPlan { int v, tpr, threads, blocks, column_blocks; bool is_long; size_t means, part, bytes; };
+struct BackwardPlan { int v, held, tpr, threads, stages, blocks, column_blocks; size_t smem, means, part, bytes; };
 
 BackwardPlan plan_backward(const came_layernorm& l)
 {
     BackwardPlan p = {};
     p.v = access_of(l, true);
-    p.is_long = l.cols > 1024 * kHeld;
-    const bool sums = l.dweight || l.dbias;
-    if (!p.is_long) {
-        p.tpr = std::max(32, round_up_power((l.cols + kHeld - 1) / kHeld));
-        p.threads = std::max(p.tpr, kBlockThreads);
-        const int groups = p.threads / p.tpr;
+    const size_t xb = dtype_bytes(l.x_dtype), gb = dtype_bytes(l.y_dtype);
+    const bool async = p.v * std::min(xb, gb) >= 4, sums = l.dweight || l.dbias;
+    // elements of a row per thread (0: the row does not fit a block)
+    if (!async) p.held = l.cols <= 8 * kBlockThreads ? 8 : 0;
+    else if (l.cols <= 8 * 32) p.held = 8;
+    else if (l.cols <= 16 * kBlockThreads) p.held = 16;
+    else if (p.v == 8 && l.cols <= 32 * kBlockThreads) p.held = 32;
+    if (p.held) {
+        p.tpr = static_cast<int>((l.cols + 32 * p.held - 1) / (32 * p.held)) * 32;
+        const int groups = std::max(1, kBlockThreads / p.tpr);
+        p.threads = groups * p.tpr;
+        const size_t stage = async ? p.held * (xb + gb) * p.threads : 0;
+        p.stages = async ? static_cast<int>(std::max<size_t>(2, std::min<size_t>(kMaxStages, kRingBytes / stage))) : 2;
+        p.smem = std::max(stage * p.stages, groups > 1 && sums ? sizeof(float) * 2 * l.cols : 0);
+        if (p.smem > kRingBytes) p.held = 0;
         const long long want = (l.rows + groups - 1) / groups;
-        p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, kSMs * (1024 / p.threads))));
-    } else {
+        p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, kSMs)));
+    }
+    if (!p.held) {
         p.column_blocks = static_cast<int>((l.cols + 32 * p.v - 1) / (32 * p.v));
         const long long want = (l.rows + 7) / 8;
         p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, std::max(1, kSMs * 8 / p.column_blocks))));
     }
     size_t at = 0;
     auto take = [&](size_t b) { const size_t here = at; at += (b + 255) / 256 * 256; return here; };
-    p.means = take(p.is_long && l.dx ? sizeof(float2) * l.rows : 0);
+    p.means = take(!p.held && l.dx ? sizeof(float2) * l.rows : 0);
     p.part = take(sums ? 8ull * p.blocks * l.cols : 0);
     p.bytes = std::max<size_t>(at, 256);
     return p;
@@ -539,8 +659,9 @@ void launch_forward(const LnArgs& a0, cudaStream_t stream)
     constexpr int kFew = 8 / V, kMany = kMost / V;
     const long long units = (a.cols + V - 1) / V;
     const bool few = a.rows <= 2 * kSMs && (units + kFew - 1) / kFew <= 1024;
-    a.tpr = std::max(32, round_up_power((units + (few ? kFew : kMany) - 1) / (few ? kFew : kMany)));
-    const int threads = std::max(a.tpr, few ? a.tpr : 256), groups = threads / a.tpr;
+    const int each = few ? kFew : kMany;
+    a.tpr = static_cast<int>((units + 32 * each - 1) / (32 * each)) * 32;
+    const int groups = few ? 1 : std::max(1, 256 / a.tpr), threads = groups * a.tpr;
     const unsigned blocks = static_cast<unsigned>((a.rows + groups - 1) / groups);
     if (units <= static_cast<long long>(a.tpr) * kFew) k_ln_forward<X, V, kFew><<<blocks, threads, 0, stream>>>(a);
     else k_ln_forward<X, V, kMany><<<blocks, threads, 0, stream>>>(a);
@@ -554,26 +675,39 @@ void launch_forward_v(const LnArgs& a, int v, cudaStream_t stream)
     else launch_forward<X, 1>(a, stream);
 }
 
-template <typename X, typename G, int V>
-cudaError_t launch_backward(LnArgs a, const BackwardPlan& p, float2* means, cudaStream_t stream)
+template <typename X, typename G, int V, int E>
+cudaError_t launch_held(LnArgs a, const BackwardPlan& p, int32_t device, cudaStream_t stream)
 {
-    if (p.is_long) {
-        if (a.y) k_ln_backward_rows<X, G, V><<<a.rows, 1024, 0, stream>>>(a, means);
-        k_ln_backward_columns<X, G, V><<<dim3(p.column_blocks, p.blocks), 256, 0, stream>>>(a, means);
-        return cudaGetLastError();
-    }
+    static std::atomic<uint64_t> done{0};
+    auto* const kernel = k_ln_backward<X, G, V, E / V, E != 32>;
+    const cudaError_t e = allow_smem(kernel, kRingBytes, device, done);
+    if (e != cudaSuccess) return e;
     a.tpr = p.tpr;
-    const size_t smem = p.threads > p.tpr && a.part ? sizeof(float) * 2 * a.cols : 0;      // (at most 2 * 4096 floats)
-    k_ln_backward<X, G, V, kHeld / V><<<p.blocks, p.threads, smem, stream>>>(a);
+    a.stages = p.stages;
+    kernel<<<p.blocks, p.threads, p.smem, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename X, typename G, int V>
+cudaError_t launch_backward(const LnArgs& a, const BackwardPlan& p, float2* means, int32_t device, cudaStream_t stream)
+{
+    constexpr bool kAsync = Ring<X, G, V, 1>::kAsync;
+    if (p.held == 8) return launch_held<X, G, V, 8>(a, p, device, stream);
+    if constexpr (kAsync)
+        if (p.held == 16) return launch_held<X, G, V, 16>(a, p, device, stream);
+    if constexpr (V == 8)
+        if (p.held == 32) return launch_held<X, G, V, 32>(a, p, device, stream);
+    if (a.y) k_ln_backward_rows<X, G, V><<<a.rows, 1024, 0, stream>>>(a, means);
+    k_ln_backward_columns<X, G, V><<<dim3(p.column_blocks, p.blocks), 256, 0, stream>>>(a, means);
     return cudaGetLastError();
 }
 
 template <typename X, typename G>
-cudaError_t launch_backward_v(const LnArgs& a, const BackwardPlan& p, float2* means, cudaStream_t stream)
+cudaError_t launch_backward_v(const LnArgs& a, const BackwardPlan& p, float2* means, int32_t device, cudaStream_t stream)
 {
-    if (p.v == 8) return launch_backward<X, G, 8>(a, p, means, stream);
-    if (p.v == 2) return launch_backward<X, G, 2>(a, p, means, stream);
-    return launch_backward<X, G, 1>(a, p, means, stream);
+    if (p.v == 8) return launch_backward<X, G, 8>(a, p, means, device, stream);
+    if (p.v == 2) return launch_backward<X, G, 2>(a, p, means, device, stream);
+    return launch_backward<X, G, 1>(a, p, means, device, stream);
 }
 
 LnArgs args_of(const came_layernorm& l, bool backward)
@@ -644,16 +778,25 @@ came_status came_layernorm_backward(const came_layernorm* l, void* workspace, in
     cudaError_t e = cudaSuccess;
     if (l->rows && (a.y || sums)) {
         if (l->x_dtype == CAME_BF16)
-            e = l->y_dtype == CAME_BF16 ? launch_backward_v<__nv_bfloat16, __nv_bfloat16>(a, p, means, stream)
-                                        : launch_backward_v<__nv_bfloat16, float>(a, p, means, stream);
+            e = l->y_dtype == CAME_BF16 ? launch_backward_v<__nv_bfloat16, __nv_bfloat16>(a, p, means, device, stream)
+                                        : launch_backward_v<__nv_bfloat16, float>(a, p, means, device, stream);
         else
-            e = l->y_dtype == CAME_BF16 ? launch_backward_v<float, __nv_bfloat16>(a, p, means, stream)
-                                        : launch_backward_v<float, float>(a, p, means, stream);
+            e = l->y_dtype == CAME_BF16 ? launch_backward_v<float, __nv_bfloat16>(a, p, means, device, stream)
+                                        : launch_backward_v<float, float>(a, p, means, device, stream);
     }
     if (e == cudaSuccess && sums && (l->rows || !(l->flags & CAME_LAYERNORM_ACCUMULATE))) {
         LnFinish f{a.part, l->dweight, l->dbias, l->rows ? p.blocks : 0, a.cols, a.w_bf16, (l->flags & CAME_LAYERNORM_ACCUMULATE) ? 1 : 0};
-        k_ln_finish<<<dim3(static_cast<unsigned>((l->cols + 31) / 32), 2), 1024, 0, stream>>>(f);
-        e = cudaGetLastError();
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>((l->cols + 31) / 32), 2);
+        cfg.blockDim = dim3(1024);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, k_ln_finish, f);
+        if (e == cudaSuccess) e = cudaGetLastError();
     }
     return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
 }
