@@ -556,6 +556,57 @@ came_status came_layernorm_workspace(const came_layernorm* l, int64_t* out_bytes
 came_status came_layernorm_backward(const came_layernorm* l, void* workspace, int64_t workspace_bytes,
                                     int32_t device, void* cuda_stream);
 
+/* ---- Learned relative position bias, and its gradient -------------------------------------------
+ *
+ * A table of learned numbers, one for each bucket of distances and attention head:
+ *   forward   out[h, i, j] = rn(table[bucket(j - i - offset), h])          i < q_len, j < k_len
+ *   backward  dtable[b, h] = rn([dtable[b, h] +] sum over n, i, j with bucket(j - i - offset) = b of dout[n, h, i, j])
+ *             the term in brackets with CAME_POSBIAS_ACCUMULATE
+ * offset is the position of query 0 among the keys.  With n buckets for a direction (CAME_POSBIAS_BIDIRECTIONAL: half
+ * of them for keys at or before the query, the other half, n further on, for keys behind it; else all of them, and keys
+ * behind the query count as distance 0), E = n / 2 (rounded down) and a distance d >= 0 of key and query,
+ *   bucket = d                                                              for d < E
+ *            min(n - 1, E + floor((n - E) log(d / E) / log(max_distance / E)))     else
+ * where a d at a border belongs above it (the borders are found once per call and compared in
+ * whole numbers).  Sums are formed in fp32, in an order that depends on the sizes alone:
+ * results are bit-reproducible.  What is written shares memory with nothing that is read (CAME_ERR_OVERLAP). */
+enum {
+    CAME_POSBIAS_BIDIRECTIONAL = 1u << 0,
+    CAME_POSBIAS_ACCUMULATE    = 1u << 1     /* backward: add to dtable */
+};
+
+typedef struct {
+    void*          table;     /* DEVICE table_dtype [buckets][table_ld]: read, or dtable          */
+    void*          data;      /* forward: DEVICE data_dtype [heads][q_len][k_len], written;
+                                 backward: dout, read: element (n, h, i, j) at n batch_stride +
+                                 h head_stride + i q_stride + j                                   */
+    const int64_t* device_offset;   /* DEVICE int64 [1], 8-byte aligned: the offset is read there by the
+                                 kernels (for captured decoding); NULL: `offset`                  */
+    int64_t        offset;    /* in [-2^40, 2^40] (what device_offset holds is clamped to that)   */
+    int64_t        q_len, k_len;    /* 0 .. 2^30                                                  */
+    int64_t        batch;     /* backward: 0 .. 2^20                                              */
+    int64_t        table_ld;  /* elements from bucket to bucket, heads .. 2^29                    */
+    int64_t        batch_stride, head_stride, q_stride;   /* backward: >= 0, elements             */
+    int32_t        heads;     /* 1 .. 65535                                                       */
+    int32_t        buckets;   /* 2 .. 1024; bidirectional: even, 4 .. 1024                        */
+    int32_t        max_distance;    /* > E (see above), up to 2^29                                */
+    int32_t        table_dtype, data_dtype;   /* came_dtype                                       */
+    uint32_t       flags;     /* CAME_POSBIAS_*                                                   */
+} came_posbias;
+
+/* Asynchronous on `cuda_stream`; allocate nothing; `device` must be current and hold every buffer.  Errors
+ * through came_last_error(NULL).  The backward pass needs `workspace` (DEVICE, 16-byte aligned, at least the
+ * bytes that came_posbias_workspace answers for the same descriptor; no CUDA call there); its contents need not be
+ * kept between calls, and calls that may run at the same time need one each. */
+came_status came_posbias_forward(const came_posbias* p, int32_t device, void* cuda_stream);
+came_status came_posbias_workspace(const came_posbias* p, int64_t* out_bytes);
+came_status came_posbias_backward(const came_posbias* p, void* workspace, int64_t workspace_bytes,
+                                  int32_t device, void* cuda_stream);
+
+/* Host-only: the bucket of the difference `relative` = key - query - offset, in *out (HOST), for the descriptor's
+ * buckets, max_distance and flags (its other members are not looked at). */
+came_status came_posbias_bucket(const came_posbias* p, int64_t relative, int32_t* out);
+
 /* Process-wide tuning knobs, read by later came_create calls (each knob is an atomic, so any
  * thread may set one; a context takes the values in force while it is being created, so set
  * them before the contexts they are meant for).  CAME_TUNE_TILE_ELEMS:

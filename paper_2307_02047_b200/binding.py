@@ -24,6 +24,7 @@ CAME_F32, CAME_BF16 = 0, 1
 CAME_I32, CAME_I64 = 0, 1
 CAME_EMBED_ACCUMULATE, CAME_EMBED_PADDING_ROW = 1, 2
 CAME_LAYERNORM_ACCUMULATE = 1
+CAME_POSBIAS_BIDIRECTIONAL, CAME_POSBIAS_ACCUMULATE = 1, 2
 CAME_T_NO_WEIGHT_DECAY = 1
 CAME_T_VEC_NO_CONFIDENCE = 2
 CAME_CREATE_KEEP_STATE = 1
@@ -56,7 +57,8 @@ EXPORTED = ["came_create", "came_step", "came_step_host", "came_destroy", "came_
             "came_clip_create", "came_clip_norm", "came_clip_grads", "came_clip_destroy",
             "came_embed_forward", "came_embed_workspace", "came_embed_backward",
             "came_adamw_create", "came_adamw_step", "came_adamw_destroy",
-            "came_layernorm_forward", "came_layernorm_workspace", "came_layernorm_backward"]
+            "came_layernorm_forward", "came_layernorm_workspace", "came_layernorm_backward",
+            "came_posbias_forward", "came_posbias_workspace", "came_posbias_backward", "came_posbias_bucket"]
 
 
 class CameError(RuntimeError):
@@ -118,6 +120,12 @@ class came_layernorm(ctypes.Structure):
                [(k, ctypes.c_int64) for k in ("rows", "cols", "x_ld", "y_ld", "dx_ld")] + [("eps", ctypes.c_double)] + \
                [(k, ctypes.c_int32) for k in ("x_dtype", "y_dtype", "dx_dtype", "weight_dtype")] + \
                [("flags", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class came_posbias(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_void_p) for k in ("table", "data", "device_offset")] + \
+               [(k, ctypes.c_int64) for k in ("offset", "q_len", "k_len", "batch", "table_ld", "batch_stride", "head_stride", "q_stride")] + \
+               [(k, ctypes.c_int32) for k in ("heads", "buckets", "max_distance", "table_dtype", "data_dtype")] + [("flags", ctypes.c_uint32)]
 
 
 _lib = None
@@ -235,8 +243,17 @@ def _bind(L):
     L.came_layernorm_workspace.restype = i32
     L.came_layernorm_backward.argtypes = [ctypes.POINTER(came_layernorm), vp, i64, i32, vp]
     L.came_layernorm_backward.restype = i32
+    L.came_posbias_forward.argtypes = [ctypes.POINTER(came_posbias), i32, vp]
+    L.came_posbias_forward.restype = i32
+    L.came_posbias_workspace.argtypes = [ctypes.POINTER(came_posbias), ctypes.POINTER(i64)]
+    L.came_posbias_workspace.restype = i32
+    L.came_posbias_backward.argtypes = [ctypes.POINTER(came_posbias), vp, i64, i32, vp]
+    L.came_posbias_backward.restype = i32
+    L.came_posbias_bucket.argtypes = [ctypes.POINTER(came_posbias), i64, ctypes.POINTER(i32)]
+    L.came_posbias_bucket.restype = i32
     # the same functions for descriptors that are packed bytes (a third of a structure's time to make)
-    for name in ("came_layernorm_forward", "came_layernorm_workspace", "came_layernorm_backward"):
+    for name in ("came_layernorm_forward", "came_layernorm_workspace", "came_layernorm_backward",
+                 "came_posbias_forward", "came_posbias_workspace", "came_posbias_backward"):
         packed, known = L[name], getattr(L, name)
         packed.argtypes, packed.restype = [ctypes.c_char_p, *known.argtypes[1:]], known.restype
         setattr(L, name + "_packed", packed)
@@ -475,6 +492,26 @@ def came_layernorm_backward(l: came_layernorm, workspace: int, workspace_bytes: 
     status = (_lib or load()).came_layernorm_backward(l, workspace, workspace_bytes, device, stream)
     if status:
         _check(status)
+
+
+def came_posbias_forward(p: came_posbias, device: int = 0, stream: int = 0) -> None:
+    _check(load().came_posbias_forward(p, device, stream))
+
+
+def came_posbias_workspace(p: came_posbias) -> int:
+    out = ctypes.c_int64()
+    _check(load().came_posbias_workspace(p, out))
+    return out.value
+
+
+def came_posbias_backward(p: came_posbias, workspace: int, workspace_bytes: int, device: int = 0, stream: int = 0) -> None:
+    _check(load().came_posbias_backward(p, workspace, workspace_bytes, device, stream))
+
+
+def came_posbias_bucket(p: came_posbias, relative: int) -> int:
+    out = ctypes.c_int32()
+    _check(load().came_posbias_bucket(p, relative, out))
+    return out.value
 
 
 def make_hparams(step: int, **kw) -> came_hparams:
@@ -1188,3 +1225,139 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out_dtype=None):
     if _torch().is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad)):
         return _layer_norm_function().apply(x, weight, bias, eps, out_dtype)
     return layer_norm_forward(x, weight, bias, eps, out_dtype=out_dtype, stats=False)
+
+
+# --- relative position bias ----------------------------------------------------------------------
+
+_pack_posbias = struct.Struct("3P8q5iI").pack
+_posbias_class = None
+
+
+def _posbias_forward_call(p, index, stream):
+    status = _lib.came_posbias_forward_packed(p, index, stream)
+    if status:
+        _check(status)
+
+
+def _posbias_backward_call(p, workspace, size, index, stream):
+    status = _lib.came_posbias_backward_packed(p, workspace, size, index, stream)
+    if status:
+        _check(status)
+
+
+def _offset_of(offset, index):
+    """(address of an offset on the device, offset on the host)."""
+    if isinstance(offset, int):
+        return 0, offset
+    torch = _torch()
+    if not isinstance(offset, torch.Tensor) or offset.dtype != torch.int64 or offset.numel() != 1:
+        raise CameError(CAME_ERR_DTYPE, "offset must be a whole number, or a CUDA tensor of one int64")
+    if offset.get_device() != index:
+        raise CameError(CAME_ERR_DEVICE, "offset must be on the table's GPU")
+    return offset.data_ptr(), 0
+
+
+def _position_bias_function():
+    """The bias as an autograd function."""
+    global _posbias_class
+    if _posbias_class is None:
+        torch = _torch()
+
+        class PositionBias(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, table, q_len, k_len, offset, bidirectional, max_distance, out_dtype):
+                # (an offset on the device is copied: the caller may have counted on when the gradient is computed)
+                ctx.offset = offset if isinstance(offset, int) else offset.clone()
+                ctx.bidirectional, ctx.max_distance, ctx.shape, ctx.dtype = bidirectional, max_distance, table.shape, table.dtype
+                return position_bias_forward(table, q_len, k_len, offset, bidirectional, max_distance, out_dtype=out_dtype)
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, grad_out):
+                if grad_out.stride(-1) != 1:
+                    grad_out = grad_out.contiguous()
+                grad = grad_out.new_empty(ctx.shape, dtype=ctx.dtype)
+                return (position_bias_backward(grad_out, grad, ctx.offset, ctx.bidirectional, ctx.max_distance),) + (None,) * 6
+
+        _posbias_class = PositionBias
+    return _posbias_class
+
+
+def position_bias_forward(table, q_len: int, k_len: int, offset=0, bidirectional: bool = True, max_distance: int = 128,
+                          out=None, out_dtype=None):
+    """``out[h, i, j] = table[bucket(j - i - offset), h]``, shape ``(heads, q_len, k_len)``: a number to add to the scores
+    of query i and key j (the buckets: see ``include/came_b200.h``).
+
+    ``table``: fp32 or bf16 CUDA matrix ``(buckets, heads)`` with contiguous rows.  ``offset``: the position of query 0 among
+    the keys, a whole number or a CUDA tensor of one int64 that the kernel reads (captured decoding).  ``bidirectional``: half
+    of the buckets for keys behind the query; else such keys count as distance 0.  ``out``: contiguous, fp32 or bf16,
+    made here (of type ``out_dtype``, the table's when that is None too) when it is None.
+
+    When autograd records and the table requires grad, the result carries the graph: the table's gradient is
+    ``position_bias_backward``'s, in its type (once differentiable).  ``out`` must be None then."""
+    if _lib is None:
+        load()
+    if table.requires_grad and _torch().is_grad_enabled():
+        if out is not None:
+            raise CameError(CAME_ERR_UNSUPPORTED, "a table that requires grad takes no out: detach it, or disable grad mode")
+        return _position_bias_function().apply(table, q_len, k_len, offset, bidirectional, max_distance, out_dtype)
+    buckets, heads, ld, code, index = _embed_table(table, "table")
+    offset_at, offset = _offset_of(offset, index)
+    if out is None:
+        if q_len < 0 or k_len < 0:
+            raise CameError(CAME_ERR_SHAPE, "q_len and k_len must be at least 0")
+        out = table.new_empty((heads, q_len, k_len), dtype=out_dtype)
+    else:
+        if out_dtype is not None and out.dtype != out_dtype:
+            raise CameError(CAME_ERR_DTYPE, f"out is {out.dtype}, not {out_dtype}")
+        if out.get_device() != index:
+            raise CameError(CAME_ERR_DEVICE, "out must be on the table's GPU")
+        if out.shape != (heads, q_len, k_len):
+            raise CameError(CAME_ERR_SHAPE, f"out must have the shape {(heads, q_len, k_len)}")
+        if not out.is_contiguous():
+            raise CameError(CAME_ERR_UNSUPPORTED, "out must be contiguous")
+    out_code = _DTYPE_CODES.get(out.dtype)
+    if out_code is None:
+        raise CameError(CAME_ERR_DTYPE, f"out must be fp32 or bf16, got {out.dtype}")
+    p = _pack_posbias(table.data_ptr(), out.data_ptr(), offset_at, offset, q_len, k_len, 0, ld, 0, 0, 0, heads, buckets,
+                      max_distance, code, out_code, CAME_POSBIAS_BIDIRECTIONAL if bidirectional else 0)
+    _call_on(index, _posbias_forward_call, p)
+    return out
+
+
+def position_bias_backward(grad_out, grad, offset=0, bidirectional: bool = True, max_distance: int = 128,
+                           accumulate: bool = False):
+    """``grad[b, h]`` = the sum of ``grad_out`` over all queries and keys (and the batch) of head h with bucket b; with
+    ``accumulate`` the sums are added to ``grad``.
+
+    ``grad_out``: fp32 or bf16, ``(heads, q_len, k_len)`` or ``(batch, heads, q_len, k_len)`` (a bias that was added to a
+    batch of scores), with any strides but a contiguous last dimension; ``grad``: fp32 or bf16 ``(buckets, heads)``.
+    Returns ``grad``.  Bit-reproducible."""
+    if _lib is None:
+        load()
+    buckets, heads, ld, code, index = _embed_table(grad, "grad")
+    offset_at, offset = _offset_of(offset, index)
+    if grad_out.get_device() != index:
+        raise CameError(CAME_ERR_DEVICE, "grad_out must be on the table's GPU")
+    data_code = _DTYPE_CODES.get(grad_out.dtype)
+    if data_code is None:
+        raise CameError(CAME_ERR_DTYPE, f"grad_out must be fp32 or bf16, got {grad_out.dtype}")
+    shape, strides = grad_out.shape, grad_out.stride()
+    if len(shape) == 3:
+        shape, strides = (1, *shape), (0, *strides)
+    if len(shape) != 4 or shape[1] != heads:
+        raise CameError(CAME_ERR_SHAPE, "grad_out must be (heads, q_len, k_len) or (batch, heads, q_len, k_len), with the heads of grad")
+    if strides[3] != 1 and shape[3] > 1:
+        raise CameError(CAME_ERR_UNSUPPORTED, "the last dimension of grad_out must be contiguous")
+    flags = (CAME_POSBIAS_BIDIRECTIONAL if bidirectional else 0) | (CAME_POSBIAS_ACCUMULATE if accumulate else 0)
+    p = _pack_posbias(grad.data_ptr(), grad_out.data_ptr(), offset_at, offset, shape[2], shape[3], shape[0], ld, *strides[:3], heads, buckets,
+                      max_distance, code, data_code, flags)
+    out = ctypes.c_int64()
+    status = _lib.came_posbias_workspace_packed(p, out)
+    if status:
+        _check(status)
+    size = out.value
+    # from torch's allocator, for the device's current stream: not reused before the call is done
+    ws = grad.new_empty((size + 3) // 4, dtype=_torch().float32)
+    _call_on(index, _posbias_backward_call, p, ws.data_ptr(), size)
+    return grad

@@ -6,7 +6,7 @@ import subprocess
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 SRCS = [os.path.join(_HERE, "csrc", s) for s in ("came_api.cu", "ops/came_clip.cu", "ops/came_embed.cu",
-                                                "ops/came_adamw.cu", "ops/came_layernorm.cu")]
+                                                "ops/came_adamw.cu", "ops/came_layernorm.cu", "ops/came_posbias.cu")]
 DEPS = SRCS + [os.path.join(_HERE, "csrc", h) for h in
                ("came_kernels.cuh", "came_pipelined.cuh", "came_stream.cuh", "ops/came_ops.cuh",
                 "ops/came_vec.cuh")] + \

@@ -20,6 +20,7 @@ constexpr int kSMs = 148;
 constexpr int kBlockThreads = 512;       // backward: threads of a block at most
 constexpr int kRingBytes = 200 << 10;    // backward: shared memory for rows on their way
 constexpr int kMaxStages = 6;
+constexpr long long kManyElements = 4ll << 20;      // forward: from here on groups go from row to row
 
 struct LnArgs {
     const void* x;
@@ -73,30 +74,84 @@ __device__ __forceinline__ void group_barrier(int group, int tpr)
     asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(tpr) : "memory");
 }
 
-// Sum over a group's threads, the same in all of them.  `room`: shared memory of the group, an entry per warp; a
-// caller that comes back before the group's next barrier takes another one.
-template <int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], int group, int tpr, int warp, float (*room)[N])
+// Two additions, products or multiply-adds at a time: half the instructions, each rounded as ever.
+__device__ __forceinline__ void add2(float& a, float& b, float x, float y)
 {
+    asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; add.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+__device__ __forceinline__ void mul2(float& a, float& b, float x, float y)
+{
+    asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mul.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
+}
+// (a, b) += (x, y) * (u, v)
+__device__ __forceinline__ void fma2(float& a, float& b, float x, float y, float u, float v)
+{
+    asm("{ .reg .b64 p, q, r; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mov.b64 r, {%4, %5}; fma.rn.f32x2 p, q, r, p; mov.b64 {%0, %1}, p; }"
+        : "+f"(a), "+f"(b) : "f"(x), "f"(y), "f"(u), "f"(v));
+}
+
+// The two sums v over a group's threads, the same in all of them.  The halves of a warp take one sum each after the first
+// exchange, so that two sums cost hardly more than one.  `room`: shared memory of the group, an entry per warp; a caller
+// that comes back before the group's next barrier takes another one.
+__device__ __forceinline__ void group_sum(float (&v)[2], int group, int tpr, int warp, float (*room)[2])
+{
+    const int lane = threadIdx.x & 31, half = lane >> 4, warps = tpr >> 5;
+    float mine = half ? v[1] : v[0];
+    mine += __shfl_xor_sync(0xffffffffu, half ? v[0] : v[1], 16);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int o = 8; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    if (warps > 1) {
+        if ((lane & 15) == 0) room[warp][half] = mine;
+        group_barrier(group, tpr);
+        mine = (lane & 15) < warps ? room[lane & 15][half] : 0.f;
+        if (warps > 16 && (lane & 15) + 16 < warps) mine += room[(lane & 15) + 16][half];
 #pragma unroll
-        for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
-    if (tpr == 32) return;
-    const int lane = threadIdx.x & 31, warps = tpr >> 5;
-    if (lane == 0)
+        for (int o = 8; o > 0; o >>= 1)
+            if (o < warps) mine += __shfl_xor_sync(0xffffffffu, mine, o);        // (lanes at `warps` and above hold zeros)
+    }
+    v[0] = __shfl_sync(0xffffffffu, mine, 0);
+    v[1] = __shfl_sync(0xffffffffu, mine, 16);
+}
+__device__ __forceinline__ float group_sum(float x, int group, int tpr, int warp, float (*room)[2])
+{
+    float v[2] = {x, 0.f};
+    group_sum(v, group, tpr, warp, room);
+    return v[0];
+}
+
+// One access of `B` bytes (4, 8, 16 or 32) from global to shared memory, asynchronously.
+template <int B>
+__device__ __forceinline__ void copy_async(uint32_t to, const void* from)
+{
+    if constexpr (B >= 16) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) room[warp][n] = v[n];
-    group_barrier(group, tpr);
+        for (int k = 0; k < B; k += 16)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + k), "l"(static_cast<const char*>(from) + k) : "memory");
+    } else {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(B) : "memory");
+    }
+}
+
+template <int B, int W>
+__device__ __forceinline__ void read_shared(uint32_t at, uint32_t (&w)[W])
+{
+    if constexpr (B >= 16) {
 #pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = lane < warps ? room[lane][n] : 0.f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
-        if (o < warps)                   // (the lanes at `warps` and above hold zeros)
-#pragma unroll
-            for (int n = 0; n < N; ++n) v[n] += __shfl_xor_sync(0xffffffffu, v[n], o);
-#pragma unroll
-    for (int n = 0; n < N; ++n) v[n] = __shfl_sync(0xffffffffu, v[n], 0);
+        for (int k = 0; k < W; k += 4)
+            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "r"(at + 4 * k));
+    } else if constexpr (B == 8) {
+        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    } else {
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void wait_all_but(int n)      // N at most: the youngest n of the copies committed may be on their way
+{
+    if constexpr (N > 0)
+        if (n < N) return wait_all_but<N - 1>(n);
+    asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory");
 }
 
 // ---- forward ------------------------------------------------------------------------------------
@@ -106,7 +161,7 @@ template <typename X, int V, int C>
 __global__ void __launch_bounds__(1024)
 k_ln_forward(const __grid_constant__ LnArgs a)
 {
-    __shared__ float room[2][32][1];     // 32 warps at most, of all groups together; one set for each sum
+    __shared__ float room[2][32][2];     // 32 warps at most, of all groups together; one set for each sum
     const int tpr = a.tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
     const int row = blockIdx.x * (blockDim.x / tpr) + group;
     if (row >= a.rows) return;           // (the whole group)
@@ -118,25 +173,24 @@ k_ln_forward(const __grid_constant__ LnArgs a)
         const int col = (c * tpr + t) * V;
         if (col < a.cols) raw[c].load(x + col);
     }
-    float sum[1] = {0.f};
+    float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if ((c * tpr + t) * V < a.cols)
 #pragma unroll
-            for (int k = 0; k < V; ++k) sum[0] += raw[c].value(k);
-    group_sum<1>(sum, group, tpr, t >> 5, room[0] + warp0);
-    const float mean = sum[0] * a.inv_cols;
-    float sq[1] = {0.f};
+            for (int k = 0; k < V; ++k) sum += raw[c].value(k);
+    const float mean = group_sum(sum, group, tpr, t >> 5, room[0] + warp0) * a.inv_cols;
+    float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
         if ((c * tpr + t) * V < a.cols)
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float d = raw[c].value(k) - mean;
-                sq[0] = fmaf(d, d, sq[0]);
+                sq = fmaf(d, d, sq);
             }
-    group_sum<1>(sq, group, tpr, t >> 5, room[1] + warp0);
-    const float rstd = __frsqrt_rn(fmaf(sq[0], a.inv_cols, a.eps));
+    sq = group_sum(sq, group, tpr, t >> 5, room[1] + warp0);
+    const float rstd = __frsqrt_rn(fmaf(sq, a.inv_cols, a.eps));
     if (t == 0 && a.mean) {
         a.mean[row] = mean;
         a.rstd[row] = rstd;
@@ -151,14 +205,130 @@ k_ln_forward(const __grid_constant__ LnArgs a)
         if (a.w) {
             load_param<V>(a.w, a.w_bf16, col, p);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] *= p[k];
+            for (int k = 0; k < V; ++k) y[k] = __fmul_rn(y[k], p[k]);
         }
         if (a.b) {
             load_param<V>(a.b, a.w_bf16, col, p);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] += p[k];
+            for (int k = 0; k < V; ++k) y[k] = __fadd_rn(y[k], p[k]);
         }
         store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, y);
+    }
+}
+
+// Many rows: a group goes from two rows to the next two.  They come through a ring in shared memory (as in the backward pass:
+// every thread copies and reads its own columns), the parameters stay in registers, and two rows share each barrier.
+template <typename X, int V, int C>
+__global__ void __launch_bounds__(kBlockThreads, 1)
+k_ln_forward_rows(const __grid_constant__ LnArgs a)
+{
+    constexpr int kX = V * static_cast<int>(sizeof(X));
+    static_assert(kX >= 4, "");
+    extern __shared__ __align__(16) char dynamic[];
+    __shared__ float room[2][kBlockThreads / 32][2];
+    const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
+    const int warp0 = group * (tpr >> 5), stages = a.stages;
+    const long long step = 2ll * gridDim.x * groups;
+    const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
+    auto place = [&](int stage, int r, int c) { return base + (((stage * 2 + r) * C + c) * blockDim.x + threadIdx.x) * kX; };
+    auto start = [&](long long row, int stage) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+            if (row + r < a.rows) {
+                const X* const x = static_cast<const X*>(a.x) + (row + r) * a.x_ld;
+#pragma unroll
+                for (int c = 0; c < C; ++c) {
+                    const int col = (c * tpr + t) * V;
+                    if (col < a.cols) copy_async<kX>(place(stage, r, c), x + col);
+                }
+            }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    const long long first = 2ll * (static_cast<long long>(blockIdx.x) * groups + group);
+    for (int k = 0; k < stages - 1; ++k) start(first + k * step, k);
+    float w[C][V], b[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = (c * tpr + t) * V;
+#pragma unroll
+        for (int k = 0; k < V; ++k) w[c][k] = 1.f, b[c][k] = 0.f;
+        if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
+        if (a.b && col < a.cols) load_param<V>(a.b, a.w_bf16, col, b[c]);
+    }
+    int stage = 0;
+    for (long long row = first; row < a.rows; row += step) {
+        wait_all_but<kMaxStages - 2>(stages - 2);
+        float x[2][C][V], sums[2][2] = {};
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                Vec<X, V> v;
+                if ((c * tpr + t) * V >= a.cols) continue;
+                read_shared<kX>(place(stage, r, c), v.w);       // (a second row that is not there: whatever the ring holds; not written)
+#pragma unroll
+                for (int k = 0; k < V; ++k) x[r][c][k] = v.value(k);
+                if constexpr (V == 1) sums[r][0] += x[r][c][0];
+                else
+#pragma unroll
+                    for (int k = 0; k < V; k += 2) add2(sums[r][0], sums[r][1], x[r][c][k], x[r][c][k + 1]);
+            }
+        float s[2] = {sums[0][0] + sums[0][1], sums[1][0] + sums[1][1]};
+        // two rows into the place of the two before these (which have been read)
+        start(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+        stage = stage + 1 == stages ? 0 : stage + 1;
+        group_sum(s, group, tpr, t >> 5, room[0] + warp0);
+        float squares[2][2] = {};
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            s[r] *= a.inv_cols;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if ((c * tpr + t) * V >= a.cols) continue;
+                if constexpr (V == 1) {
+                    x[r][c][0] -= s[r];
+                    squares[r][0] = fmaf(x[r][c][0], x[r][c][0], squares[r][0]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; k += 2) {
+                        add2(x[r][c][k], x[r][c][k + 1], -s[r], -s[r]);
+                        fma2(squares[r][0], squares[r][1], x[r][c][k], x[r][c][k + 1], x[r][c][k], x[r][c][k + 1]);
+                    }
+                }
+            }
+        }
+        float q[2] = {squares[0][0] + squares[0][1], squares[1][0] + squares[1][1]};
+        group_sum(q, group, tpr, t >> 5, room[1] + warp0);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            if (row + r >= a.rows) continue;
+            const float rstd = __frsqrt_rn(fmaf(q[r], a.inv_cols, a.eps));
+            if (t == 0 && a.mean) {
+                a.mean[row + r] = s[r];
+                a.rstd[row + r] = rstd;
+            }
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const int col = (c * tpr + t) * V;
+                if (col >= a.cols) continue;
+                float y[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) y[k] = x[r][c][k];
+                if constexpr (V == 1) {
+                    y[0] = fmaf(y[0] * rstd, w[c][0], b[c][0]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < V; k += 2) {
+                        float p = b[c][k], o = b[c][k + 1];
+                        mul2(y[k], y[k + 1], rstd, rstd);
+                        fma2(p, o, y[k], y[k + 1], w[c][k], w[c][k + 1]);
+                        y[k] = p;
+                        y[k + 1] = o;
+                    }
+                }
+                store_as<V>(a.y, a.y_bf16, (row + r) * a.y_ld + col, y);
+            }
+        }
     }
 }
 
@@ -167,20 +337,19 @@ template <typename X, int V>
 __global__ void __launch_bounds__(1024)
 k_ln_forward_long(const __grid_constant__ LnArgs a)
 {
-    __shared__ float room[2][32][1];
+    __shared__ float room[2][32][2];
     const int row = blockIdx.x, t = threadIdx.x;
     const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
-    float sum[1] = {0.f}, sq[1] = {0.f};
+    float sum = 0.f, sq = 0.f;
     for (int col = t * V; col < a.cols; col += 1024 * V) {
         Vec<X, V> v;
         v.load(x + col);
         float s = 0.f;
 #pragma unroll
         for (int k = 0; k < V; ++k) s += v.value(k);
-        sum[0] += s;
+        sum += s;
     }
-    group_sum<1>(sum, 0, 1024, t >> 5, room[0]);
-    const float mean = sum[0] * a.inv_cols;
+    const float mean = group_sum(sum, 0, 1024, t >> 5, room[0]) * a.inv_cols;
     for (int col = t * V; col < a.cols; col += 1024 * V) {
         Vec<X, V> v;
         v.load(x + col);
@@ -190,10 +359,10 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
             const float d = v.value(k) - mean;
             s = fmaf(d, d, s);
         }
-        sq[0] += s;
+        sq += s;
     }
-    group_sum<1>(sq, 0, 1024, t >> 5, room[1]);
-    const float rstd = __frsqrt_rn(fmaf(sq[0], a.inv_cols, a.eps));
+    sq = group_sum(sq, 0, 1024, t >> 5, room[1]);
+    const float rstd = __frsqrt_rn(fmaf(sq, a.inv_cols, a.eps));
     if (t == 0 && a.mean) {
         a.mean[row] = mean;
         a.rstd[row] = rstd;
@@ -207,31 +376,18 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
         if (a.w) {
             load_param<V>(a.w, a.w_bf16, col, p);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] *= p[k];
+            for (int k = 0; k < V; ++k) y[k] = __fmul_rn(y[k], p[k]);
         }
         if (a.b) {
             load_param<V>(a.b, a.w_bf16, col, p);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] += p[k];
+            for (int k = 0; k < V; ++k) y[k] = __fadd_rn(y[k], p[k]);
         }
         store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, y);
     }
 }
 
 // ---- backward -----------------------------------------------------------------------------------
-
-// One access of `B` bytes (4, 8, 16 or 32) from global to shared memory, asynchronously.
-template <int B>
-__device__ __forceinline__ void copy_async(uint32_t to, const void* from)
-{
-    if constexpr (B >= 16) {
-#pragma unroll
-        for (int k = 0; k < B; k += 16)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + k), "l"(static_cast<const char*>(from) + k) : "memory");
-    } else {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(B) : "memory");
-    }
-}
 
 // What a thread has of the rows that are on their way.  Every thread copies, and later reads, its own columns
 // only, so nothing but its own copies has to be waited for.  bf16 that is not aligned to 4 bytes cannot be copied so:
@@ -267,24 +423,11 @@ struct Ring {
             }
         }
     }
-    template <int B, int W>
-    static __device__ __forceinline__ void read(uint32_t at, uint32_t (&w)[W])
-    {
-        if constexpr (B >= 16) {
-#pragma unroll
-            for (int k = 0; k < W; k += 4)
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "r"(at + 4 * k));
-        } else if constexpr (B == 8) {
-            asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
-        } else {
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
-        }
-    }
     __device__ __forceinline__ void take(int stage, int c, Vec<X, V>& vx, Vec<G, V>& vg) const
     {
         if constexpr (kAsync) {
-            read<kX>(x_at(stage, c), vx.w);
-            read<kG>(g_at(stage, c), vg.w);
+            read_shared<kX>(x_at(stage, c), vx.w);
+            read_shared<kG>(g_at(stage, c), vg.w);
         } else {
             vx = x[c];
             vg = dy[c];
@@ -292,16 +435,8 @@ struct Ring {
     }
 };
 
-template <int N>
-__device__ __forceinline__ void wait_all_but(int n)      // N at most: the youngest n of the copies committed may be on their way
-{
-    if constexpr (N > 0)
-        if (n < N) return wait_all_but<N - 1>(n);
-    asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory");
-}
-
-// C accesses of V elements per thread.  kHold: what the second half needs stays in registers; else it is read from the ring
-// (and the weight from memory) again.
+// C accesses of V elements per thread.  kHold: the weight and what the second half needs stay in registers; else the ring
+// is read again, and the weight is kept in shared memory.
 template <typename X, typename G, int V, int C, bool kHold>
 __global__ void __launch_bounds__(kBlockThreads, 1)
 k_ln_backward(const __grid_constant__ LnArgs a)
@@ -327,6 +462,27 @@ k_ln_backward(const __grid_constant__ LnArgs a)
     }
     R ring;
     ring.base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
+    const uint32_t weights = ring.base;
+    auto weight_at = [&](int c, float (&x)[V]) {         // as fp32 in front of the ring, each thread its own columns
+        Vec<float, V> v;
+        read_shared<4 * V>(weights + (c * blockDim.x + threadIdx.x) * 4 * V, v.w);
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = v.value(k);
+    };
+    if constexpr (!kHold) {
+        ring.base += C * V * 4 * blockDim.x;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * tpr + t) * V;
+            float x[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) x[k] = 1.f;
+            if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, x);
+#pragma unroll
+            for (int k = 0; k < V; ++k) reinterpret_cast<float*>(dynamic)[(c * blockDim.x + threadIdx.x) * V + k] = x[k];
+        }
+        __syncthreads();
+    }
     const long long first = static_cast<long long>(blockIdx.x) * groups + group;
     // stages - 1 rows are on their way while one is computed
     for (int k = 0; k < (R::kAsync ? stages - 1 : 1); ++k) {
@@ -338,7 +494,7 @@ k_ln_backward(const __grid_constant__ LnArgs a)
     int stage = 0, turn = 0;
     for (long long row = first; row < a.rows; row += step, turn ^= 1) {
         float h[kHold ? C : 1][V], d[kHold ? C : 1][V];
-        float s[2] = {0.f, 0.f};         // sums of d and of d h
+        float ds[2] = {}, dh[2] = {};    // sums of d and of d h
         const float now_mean = mean, now_rstd = rstd;
         const int now = stage;
         Vec<X, V> vx[R::kAsync ? 1 : C];
@@ -363,24 +519,34 @@ k_ln_backward(const __grid_constant__ LnArgs a)
             const int col = (c * tpr + t) * V, at = kHold ? c : 0, from = R::kAsync ? 0 : c;
             if (col >= a.cols) continue;
             if constexpr (R::kAsync) ring.take(now, c, vx[0], vg[0]);
-            if constexpr (!kHold) {
+            if constexpr (!kHold) weight_at(c, w[0]);
+            if constexpr (V == 1) {
+                const float g = vg[from].value(0);
+                h[at][0] = (vx[from].value(0) - now_mean) * now_rstd;
+                d[at][0] = g * w[at][0];
+                dw[c][0] = fmaf(g, h[at][0], dw[c][0]);
+                db[c][0] += g;
+                ds[0] += d[at][0];
+                dh[0] = fmaf(d[at][0], h[at][0], dh[0]);
+            } else {
 #pragma unroll
-                for (int k = 0; k < V; ++k) w[0][k] = 1.f;
-                if (a.w) load_param<V>(a.w, a.w_bf16, col, w[0]);
-            }
-#pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float g = vg[from].value(k);
-                h[at][k] = (vx[from].value(k) - now_mean) * now_rstd;
-                d[at][k] = g * w[at][k];
-                dw[c][k] = fmaf(g, h[at][k], dw[c][k]);
-                db[c][k] += g;
-                s[0] += d[at][k];
-                s[1] = fmaf(d[at][k], h[at][k], s[1]);
+                for (int k = 0; k < V; k += 2) {
+                    const float g = vg[from].value(k), g1 = vg[from].value(k + 1);
+                    h[at][k] = vx[from].value(k), h[at][k + 1] = vx[from].value(k + 1);
+                    d[at][k] = g, d[at][k + 1] = g1;
+                    add2(h[at][k], h[at][k + 1], -now_mean, -now_mean);
+                    mul2(h[at][k], h[at][k + 1], now_rstd, now_rstd);
+                    mul2(d[at][k], d[at][k + 1], w[at][k], w[at][k + 1]);
+                    fma2(dw[c][k], dw[c][k + 1], g, g1, h[at][k], h[at][k + 1]);
+                    add2(db[c][k], db[c][k + 1], g, g1);
+                    add2(ds[0], ds[1], d[at][k], d[at][k + 1]);
+                    fma2(dh[0], dh[1], d[at][k], d[at][k + 1], h[at][k], h[at][k + 1]);
+                }
             }
         }
+        float s[2] = {ds[0] + ds[1], dh[0] + dh[1]};
         if (!a.y) continue;
-        group_sum<2>(s, group, tpr, t >> 5, room[turn] + warp0);
+        group_sum(s, group, tpr, t >> 5, room[turn] + warp0);
         const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
@@ -389,17 +555,24 @@ k_ln_backward(const __grid_constant__ LnArgs a)
             float o[V];
             if constexpr (!kHold) {
                 ring.take(now, c, vx[0], vg[0]);
-#pragma unroll
-                for (int k = 0; k < V; ++k) w[0][k] = 1.f;
-                if (a.w) load_param<V>(a.w, a.w_bf16, col, w[0]);
+                weight_at(c, w[0]);
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     h[0][k] = (vx[0].value(k) - now_mean) * now_rstd;
                     d[0][k] = vg[0].value(k) * w[0][k];
                 }
             }
+            if constexpr (V == 1) {
+                o[0] = now_rstd * fmaf(h[at][0], -c2, d[at][0] - c1);
+            } else {
 #pragma unroll
-            for (int k = 0; k < V; ++k) o[k] = now_rstd * fmaf(-h[at][k], c2, d[at][k] - c1);
+                for (int k = 0; k < V; k += 2) {
+                    o[k] = d[at][k], o[k + 1] = d[at][k + 1];
+                    add2(o[k], o[k + 1], -c1, -c1);
+                    fma2(o[k], o[k + 1], h[at][k], h[at][k + 1], -c2, -c2);
+                    mul2(o[k], o[k + 1], now_rstd, now_rstd);
+                }
+            }
             store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, o);
         }
     }
@@ -433,7 +606,7 @@ template <typename X, typename G, int V>
 __global__ void __launch_bounds__(1024)
 k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
 {
-    __shared__ float room[1][32][2];
+    __shared__ float room[32][2];
     const int row = blockIdx.x;
     const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
     const G* const dy = static_cast<const G*>(a.dy) + row * a.dy_ld;
@@ -457,7 +630,7 @@ k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
         s[0] += p;
         s[1] += q;
     }
-    group_sum<2>(s, 0, 1024, threadIdx.x >> 5, room[0]);
+    group_sum(s, 0, 1024, threadIdx.x >> 5, room);
     if (threadIdx.x == 0) out[row] = make_float2(s[0] * a.inv_cols, s[1] * a.inv_cols);
 }
 
@@ -609,6 +782,9 @@ int access_of(const came_layernorm& l, bool backward)
     return 1;
 }
 
+// Threads per row, in whole warps, where each holds `held` elements.
+int threads_per_row(long long cols, int held) { return static_cast<int>((cols + 32 * held - 1) / (32 * held)) * 32; }
+
 struct BackwardPlan { int v, held, tpr, threads, stages, blocks, column_blocks; size_t smem, means, part, bytes; };
 
 BackwardPlan plan_backward(const came_layernorm& l)
@@ -623,12 +799,13 @@ BackwardPlan plan_backward(const came_layernorm& l)
     else if (l.cols <= 16 * kBlockThreads) p.held = 16;
     else if (p.v == 8 && l.cols <= 32 * kBlockThreads) p.held = 32;
     if (p.held) {
-        p.tpr = static_cast<int>((l.cols + 32 * p.held - 1) / (32 * p.held)) * 32;
+        p.tpr = threads_per_row(l.cols, p.held);
         const int groups = std::max(1, kBlockThreads / p.tpr);
         p.threads = groups * p.tpr;
         const size_t stage = async ? p.held * (xb + gb) * p.threads : 0;
-        p.stages = async ? static_cast<int>(std::max<size_t>(2, std::min<size_t>(kMaxStages, kRingBytes / stage))) : 2;
-        p.smem = std::max(stage * p.stages, groups > 1 && sums ? sizeof(float) * 2 * l.cols : 0);
+        const size_t weights = p.held == 32 ? sizeof(float) * 32 * p.threads : 0;
+        p.stages = async ? static_cast<int>(std::max<size_t>(2, std::min<size_t>(kMaxStages, (kRingBytes - weights) / stage))) : 2;
+        p.smem = std::max(weights + stage * p.stages, groups > 1 && sums ? sizeof(float) * 2 * l.cols : 0);
         if (p.smem > kRingBytes) p.held = 0;
         const long long want = (l.rows + groups - 1) / groups;
         p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, kSMs)));
@@ -646,33 +823,52 @@ BackwardPlan plan_backward(const came_layernorm& l)
     return p;
 }
 
-template <typename X, int V>
-void launch_forward(const LnArgs& a0, cudaStream_t stream)
+template <typename X, int V, int E>
+cudaError_t launch_forward_rows(LnArgs a, int32_t device, cudaStream_t stream)
 {
-    LnArgs a = a0;
-    constexpr int kMost = 32;            // elements that a thread may hold
+    static std::atomic<uint64_t> done{0};
+    auto* const kernel = k_ln_forward_rows<X, V, E / V>;
+    const cudaError_t e = allow_smem(kernel, kRingBytes, device, done);
+    if (e != cudaSuccess) return e;
+    a.tpr = threads_per_row(a.cols, E);
+    const int groups = std::max(1, kBlockThreads / a.tpr), threads = groups * a.tpr;
+    const int stage = 2 * E * static_cast<int>(sizeof(X)) * threads;         // (64 KB at most)
+    a.stages = std::min(kMaxStages, kRingBytes / stage);
+    const long long want = (a.rows + 2 * groups - 1) / (2 * groups);
+    kernel<<<static_cast<unsigned>(std::min<long long>(want, kSMs)), threads, static_cast<size_t>(stage) * a.stages, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename X, int V>
+cudaError_t launch_forward(LnArgs a, int32_t device, cudaStream_t stream)
+{
+    constexpr int kMost = V == 8 ? 32 : 16;      // elements that a thread may hold
+    // (fp32 rows in wide accesses: a block per few rows is faster from 257 columns on, 612 against 735 us at 128k x 4096: fewer
+    // instructions for a byte, so that occupancy hides the latency)
+    if constexpr (V * sizeof(X) >= 4)
+        if (a.cols <= 16 * kBlockThreads && static_cast<long long>(a.rows) * a.cols >= kManyElements && (V * sizeof(X) < 32 || a.cols <= 8 * 32))
+            return a.cols <= 8 * 32 ? launch_forward_rows<X, V, 8>(a, device, stream) : launch_forward_rows<X, V, 16>(a, device, stream);
     if (a.cols > 1024 * kMost) {
         k_ln_forward_long<X, V><<<a.rows, 1024, 0, stream>>>(a);
-        return;
+        return cudaGetLastError();
     }
-    // Few rows: as many threads for each as there are accesses.  Many rows: more elements for a thread.
-    constexpr int kFew = 8 / V, kMany = kMost / V;
-    const long long units = (a.cols + V - 1) / V;
-    const bool few = a.rows <= 2 * kSMs && (units + kFew - 1) / kFew <= 1024;
-    const int each = few ? kFew : kMany;
-    a.tpr = static_cast<int>((units + 32 * each - 1) / (32 * each)) * 32;
+    // Few rows: as many threads for each as there are accesses.  More rows: more elements for a thread.
+    const bool few = a.rows <= 2 * kSMs && a.cols <= 8 * 1024;
+    const int each = few ? 8 : kMost;
+    a.tpr = threads_per_row(a.cols, each);
     const int groups = few ? 1 : std::max(1, 256 / a.tpr), threads = groups * a.tpr;
     const unsigned blocks = static_cast<unsigned>((a.rows + groups - 1) / groups);
-    if (units <= static_cast<long long>(a.tpr) * kFew) k_ln_forward<X, V, kFew><<<blocks, threads, 0, stream>>>(a);
-    else k_ln_forward<X, V, kMany><<<blocks, threads, 0, stream>>>(a);
+    if (a.cols <= a.tpr * 8) k_ln_forward<X, V, 8 / V><<<blocks, threads, 0, stream>>>(a);
+    else k_ln_forward<X, V, kMost / V><<<blocks, threads, 0, stream>>>(a);
+    return cudaGetLastError();
 }
 
 template <typename X>
-void launch_forward_v(const LnArgs& a, int v, cudaStream_t stream)
+cudaError_t launch_forward_v(const LnArgs& a, int v, int32_t device, cudaStream_t stream)
 {
-    if (v == 8) launch_forward<X, 8>(a, stream);
-    else if (v == 2) launch_forward<X, 2>(a, stream);
-    else launch_forward<X, 1>(a, stream);
+    if (v == 8) return launch_forward<X, 8>(a, device, stream);
+    if (v == 2) return launch_forward<X, 2>(a, device, stream);
+    return launch_forward<X, 1>(a, device, stream);
 }
 
 template <typename X, typename G, int V, int E>
@@ -745,9 +941,8 @@ came_status came_layernorm_forward(const came_layernorm* l, int32_t device, void
     const LnArgs a = args_of(*l, false);
     const int v = access_of(*l, false);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    if (l->x_dtype == CAME_BF16) launch_forward_v<__nv_bfloat16>(a, v, stream);
-    else                         launch_forward_v<float>(a, v, stream);
-    const cudaError_t e = cudaGetLastError();
+    const cudaError_t e = l->x_dtype == CAME_BF16 ? launch_forward_v<__nv_bfloat16>(a, v, device, stream)
+                                                  : launch_forward_v<float>(a, v, device, stream);
     return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
 }
 

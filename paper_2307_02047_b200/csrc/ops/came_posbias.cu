@@ -1,0 +1,506 @@
+// Learned relative position bias by buckets of distances, and its gradient.
+//
+//   out[h, i, j] = table[bucket(j - i - offset), h]
+//   dtable[b, h] = sum over (n, i, j) with that bucket of dout[n, h, i, j]
+//
+// Everything depends on j - i alone.  Forward: a block writes a tile of one head from a line of the tile's
+// diagonals in shared memory.  Backward: a warp adds up the diagonals of its tile in registers, going down the rows, and
+// the buckets, which are intervals of diagonals, at the end.
+#include "came_vec.cuh"
+
+#include <algorithm>
+#include <cmath>
+
+namespace {
+
+using namespace came_ops;
+
+constexpr int kMostBuckets = 1024;
+constexpr int kSMs = 148;
+constexpr int kTileColumns = 256;        // backward: columns of a warp's tile, eight per lane
+constexpr int kWarps = 8;
+constexpr long long kFar = 1ll << 40;
+
+// Distances of one direction: bucket m begins at start[m].
+template <int M>
+struct Buckets {
+    int n;                               // buckets of a direction, M at most
+    int both;
+    int start[M];
+};
+constexpr int kFewBuckets = 64;          // (the tables travel with the launch)
+
+struct BiasArgs {
+    void*          table;
+    void*          data;
+    const int64_t* device_offset;
+    long long      offset;
+    long long      q, k, batch, table_ld, batch_stride, head_stride, q_stride;
+    int            heads, buckets, table_bf16;
+    int            tile_rows, tile_vectors;          // forward
+    int            row_tiles, column_tiles, batches; // backward: tiles of a head, batches per warp
+    int            batch_groups;
+    float*         part;                 // backward: [heads][units][buckets]
+};
+
+__device__ __forceinline__ long long offset_of(const BiasArgs& a)
+{
+    if (!a.device_offset) return a.offset;
+    return max(-kFar, min(kFar, static_cast<long long>(*a.device_offset)));
+}
+
+// Bucket, within its direction, of a distance: the last m with start[m] <= d.
+__device__ __forceinline__ int bucket_of(const int* start, int n, long long d)
+{
+    int lo = 0, hi = n;                  // start[lo] <= d < start[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= d) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+__host__ __device__ __forceinline__ long long distance_of(long long relative, int both)
+{
+    return relative > 0 ? (both ? relative : 0) : -relative;
+}
+
+// ---- forward ------------------------------------------------------------------------------------
+
+// A tile: tile_rows rows and tile_vectors accesses of 16 bytes in each, aligned in memory: row i's accesses begin at its
+// first aligned column, wherever that is.  The line of the tile's diagonals is kept once for every alignment
+// of a group of N values, so that each access is one load from shared memory and one store.
+template <typename T, int M>
+__global__ void __launch_bounds__(256)
+k_posbias_forward(const __grid_constant__ BiasArgs a, const __grid_constant__ Buckets<M> buckets)
+{
+    constexpr int N = 16 / static_cast<int>(sizeof(T));
+    extern __shared__ __align__(16) char dynamic[];
+    __shared__ int start[M];
+    T* const line = reinterpret_cast<T*>(dynamic);
+    const int tr = a.tile_rows, tv = a.tile_vectors, length = (tr + N * tv + N + N - 1) / N * N;
+    const int h = blockIdx.z;
+    const long long i0 = static_cast<long long>(blockIdx.y) * tr, v0 = static_cast<long long>(blockIdx.x) * tv;
+    for (int m = threadIdx.x; m < buckets.n; m += 256) start[m] = buckets.start[m];
+    __syncthreads();
+    // line[x]: the diagonal of column N v0 + x - (tr - 1) in row i0
+    const long long origin = N * v0 - (tr - 1) - i0 - offset_of(a);
+    for (int x = threadIdx.x; x < length; x += 256) {
+        const long long relative = origin + x;
+        const int b = bucket_of(start, buckets.n, distance_of(relative, buckets.both)) + (buckets.both && relative > 0 ? buckets.n : 0);
+        const long long at = b * a.table_ld + h;
+        const float value = a.table_bf16 ? to_float(static_cast<const __nv_bfloat16*>(a.table)[at]) : static_cast<const float*>(a.table)[at];
+        const T t = from_float<T>(value);
+#pragma unroll
+        for (int s = 0; s < N; ++s)
+            if (x >= s) line[s * length + x - s] = t;
+    }
+    __syncthreads();
+    T* const out = static_cast<T*>(a.data) + h * a.q * a.k;
+    const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(out) / sizeof(T)) % N);
+    const int rows_at_once = 256 / tv, v = threadIdx.x % tv;
+    const long long vector = v0 + v;
+    for (int r = threadIdx.x / tv; r < tr && i0 + r < a.q; r += rows_at_once) {
+        const long long i = i0 + r;
+        const int ahead = static_cast<int>((N - (skew + i * a.k) % N) % N);      // elements before the row's first aligned one
+        const long long have = (a.k - ahead) >= 0 ? (a.k - ahead) / N : -1;
+        T* const row = out + i * a.k;
+        const int x = ahead + N * v + (tr - 1) - r;
+        if (vector < have) {
+            const uint4 w = *reinterpret_cast<const uint4*>(line + (x % N) * length + x / N * N);
+            *reinterpret_cast<uint4*>(row + ahead + N * vector) = w;
+        } else if (vector == have) {
+            for (int e = 0; e < N && ahead + N * vector + e < a.k; ++e) row[ahead + N * vector + e] = line[x + e];
+        }
+        if (vector == 0)
+            for (int e = 0; e < ahead && e < a.k; ++e) row[e] = line[e + (tr - 1) - r];
+    }
+}
+
+// ---- backward -----------------------------------------------------------------------------------
+
+__device__ __forceinline__ void add_value(float& sum, const Vec<float, 8>& v, int k) { sum += v.value(k); }
+__device__ __forceinline__ void add_value(float& sum, const Vec<__nv_bfloat16, 8>& v, int k)
+{
+    const uint16_t h = static_cast<uint16_t>(k & 1 ? v.w[k >> 1] >> 16 : v.w[k >> 1] & 0xffffu);
+    asm("add.rn.f32.bf16 %0, %1, %0;" : "+f"(sum) : "h"(h));
+}
+
+// Eight columns of a row, of which `left` are there; V elements per access.
+template <typename T, int V>
+__device__ __forceinline__ void load_row(Vec<T, 8>& to, const T* p, long long left)
+{
+    if constexpr (V == 8) {
+        if (left >= 8) to.load(p);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; k += V) {
+            Vec<T, V> v;
+#pragma unroll
+            for (int j = 0; j < Vec<T, V>::W; ++j) v.w[j] = 0u;
+            if (k < left) v.load(p + k);
+            if constexpr (V * sizeof(T) >= 4) {
+#pragma unroll
+                for (int j = 0; j < Vec<T, V>::W; ++j) to.w[k * sizeof(T) / 4 + j] = v.w[j];
+            } else {
+                if (k & 1) to.w[k >> 1] |= v.w[0] << 16;
+                else to.w[k >> 1] = v.w[0];
+            }
+        }
+    }
+}
+
+// One warp: tile_rows rows (a multiple of 8) and 256 columns of a head, `batches` of the batch.  In a group of eight rows a lane's eight
+// columns meet fifteen diagonals; eight of these are complete for the lane when the group is done and go to the warp's line in
+// shared memory, the others are the next group's upper ones.  Lanes and groups that meet the same diagonal follow one
+// another in the warp's order, so the sums' order is fixed.
+template <typename T, int V, int M>
+__global__ void __launch_bounds__(kWarps * 32)
+k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ Buckets<M> buckets)
+{
+    extern __shared__ __align__(16) char dynamic[];
+    __shared__ int start[M];
+    release_dependents();
+    for (int m = threadIdx.x; m < buckets.n; m += kWarps * 32) start[m] = buckets.start[m];
+    __syncthreads();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tr = a.tile_rows, length = tr + kTileColumns;
+    const long long units = static_cast<long long>(a.row_tiles) * a.column_tiles * a.batch_groups;
+    const long long unit = static_cast<long long>(blockIdx.x) * kWarps + warp;
+    const int h = blockIdx.y;
+    if (unit >= units) return;
+    float* const line = reinterpret_cast<float*>(dynamic) + warp * length;       // line[x]: the diagonal column - row = x - tr
+    for (int x = lane; x < length; x += 32) line[x] = 0.f;
+    __syncwarp();
+    const long long tile = unit / a.batch_groups;
+    const long long i0 = tile / a.column_tiles * tr, j0 = tile % a.column_tiles * kTileColumns;
+    const long long n0 = unit % a.batch_groups * a.batches, n1 = min(a.batch, n0 + a.batches);
+    const int rows = static_cast<int>(min(static_cast<long long>(tr), a.q - i0));
+    const long long left = a.k - j0 - 8 * lane;
+    auto flush = [&](const float* sums, int base) {      // eight diagonals of every lane, side by side
+        float4* const to = reinterpret_cast<float4*>(line + base + 8 * lane);
+        float4 x = to[0], y = to[1];
+        x.x += sums[0], x.y += sums[1], x.z += sums[2], x.w += sums[3];
+        y.x += sums[4], y.y += sums[5], y.z += sums[6], y.w += sums[7];
+        to[0] = x, to[1] = y;
+        __syncwarp();
+    };
+    for (long long n = n0; n < n1; ++n) {
+        const T* p = static_cast<const T*>(a.data) + n * a.batch_stride + h * a.head_stride + i0 * a.q_stride + j0 + 8 * lane;
+        float sums[15];                  // sums[d + 7]: the diagonal d = column - row within the group
+#pragma unroll
+        for (int d = 0; d < 15; ++d) sums[d] = 0.f;
+        int base = tr;
+        for (int r = 0; r < rows; r += 8, base -= 8) {
+            Vec<T, 8> v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+#pragma unroll
+                for (int j = 0; j < Vec<T, 8>::W; ++j) v[u].w[j] = 0u;
+                if (r + u < rows && left > 0) load_row<T, V>(v[u], p + u * a.q_stride, left);
+            }
+            p += 8 * a.q_stride;
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) add_value(sums[k - u + 7], v[u], k);
+            flush(sums + 7, base);
+#pragma unroll
+            for (int d = 14; d >= 8; --d) sums[d] = sums[d - 8];
+#pragma unroll
+            for (int d = 0; d < 8; ++d) sums[d] = 0.f;
+        }
+        flush(sums + 7, base);           // (sums[7] is zero: its place belongs to the group before)
+    }
+    // Buckets, in the order of their diagonals: -(n - 1) .. 0 before the query, 1 .. n - 1 behind it.
+    const long long origin = j0 - i0 - offset_of(a) - tr;        // line[x] has key - query - offset = origin + x
+    float* const part = a.part + (h * units + unit) * a.buckets;
+    for (int b = lane; b < a.buckets; b += 32) part[b] = 0.f;
+    __syncwarp();
+    auto order = [&](long long relative) {
+        const int b = bucket_of(start, buckets.n, distance_of(relative, buckets.both));
+        return relative > 0 && buckets.both ? b : -b;
+    };
+    const int first = order(origin), last = order(origin + length - 1);
+    for (int o = first; o <= last; ++o) {
+        const int m = o < 0 ? -o : o;
+        const bool end = m == buckets.n - 1;
+        long long lo, hi;                // the bucket's interval of relative positions
+        if (o > 0) {
+            lo = start[m];
+            hi = end ? 2 * kFar + length : start[m + 1];
+        } else {
+            lo = end ? -2 * kFar - length : 1 - static_cast<long long>(start[m + 1]);
+            hi = 1 - static_cast<long long>(start[m]);
+            if (o == 0) hi = buckets.both ? 1 : 2 * kFar + length;
+        }
+        const int x0 = static_cast<int>(max(0ll, min(static_cast<long long>(length), lo - origin)));
+        const int x1 = static_cast<int>(max(0ll, min(static_cast<long long>(length), hi - origin)));
+        float s = 0.f;
+        for (int x = x0 + lane; x < x1; x += 32) s += line[x];
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+        if (lane == 0) part[o > 0 ? buckets.n + m : m] = s;
+    }
+}
+
+// Adds a head's units: 32 buckets for each block, 32 warps that take every 32nd unit.
+__global__ void __launch_bounds__(1024)
+k_posbias_finish(const __grid_constant__ BiasArgs a, long long units, int accumulate)
+{
+    __shared__ float s[32][33];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = blockIdx.x * 32 + lane, h = blockIdx.y;
+    wait_for_previous_grid();
+    float v = 0.f;
+    if (b < a.buckets)
+        for (long long u = warp; u < units; u += 32) v += a.part[(h * units + u) * a.buckets + b];
+    s[warp][lane] = v;
+    __syncthreads();
+    if (warp != 0 || b >= a.buckets) return;
+    float t = 0.f;
+    for (int g = 0; g < 32; ++g) t += s[g][lane];
+    const long long at = b * a.table_ld + h;
+    if (a.table_bf16) {
+        __nv_bfloat16* const o = static_cast<__nv_bfloat16*>(a.table) + at;
+        *o = __float2bfloat16_rn(accumulate ? to_float(*o) + t : t);
+    } else {
+        float* const o = static_cast<float*>(a.table) + at;
+        *o = accumulate ? *o + t : t;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+
+came_status validate_buckets(const came_posbias& p)
+{
+    const bool both = p.flags & CAME_POSBIAS_BIDIRECTIONAL;
+    if (p.buckets < (both ? 4 : 2) || p.buckets > kMostBuckets || (both && p.buckets % 2))
+        return report(CAME_ERR_SHAPE, "buckets must lie in [2, 1024], bidirectional: be even and at least 4");
+    const int n = both ? p.buckets / 2 : p.buckets;
+    if (p.max_distance <= n / 2 || p.max_distance > (1 << 29))
+        return report(CAME_ERR_HPARAM, "max_distance must lie above the distances that have a bucket each, up to 2^29");
+    return CAME_OK;
+}
+
+template <int M>
+void fill_buckets(const came_posbias& p, Buckets<M>& b)
+{
+    b.both = (p.flags & CAME_POSBIAS_BIDIRECTIONAL) ? 1 : 0;
+    b.n = b.both ? p.buckets / 2 : p.buckets;
+    const int e = b.n / 2, steps = b.n - e;
+    for (int m = 0; m < b.n; ++m) {
+        if (m <= e) { b.start[m] = m; continue; }
+        // the smallest d with E (max_distance / E)^((m - E) / steps) <= d; what is this near to a whole number is one
+        const double border = e * std::pow(static_cast<double>(p.max_distance) / e, static_cast<double>(m - e) / steps);
+        const double whole = std::nearbyint(border);
+        b.start[m] = static_cast<int>(std::fabs(border - whole) <= 1e-13 * border ? whole : std::ceil(border));
+    }
+}
+
+came_status validate_posbias(const came_posbias* p, bool backward)
+{
+    if (!p) return report(CAME_ERR_NULL, "descriptor is NULL");
+    if (p->q_len < 0 || p->q_len > (1ll << 30) || p->k_len < 0 || p->k_len > (1ll << 30) || p->heads < 1 || p->heads > 65535)
+        return report(CAME_ERR_SHAPE, "q_len and k_len must lie in [0, 2^30], heads in [1, 65535]");
+    if (p->flags & ~static_cast<uint32_t>(CAME_POSBIAS_BIDIRECTIONAL | CAME_POSBIAS_ACCUMULATE)) return report(CAME_ERR_UNSUPPORTED, "unknown flag");
+    if ((p->flags & CAME_POSBIAS_ACCUMULATE) && !backward) return report(CAME_ERR_UNSUPPORTED, "accumulation applies to the backward pass only");
+    const came_status s = validate_buckets(*p);
+    if (s != CAME_OK) return s;
+    if (p->offset < -kFar || p->offset > kFar) return report(CAME_ERR_SHAPE, "offset must lie in [-2^40, 2^40]");
+    if (p->table_ld < p->heads || p->table_ld > (1ll << 29)) return report(CAME_ERR_SHAPE, "table_ld must lie in [heads, 2^29]");
+    if (!known_dtype(p->table_dtype) || !known_dtype(p->data_dtype)) return report(CAME_ERR_DTYPE, "unknown dtype");
+    const double most = static_cast<double>(1ll << 40);
+    if (static_cast<double>(p->heads) * p->q_len * p->k_len > most) return report(CAME_ERR_SHAPE, "more than 2^40 elements");
+    if (backward) {
+        if (p->batch < 0 || p->batch > (1 << 20)) return report(CAME_ERR_SHAPE, "batch must lie in [0, 2^20]");
+        if (p->batch_stride < 0 || p->head_stride < 0 || p->q_stride < 0 ||
+            static_cast<double>(p->batch) * p->batch_stride > most || static_cast<double>(p->heads) * p->head_stride > most ||
+            static_cast<double>(p->q_len) * p->q_stride > most)
+            return report(CAME_ERR_SHAPE, "a stride is negative, or too large");
+    }
+    const bool empty = !p->q_len || !p->k_len || (backward && !p->batch);
+    if (!p->table || (!empty && !p->data)) return report(CAME_ERR_NULL, "table and data are required");
+    if (!aligned_to(p->table, dtype_bytes(p->table_dtype)) || !aligned_to(p->data, dtype_bytes(p->data_dtype)) || !aligned_to(p->device_offset, 8))
+        return report(CAME_ERR_ALIGN, "a pointer is not aligned to its element size");
+    struct Range { uintptr_t lo, hi; };
+    auto range = [](const void* q, unsigned long long n) { return Range{reinterpret_cast<uintptr_t>(q), reinterpret_cast<uintptr_t>(q) + n}; };
+    auto meet = [](const Range& x, const Range& y) { return x.lo < y.hi && y.lo < x.hi; };
+    const unsigned long long last = backward ? (p->batch - 1) * p->batch_stride + (p->heads - 1) * p->head_stride + (p->q_len - 1) * p->q_stride + p->k_len
+                                             : static_cast<unsigned long long>(p->heads) * p->q_len * p->k_len;
+    const Range table = range(p->table, ((p->buckets - 1) * p->table_ld + p->heads) * dtype_bytes(p->table_dtype));
+    const Range data = range(p->data, empty ? 0 : last * dtype_bytes(p->data_dtype));
+    const Range offset = range(p->device_offset, p->device_offset ? 8 : 0);
+    if ((!empty && meet(table, data)) || meet(offset, backward ? table : data)) return report(CAME_ERR_OVERLAP, "the output shares memory with an input");
+    return CAME_OK;
+}
+
+struct BackwardPlan { int tile_rows, row_tiles, column_tiles, batches, batch_groups, v; long long units, bytes; };
+
+// Rows of a tile, and batches for a warp: as large as leaves every SM about 32 warps, so that a diagonal's sums stay in
+// registers and shared memory for long.
+BackwardPlan plan_backward(const came_posbias& p)
+{
+    BackwardPlan b = {};
+    b.v = 1;
+    for (int v : {8, 2}) {
+        const bool fits = p.k_len % v == 0 && (p.q_len <= 1 || p.q_stride % v == 0) && (p.heads == 1 || p.head_stride % v == 0) &&
+                          (p.batch <= 1 || p.batch_stride % v == 0) && aligned_to(p.data, v * dtype_bytes(p.data_dtype));
+        if (fits) { b.v = v; break; }
+    }
+    const long long want = kSMs * 32;
+    const long long columns = std::max<int64_t>(1, (p.k_len + kTileColumns - 1) / kTileColumns);
+    b.tile_rows = 128;
+    auto tiles = [&] { return columns * std::max<int64_t>(1, (p.q_len + b.tile_rows - 1) / b.tile_rows) * p.heads; };
+    while (b.tile_rows > 16 && tiles() * std::max<int64_t>(1, p.batch) < want) b.tile_rows /= 2;
+    b.column_tiles = static_cast<int>(columns);
+    b.row_tiles = static_cast<int>(std::max<int64_t>(1, (p.q_len + b.tile_rows - 1) / b.tile_rows));
+    const long long batch = std::max<int64_t>(1, p.batch);
+    const long long groups = std::min(batch, std::max(1ll, want / tiles()));
+    b.batches = static_cast<int>((batch + groups - 1) / groups);
+    b.batch_groups = static_cast<int>((batch + b.batches - 1) / b.batches);
+    b.units = static_cast<long long>(b.row_tiles) * b.column_tiles * b.batch_groups;
+    b.bytes = b.units * p.heads * p.buckets * 4;
+    return b;
+}
+
+BiasArgs args_of(const came_posbias& p)
+{
+    BiasArgs a = {};
+    a.table = p.table;
+    a.data = p.data;
+    a.device_offset = p.device_offset;
+    a.offset = p.offset;
+    a.q = p.q_len;
+    a.k = p.k_len;
+    a.batch = p.batch;
+    a.table_ld = p.table_ld;
+    a.batch_stride = p.batch_stride;
+    a.head_stride = p.head_stride;
+    a.q_stride = p.q_stride;
+    a.heads = p.heads;
+    a.buckets = p.buckets;
+    a.table_bf16 = p.table_dtype == CAME_BF16;
+    return a;
+}
+
+template <typename T, int M>
+came_status launch_forward(const came_posbias& p, cudaStream_t stream)
+{
+    constexpr int N = 16 / sizeof(T);
+    BiasArgs a = args_of(p);
+    Buckets<M> b;
+    fill_buckets(p, b);
+    const long long vectors = p.k_len / N + 1;           // (the last one, or the only one, may be part of one)
+    // Tiles of 64 rows; of few rows and a quarter of the columns where that leaves SMs without a block.
+    a.tile_vectors = 128;
+    a.tile_rows = static_cast<int>(std::min<int64_t>(64, p.q_len));
+    auto blocks = [&] { return (vectors + a.tile_vectors - 1) / a.tile_vectors * ((p.q_len + a.tile_rows - 1) / a.tile_rows) * p.heads; };
+    if (blocks() < 2 * kSMs) a.tile_vectors = 32;
+    while (a.tile_rows > 8 && blocks() < 2 * kSMs) a.tile_rows /= 2;
+    const long long x = (vectors + a.tile_vectors - 1) / a.tile_vectors, y = (p.q_len + a.tile_rows - 1) / a.tile_rows;
+    if (x > 0x7fffffffll || y > 65535) {
+        // (2^30 rows of 64 do not fit a grid's second dimension)
+        return report(CAME_ERR_SHAPE, "q_len is beyond 65535 tiles of 64 rows: call for parts of it");
+    }
+    const size_t length = (a.tile_rows + N * a.tile_vectors + N + N - 1) / N * N;
+    k_posbias_forward<T, M><<<dim3(static_cast<unsigned>(x), static_cast<unsigned>(y), p.heads), 256, length * 16, stream>>>(a, b);
+    const cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
+}
+
+template <typename T, int M>
+cudaError_t launch_backward(const BiasArgs& a, const came_posbias& d, const BackwardPlan& p, cudaStream_t stream)
+{
+    Buckets<M> b;
+    fill_buckets(d, b);
+    const dim3 grid(static_cast<unsigned>((p.units + kWarps - 1) / kWarps), a.heads);
+    const size_t smem = sizeof(float) * kWarps * (p.tile_rows + kTileColumns);   // (12 KB at most)
+    if (p.v == 8) k_posbias_backward<T, 8, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
+    else if (p.v == 2) k_posbias_backward<T, 2, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
+    else k_posbias_backward<T, 1, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
+    return cudaGetLastError();
+}
+
+bool few_buckets(const came_posbias& p) { return p.buckets <= kFewBuckets; }
+
+}  // namespace
+
+extern "C" {
+
+came_status came_posbias_bucket(const came_posbias* p, int64_t relative, int32_t* out)
+{
+    if (!p || !out) return report(CAME_ERR_NULL, "descriptor and out are required");
+    const came_status s = validate_buckets(*p);
+    if (s != CAME_OK) return s;
+    Buckets<kMostBuckets> b;
+    fill_buckets(*p, b);
+    const long long d = distance_of(std::max<int64_t>(-kFar, std::min<int64_t>(kFar, relative)), b.both);
+    const int m = static_cast<int>(std::upper_bound(b.start, b.start + b.n, d) - b.start) - 1;
+    *out = m + (b.both && relative > 0 ? b.n : 0);
+    return CAME_OK;
+}
+
+came_status came_posbias_forward(const came_posbias* p, int32_t device, void* cuda_stream)
+{
+    came_status s = validate_posbias(p, false);
+    if (s != CAME_OK) return s;
+    if ((s = require_current_device(device)) != CAME_OK) return s;
+    if (!p->q_len || !p->k_len) return CAME_OK;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    if (few_buckets(*p))
+        return p->data_dtype == CAME_BF16 ? launch_forward<__nv_bfloat16, kFewBuckets>(*p, stream) : launch_forward<float, kFewBuckets>(*p, stream);
+    return p->data_dtype == CAME_BF16 ? launch_forward<__nv_bfloat16, kMostBuckets>(*p, stream) : launch_forward<float, kMostBuckets>(*p, stream);
+}
+
+came_status came_posbias_workspace(const came_posbias* p, int64_t* out_bytes)
+{
+    if (!out_bytes) return report(CAME_ERR_NULL, "out_bytes is NULL");
+    const came_status s = validate_posbias(p, true);
+    if (s != CAME_OK) return s;
+    *out_bytes = std::max<int64_t>(256, plan_backward(*p).bytes);
+    return CAME_OK;
+}
+
+came_status came_posbias_backward(const came_posbias* p, void* workspace, int64_t workspace_bytes, int32_t device, void* cuda_stream)
+{
+    came_status s = validate_posbias(p, true);
+    if (s != CAME_OK) return s;
+    const BackwardPlan plan = plan_backward(*p);
+    if (!workspace) return report(CAME_ERR_NULL, "workspace is NULL");
+    if (!aligned_to(workspace, 16)) return report(CAME_ERR_ALIGN, "workspace not 16-byte aligned");
+    if (workspace_bytes < plan.bytes) return report(CAME_ERR_SHAPE, "workspace smaller than came_posbias_workspace says");
+    if (plan.units > (1ll << 31)) return report(CAME_ERR_SHAPE, "too many tiles for one launch");
+    if ((s = require_current_device(device)) != CAME_OK) return s;
+    const bool accumulate = p->flags & CAME_POSBIAS_ACCUMULATE, empty = !p->q_len || !p->k_len || !p->batch;
+    if (empty && accumulate) return CAME_OK;
+    const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    BiasArgs a = args_of(*p);
+    a.part = static_cast<float*>(workspace);
+    a.tile_rows = plan.tile_rows;
+    a.row_tiles = plan.row_tiles;
+    a.column_tiles = plan.column_tiles;
+    a.batches = plan.batches;
+    a.batch_groups = plan.batch_groups;
+    cudaError_t e = cudaSuccess;
+    const bool small = p->data_dtype == CAME_BF16;
+    if (!empty && few_buckets(*p))
+        e = small ? launch_backward<__nv_bfloat16, kFewBuckets>(a, *p, plan, stream) : launch_backward<float, kFewBuckets>(a, *p, plan, stream);
+    else if (!empty)
+        e = small ? launch_backward<__nv_bfloat16, kMostBuckets>(a, *p, plan, stream) : launch_backward<float, kMostBuckets>(a, *p, plan, stream);
+    if (e == cudaSuccess) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>((p->buckets + 31) / 32), p->heads);
+        cfg.blockDim = dim3(1024);
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        e = cudaLaunchKernelEx(&cfg, k_posbias_finish, a, empty ? 0ll : plan.units, accumulate ? 1 : 0);
+        if (e == cudaSuccess) e = cudaGetLastError();
+    }
+    return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
+}
+
+}  // extern "C"

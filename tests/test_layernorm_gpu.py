@@ -312,3 +312,32 @@ def test_refusals(env):
         with pytest.raises(binding.CameError) as e:
             bad()
         assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("rows,cols,extra,offset", [(70001, 64, 0, 0), (20001, 250, 0, 0), (16385, 256, 8, 0), (9001, 513, 0, 1), (5001, 1000, 0, 0), (3003, 2050, 2, 0),
+                                                    (1031, 4096, 0, 0), (901, 5120, 0, 0), (515, 8192, 0, 8), (300, 16384, 0, 0), (297, 12296, 0, 0)])
+@pytest.mark.parametrize("dtype,out,wdt", [("f32", "f32", "bf16"), ("bf16", "bf16", "f32")])
+def test_many_rows_in_both_directions(env, rows, cols, extra, offset, dtype, out, wdt):
+    """Groups that go from row to row, with full and partly filled last turns."""
+    torch, binding = env
+    a = Arena(torch)
+    x, w, b, new = _inputs(torch, a, rows, cols, cols + extra, offset, dtype, wdt, 15)
+    y = a.matrix(rows, cols, cols + extra, offset, out)
+    _, mean, rstd = binding.layer_norm_forward(x, w, b, 1e-5, out=y)
+    _check_forward(torch, x, w, b, 1e-5, y, mean, rstd, out)
+    dy, dx = a.matrix(rows, cols, cols + extra, offset, dtype), a.matrix(rows, cols, cols + extra, offset, dtype)
+    dy.copy_(new(rows, cols))
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    binding.layer_norm_backward(dy, x, mean, rstd, w, grad_x=dx, grad_weight=dw, grad_bias=db)
+    assert a.intact()
+    g, r = dy.double(), rstd.double()[:, None]
+    h = (x.double() - mean.double()[:, None]) * r
+    d = g * w.double()
+    c1, c2 = d.mean(1, keepdim=True), (d * h).mean(1, keepdim=True)
+    want = r * (d - c1 - h * c2)
+    tol = r * (6 * U * (d.abs() + c1.abs() + (h * c2).abs()) + _chain(cols) * (d.abs().mean(1, keepdim=True) + h.abs() * (d * h).abs().mean(1, keepdim=True)))
+    tol = (tol + HALF[dtype] * want.abs()) * (1 + HALF[dtype]) + 1e-40
+    assert bool(((dx.double() - want).abs() <= tol).all())
+    for got, terms in ((dw, g * h), (db, g)):
+        tol = (rows / 148 + 70) * U * terms.abs().sum(0) + HALF[wdt] * terms.sum(0).abs() * (1 + HALF[wdt]) + 1e-40
+        assert bool(((got.double() - terms.sum(0)).abs() <= tol).all())
