@@ -98,23 +98,23 @@ k_posbias_forward(const __grid_constant__ BiasArgs a, const __grid_constant__ Bu
     }
     __syncthreads();
     T* const out = static_cast<T*>(a.data) + h * a.q * a.k;
-    const int skew = static_cast<int>((reinterpret_cast<uintptr_t>(out) / sizeof(T)) % N);
+    const unsigned skew = static_cast<unsigned>(reinterpret_cast<uintptr_t>(out) / sizeof(T)), keys = static_cast<unsigned>(a.k);
     const int rows_at_once = 256 / tv, v = threadIdx.x % tv;
-    const long long vector = v0 + v;
-    for (int r = threadIdx.x / tv; r < tr && i0 + r < a.q; r += rows_at_once) {
-        const long long i = i0 + r;
-        const int ahead = static_cast<int>((N - (skew + i * a.k) % N) % N);      // elements before the row's first aligned one
-        const long long have = (a.k - ahead) >= 0 ? (a.k - ahead) / N : -1;
-        T* const row = out + i * a.k;
-        const int x = ahead + N * v + (tr - 1) - r;
+    const unsigned vector = static_cast<unsigned>(v0) + v;
+    const int rows = static_cast<int>(min(static_cast<long long>(tr), a.q - i0));
+    T* row = out + (i0 + threadIdx.x / tv) * a.k;
+    for (int r = threadIdx.x / tv; r < rows; r += rows_at_once, row += rows_at_once * a.k) {
+        const unsigned ahead = (N - (skew + static_cast<unsigned>(i0 + r) * keys) % N) % N;      // elements before the row's first aligned one
+        const unsigned have = keys >= ahead ? (keys - ahead) / N : 0u;                           // whole accesses of the row
+        const unsigned x = ahead + N * v + (tr - 1) - r;
+        T* const to = row + ahead + static_cast<size_t>(N) * vector;
         if (vector < have) {
-            const uint4 w = *reinterpret_cast<const uint4*>(line + (x % N) * length + x / N * N);
-            *reinterpret_cast<uint4*>(row + ahead + N * vector) = w;
+            *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(line + (x % N) * length + x / N * N);
         } else if (vector == have) {
-            for (int e = 0; e < N && ahead + N * vector + e < a.k; ++e) row[ahead + N * vector + e] = line[x + e];
+            for (unsigned e = 0; e < N && ahead + N * vector + e < keys; ++e) to[e] = line[x + e];
         }
         if (vector == 0)
-            for (int e = 0; e < ahead && e < a.k; ++e) row[e] = line[e + (tr - 1) - r];
+            for (unsigned e = 0; e < ahead && e < keys; ++e) row[e] = line[e + (tr - 1) - r];
     }
 }
 
