@@ -35,7 +35,8 @@ struct LnArgs {
     long long   x_ld, y_ld, dy_ld;
     float       eps, inv_cols;
     int         tpr;                     // threads per row
-    int         stages;                  // backward: rows in the ring, 2 to kMaxStages
+    int         stages;                  // places in the ring, 2 to kMaxStages
+    int         period;                  // rows until one begins at the same place relative to an aligned address
     int         w_bf16, y_bf16;
 };
 
@@ -67,6 +68,41 @@ __device__ __forceinline__ void store_as(void* p, int is_bf16, long long at, con
         v.set(x);
         v.store(static_cast<float*>(p) + at);
     }
+}
+
+// Eight columns from `column` on, those of them that the row has (kSkew: perhaps not all).
+template <bool kSkew>
+__device__ __forceinline__ void load_columns(const void* p, int is_bf16, int column, int cols, float (&x)[8])
+{
+    if (!p || column >= cols) return;
+    if constexpr (!kSkew) {
+        load_param<8>(p, is_bf16, column, x);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (static_cast<unsigned>(column + k) < static_cast<unsigned>(cols)) {
+                float one[1];
+                load_param<1>(p, is_bf16, column + k, one);
+                x[k] = one[0];
+            }
+    }
+}
+
+template <bool kSkew>
+__device__ __forceinline__ void store_columns(void* p, int is_bf16, long long row, int column, int cols, const float (&x)[8])
+{
+    if constexpr (kSkew) {
+        if (column < 0 || column + 8 > cols) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (static_cast<unsigned>(column + k) < static_cast<unsigned>(cols)) {
+                    const float one[1] = {x[k]};
+                    store_as<1>(p, is_bf16, row + column + k, one);
+                }
+            return;
+        }
+    }
+    store_as<8>(p, is_bf16, row + column, x);
 }
 
 __device__ __forceinline__ void group_barrier(int group, int tpr)
@@ -119,31 +155,29 @@ __device__ __forceinline__ float group_sum(float x, int group, int tpr, int warp
     return v[0];
 }
 
-// One access of `B` bytes (4, 8, 16 or 32) from global to shared memory, asynchronously.
-template <int B>
-__device__ __forceinline__ void copy_async(uint32_t to, const void* from)
+// Eight elements from global to shared memory, asynchronously; of the `left` elements that there are, the others become zero.
+template <typename T, bool kEnd>
+__device__ __forceinline__ void copy_async(uint32_t to, const T* from, long long left)
 {
-    if constexpr (B >= 16) {
+    constexpr int N = 16 / static_cast<int>(sizeof(T));
 #pragma unroll
-        for (int k = 0; k < B; k += 16)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + k), "l"(static_cast<const char*>(from) + k) : "memory");
-    } else {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(B) : "memory");
+    for (int k = 0; k < 8; k += N) {
+        if constexpr (kEnd) {
+            const int bytes = static_cast<int>(max(0ll, min(static_cast<long long>(N), left - k))) * static_cast<int>(sizeof(T));
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to + k * static_cast<int>(sizeof(T))), "l"(bytes ? from + k : from), "r"(bytes) : "memory");
+        } else {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to + k * static_cast<int>(sizeof(T))), "l"(from + k) : "memory");
+        }
     }
 }
 
-template <int B, int W>
+// W words from shared memory
+template <int W>
 __device__ __forceinline__ void read_shared(uint32_t at, uint32_t (&w)[W])
 {
-    if constexpr (B >= 16) {
 #pragma unroll
-        for (int k = 0; k < W; k += 4)
-            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "r"(at + 4 * k));
-    } else if constexpr (B == 8) {
-        asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
-    } else {
-        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[0]) : "r"(at));
-    }
+    for (int k = 0; k < W; k += 4)
+        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(w[k]), "=r"(w[k + 1]), "=r"(w[k + 2]), "=r"(w[k + 3]) : "r"(at + 4 * k));
 }
 
 template <int N>
@@ -173,6 +207,17 @@ k_ln_forward(const __grid_constant__ LnArgs a)
         const int col = (c * tpr + t) * V;
         if (col < a.cols) raw[c].load(x + col);
     }
+    // (few elements per thread: the parameters are on their way while the sums are formed)
+    constexpr bool kEarly = C * V <= 8;
+    float w[kEarly ? C : 1][V], b[kEarly ? C : 1][V];
+    if constexpr (kEarly) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * tpr + t) * V;
+            if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
+            if (a.b && col < a.cols) load_param<V>(a.b, a.w_bf16, col, b[c]);
+        }
+    }
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -199,83 +244,103 @@ k_ln_forward(const __grid_constant__ LnArgs a)
     for (int c = 0; c < C; ++c) {
         const int col = (c * tpr + t) * V;
         if (col >= a.cols) continue;
-        float y[V], p[V];
+        const int at = kEarly ? c : 0;
+        float y[V];
 #pragma unroll
         for (int k = 0; k < V; ++k) y[k] = (raw[c].value(k) - mean) * rstd;
         if (a.w) {
-            load_param<V>(a.w, a.w_bf16, col, p);
+            if constexpr (!kEarly) load_param<V>(a.w, a.w_bf16, col, w[0]);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] = __fmul_rn(y[k], p[k]);
+            for (int k = 0; k < V; ++k) y[k] = __fmul_rn(y[k], w[at][k]);
         }
         if (a.b) {
-            load_param<V>(a.b, a.w_bf16, col, p);
+            if constexpr (!kEarly) load_param<V>(a.b, a.w_bf16, col, b[0]);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] = __fadd_rn(y[k], p[k]);
+            for (int k = 0; k < V; ++k) y[k] = __fadd_rn(y[k], b[at][k]);
         }
         store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, y);
     }
 }
 
-// Many rows: a group goes from two rows to the next two.  They come through a ring in shared memory (as in the backward pass:
-// every thread copies and reads its own columns), the parameters stay in registers, and two rows share each barrier.
-template <typename X, int V, int C>
+// The rows that a group of the kernels below takes, and where its threads' columns lie.  Rows whose stride is no multiple of eight
+// elements begin at other places relative to an aligned address, again and again after `period` rows: a group takes rows of one
+// such place only, so that it can make aligned accesses and keep its columns.  Thread t's access c is at column (c tpr + t) 8 - skew;
+// of the ones that reach over an end of the row, the elements outside are left out.
+struct Rows {
+    long long first, step;               // rows first, first + step, ...
+    int skew;
+    __device__ __forceinline__ Rows(const LnArgs& a, int groups, int group, int at_once)
+    {
+        const long long id = static_cast<long long>(blockIdx.x) * groups + group, per = static_cast<long long>(gridDim.x) * groups / a.period;
+        const long long place = id % a.period, turn = id / a.period;
+        first = turn < per ? place + a.period * at_once * turn : a.rows;
+        step = a.period * at_once * per;
+        skew = static_cast<int>((place * a.x_ld) & 7);
+    }
+};
+
+// Many rows: a group goes from two rows to the next two.  They come through a ring in shared memory (every thread copies and
+// reads its own columns, so it waits for nothing but its own copies), the parameters stay in registers, and two rows share each
+// barrier.
+template <typename X, int C, bool kSkew>
 __global__ void __launch_bounds__(kBlockThreads, 1)
 k_ln_forward_rows(const __grid_constant__ LnArgs a)
 {
-    constexpr int kX = V * static_cast<int>(sizeof(X));
-    static_assert(kX >= 4, "");
+    constexpr int kX = 8 * static_cast<int>(sizeof(X));
     extern __shared__ __align__(16) char dynamic[];
     __shared__ float room[2][kBlockThreads / 32][2];
     const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
     const int warp0 = group * (tpr >> 5), stages = a.stages;
-    const long long step = 2ll * gridDim.x * groups;
+    const Rows rows(a, groups, group, 2);
+    const int skew = kSkew ? rows.skew : 0;
+    const long long other = kSkew ? a.period : 1, end = kSkew ? static_cast<long long>(a.rows - 1) * a.x_ld + a.cols : 0;
+    auto column = [&](int c) { return (c * tpr + t) * 8 - skew; };
+    auto outside = [&](int c, int k) { return static_cast<unsigned>(column(c) + k) >= static_cast<unsigned>(a.cols); };
+    auto partial = [&](int c) { return kSkew && (column(c) < 0 || column(c) + 8 > a.cols); };
     const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
     auto place = [&](int stage, int r, int c) { return base + (((stage * 2 + r) * C + c) * blockDim.x + threadIdx.x) * kX; };
     auto start = [&](long long row, int stage) {
 #pragma unroll
         for (int r = 0; r < 2; ++r)
-            if (row + r < a.rows) {
-                const X* const x = static_cast<const X*>(a.x) + (row + r) * a.x_ld;
+            if (row + r * other < a.rows) {
+                const long long at = (row + r * other) * a.x_ld;
 #pragma unroll
-                for (int c = 0; c < C; ++c) {
-                    const int col = (c * tpr + t) * V;
-                    if (col < a.cols) copy_async<kX>(place(stage, r, c), x + col);
-                }
+                for (int c = 0; c < C; ++c)
+                    if (column(c) < a.cols) copy_async<X, kSkew>(place(stage, r, c), static_cast<const X*>(a.x) + at + column(c), end - at - column(c));
             }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    const long long first = 2ll * (static_cast<long long>(blockIdx.x) * groups + group);
-    for (int k = 0; k < stages - 1; ++k) start(first + k * step, k);
-    float w[C][V], b[C][V];
+    for (int k = 0; k < stages - 1; ++k) start(rows.first + k * rows.step, k);
+    float w[C][8], b[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col = (c * tpr + t) * V;
 #pragma unroll
-        for (int k = 0; k < V; ++k) w[c][k] = 1.f, b[c][k] = 0.f;
-        if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
-        if (a.b && col < a.cols) load_param<V>(a.b, a.w_bf16, col, b[c]);
+        for (int k = 0; k < 8; ++k) w[c][k] = 1.f, b[c][k] = 0.f;
+        load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, w[c]);
+        load_columns<kSkew>(a.b, a.w_bf16, column(c), a.cols, b[c]);
     }
     int stage = 0;
-    for (long long row = first; row < a.rows; row += step) {
+    for (long long row = rows.first; row < a.rows; row += rows.step) {
         wait_all_but<kMaxStages - 2>(stages - 2);
-        float x[2][C][V], sums[2][2] = {};
+        float x[2][C][8], sums[2][2] = {};
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                Vec<X, V> v;
-                if ((c * tpr + t) * V >= a.cols) continue;
-                read_shared<kX>(place(stage, r, c), v.w);       // (a second row that is not there: whatever the ring holds; not written)
+                Vec<X, 8> v;
+                if (column(c) >= a.cols) continue;
+                read_shared(place(stage, r, c), v.w);            // (a second row that is not there: whatever the ring holds; not written)
 #pragma unroll
-                for (int k = 0; k < V; ++k) x[r][c][k] = v.value(k);
-                if constexpr (V == 1) sums[r][0] += x[r][c][0];
-                else
+                for (int k = 0; k < 8; ++k) x[r][c][k] = v.value(k);
+                if (partial(c))
 #pragma unroll
-                    for (int k = 0; k < V; k += 2) add2(sums[r][0], sums[r][1], x[r][c][k], x[r][c][k + 1]);
+                    for (int k = 0; k < 8; ++k) x[r][c][k] = outside(c, k) ? 0.f : x[r][c][k];
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) add2(sums[r][0], sums[r][1], x[r][c][k], x[r][c][k + 1]);
             }
         float s[2] = {sums[0][0] + sums[0][1], sums[1][0] + sums[1][1]};
         // two rows into the place of the two before these (which have been read)
-        start(row + (stages - 1) * step, stage == 0 ? stages - 1 : stage - 1);
+        start(row + (stages - 1) * rows.step, stage == 0 ? stages - 1 : stage - 1);
         stage = stage + 1 == stages ? 0 : stage + 1;
         group_sum(s, group, tpr, t >> 5, room[0] + warp0);
         float squares[2][2] = {};
@@ -284,49 +349,39 @@ k_ln_forward_rows(const __grid_constant__ LnArgs a)
             s[r] *= a.inv_cols;
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                if ((c * tpr + t) * V >= a.cols) continue;
-                if constexpr (V == 1) {
-                    x[r][c][0] -= s[r];
-                    squares[r][0] = fmaf(x[r][c][0], x[r][c][0], squares[r][0]);
-                } else {
+                if (column(c) >= a.cols) continue;
 #pragma unroll
-                    for (int k = 0; k < V; k += 2) {
-                        add2(x[r][c][k], x[r][c][k + 1], -s[r], -s[r]);
-                        fma2(squares[r][0], squares[r][1], x[r][c][k], x[r][c][k + 1], x[r][c][k], x[r][c][k + 1]);
-                    }
-                }
+                for (int k = 0; k < 8; k += 2) add2(x[r][c][k], x[r][c][k + 1], -s[r], -s[r]);
+                if (partial(c))
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) x[r][c][k] = outside(c, k) ? 0.f : x[r][c][k];
+#pragma unroll
+                for (int k = 0; k < 8; k += 2) fma2(squares[r][0], squares[r][1], x[r][c][k], x[r][c][k + 1], x[r][c][k], x[r][c][k + 1]);
             }
         }
         float q[2] = {squares[0][0] + squares[0][1], squares[1][0] + squares[1][1]};
         group_sum(q, group, tpr, t >> 5, room[1] + warp0);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            if (row + r >= a.rows) continue;
+            const long long here = row + r * other;
+            if (here >= a.rows) continue;
             const float rstd = __frsqrt_rn(fmaf(q[r], a.inv_cols, a.eps));
             if (t == 0 && a.mean) {
-                a.mean[row + r] = s[r];
-                a.rstd[row + r] = rstd;
+                a.mean[here] = s[r];
+                a.rstd[here] = rstd;
             }
 #pragma unroll
             for (int c = 0; c < C; ++c) {
-                const int col = (c * tpr + t) * V;
-                if (col >= a.cols) continue;
-                float y[V];
+                if (column(c) >= a.cols) continue;
+                float y[8];
 #pragma unroll
-                for (int k = 0; k < V; ++k) y[k] = x[r][c][k];
-                if constexpr (V == 1) {
-                    y[0] = fmaf(y[0] * rstd, w[c][0], b[c][0]);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < V; k += 2) {
-                        float p = b[c][k], o = b[c][k + 1];
-                        mul2(y[k], y[k + 1], rstd, rstd);
-                        fma2(p, o, y[k], y[k + 1], w[c][k], w[c][k + 1]);
-                        y[k] = p;
-                        y[k + 1] = o;
-                    }
+                for (int k = 0; k < 8; k += 2) {
+                    float p = x[r][c][k], o = x[r][c][k + 1];
+                    y[k] = b[c][k], y[k + 1] = b[c][k + 1];
+                    mul2(p, o, rstd, rstd);
+                    fma2(y[k], y[k + 1], p, o, w[c][k], w[c][k + 1]);
                 }
-                store_as<V>(a.y, a.y_bf16, (row + r) * a.y_ld + col, y);
+                store_columns<kSkew>(a.y, a.y_bf16, here * a.y_ld, column(c), a.cols, y);
             }
         }
     }
@@ -389,215 +444,167 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
 
 // ---- backward -----------------------------------------------------------------------------------
 
-// What a thread has of the rows that are on their way.  Every thread copies, and later reads, its own columns
-// only, so nothing but its own copies has to be waited for.  bf16 that is not aligned to 4 bytes cannot be copied so:
-// there one row ahead is loaded into registers.
-template <typename X, typename G, int V, int C>
-struct Ring {
-    static constexpr bool kAsync = V * sizeof(X) >= 4 && V * sizeof(G) >= 4;
-    static constexpr int  kX = V * static_cast<int>(sizeof(X)), kG = V * static_cast<int>(sizeof(G));
-    static constexpr int  kStage = C * (kX + kG);        // bytes per thread and stage
-
-    uint32_t base;
-    Vec<X, V> x[C];
-    Vec<G, V> dy[C];
-
-    // (accesses of a warp lie side by side: stage, then access, then thread)
-    __device__ __forceinline__ uint32_t x_at(int stage, int c) const { return base + stage * kStage * blockDim.x + (c * blockDim.x + threadIdx.x) * kX; }
-    __device__ __forceinline__ uint32_t g_at(int stage, int c) const { return base + (stage * kStage + C * kX) * blockDim.x + (c * blockDim.x + threadIdx.x) * kG; }
-
-    __device__ __forceinline__ void start(const LnArgs& a, long long row, int t, int stage)
-    {
-        const X* const px = static_cast<const X*>(a.x) + row * a.x_ld;
-        const G* const pg = static_cast<const G*>(a.dy) + row * a.dy_ld;
-#pragma unroll
-        for (int c = 0; c < C; ++c) {
-            const int col = (c * a.tpr + t) * V;
-            if (col >= a.cols) continue;
-            if constexpr (kAsync) {
-                copy_async<kX>(x_at(stage, c), px + col);
-                copy_async<kG>(g_at(stage, c), pg + col);
-            } else {
-                x[c].load(px + col);
-                dy[c].load(pg + col);
-            }
-        }
-    }
-    __device__ __forceinline__ void take(int stage, int c, Vec<X, V>& vx, Vec<G, V>& vg) const
-    {
-        if constexpr (kAsync) {
-            read_shared<kX>(x_at(stage, c), vx.w);
-            read_shared<kG>(g_at(stage, c), vg.w);
-        } else {
-            vx = x[c];
-            vg = dy[c];
-        }
-    }
-};
-
-// C accesses of V elements per thread.  kHold: the weight and what the second half needs stay in registers; else the ring
+// C accesses of 8 elements per thread.  kHold: the weight and what the second half needs stay in registers; else the ring
 // is read again, and the weight is kept in shared memory.
-template <typename X, typename G, int V, int C, bool kHold>
+template <typename X, typename G, int C, bool kHold, bool kSkew>
 __global__ void __launch_bounds__(kBlockThreads, 1)
 k_ln_backward(const __grid_constant__ LnArgs a)
 {
-    using R = Ring<X, G, V, C>;
+    constexpr int kX = 8 * static_cast<int>(sizeof(X)), kG = 8 * static_cast<int>(sizeof(G)), kStage = C * (kX + kG);
     extern __shared__ __align__(16) char dynamic[];      // the ring; at the end the groups' sums: [2][cols]
     __shared__ float room[2][kBlockThreads / 32][2];
     release_dependents();
     const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
-    const int warp0 = group * (tpr >> 5), stages = R::kAsync ? a.stages : 1;
-    const long long step = static_cast<long long>(gridDim.x) * groups;
-    float w[kHold ? C : 1][V], dw[C][V], db[C][V];
+    const int warp0 = group * (tpr >> 5), stages = a.stages;
+    const Rows rows(a, groups, group, 1);
+    const int skew = kSkew ? rows.skew : 0;
+    const long long end_x = kSkew ? static_cast<long long>(a.rows - 1) * a.x_ld + a.cols : 0, end_g = kSkew ? static_cast<long long>(a.rows - 1) * a.dy_ld + a.cols : 0;
+    auto column = [&](int c) { return (c * tpr + t) * 8 - skew; };
+    auto outside = [&](int c, int k) { return static_cast<unsigned>(column(c) + k) >= static_cast<unsigned>(a.cols); };
+    auto partial = [&](int c) { return kSkew && (column(c) < 0 || column(c) + 8 > a.cols); };
+    float w[kHold ? C : 1][8], dw[C][8], db[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        const int col = (c * tpr + t) * V;
 #pragma unroll
-        for (int k = 0; k < V; ++k) dw[c][k] = db[c][k] = 0.f;
+        for (int k = 0; k < 8; ++k) dw[c][k] = db[c][k] = 0.f;
         if constexpr (kHold) {
 #pragma unroll
-            for (int k = 0; k < V; ++k) w[c][k] = 1.f;
-            if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, w[c]);
+            for (int k = 0; k < 8; ++k) w[c][k] = 1.f;
+            load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, w[c]);
         }
     }
-    R ring;
-    ring.base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
-    const uint32_t weights = ring.base;
-    auto weight_at = [&](int c, float (&x)[V]) {         // as fp32 in front of the ring, each thread its own columns
-        Vec<float, V> v;
-        read_shared<4 * V>(weights + (c * blockDim.x + threadIdx.x) * 4 * V, v.w);
-#pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = v.value(k);
-    };
+    uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
+    const uint32_t weights = base + threadIdx.x * 32;            // !kHold: as fp32 in front of the ring, each thread its own columns
     if constexpr (!kHold) {
-        ring.base += C * V * 4 * blockDim.x;
+        base += C * 32 * blockDim.x;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * tpr + t) * V;
-            float x[V];
+            float x[8];
 #pragma unroll
-            for (int k = 0; k < V; ++k) x[k] = 1.f;
-            if (a.w && col < a.cols) load_param<V>(a.w, a.w_bf16, col, x);
+            for (int k = 0; k < 8; ++k) x[k] = 1.f;
+            load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, x);
 #pragma unroll
-            for (int k = 0; k < V; ++k) reinterpret_cast<float*>(dynamic)[(c * blockDim.x + threadIdx.x) * V + k] = x[k];
+            for (int k = 0; k < 8; ++k) reinterpret_cast<float*>(dynamic)[(c * blockDim.x + threadIdx.x) * 8 + k] = x[k];
         }
         __syncthreads();
     }
-    const long long first = static_cast<long long>(blockIdx.x) * groups + group;
+    auto weight_at = [&](int c) {
+        Vec<float, 8> v;
+        read_shared(weights + c * blockDim.x * 32, v.w);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[0][k] = v.value(k);
+    };
+    // (accesses of a warp lie side by side: stage, then access, then thread)
+    auto x_at = [&](int stage, int c) { return base + stage * kStage * blockDim.x + (c * blockDim.x + threadIdx.x) * kX; };
+    auto g_at = [&](int stage, int c) { return base + (stage * kStage + C * kX) * blockDim.x + (c * blockDim.x + threadIdx.x) * kG; };
+    auto start = [&](long long row, int stage) {
+        if (row < a.rows) {
+            const long long px = row * a.x_ld, pg = row * a.dy_ld;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                if (column(c) >= a.cols) continue;
+                copy_async<X, kSkew>(x_at(stage, c), static_cast<const X*>(a.x) + px + column(c), end_x - px - column(c));
+                copy_async<G, kSkew>(g_at(stage, c), static_cast<const G*>(a.dy) + pg + column(c), end_g - pg - column(c));
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
     // stages - 1 rows are on their way while one is computed
-    for (int k = 0; k < (R::kAsync ? stages - 1 : 1); ++k) {
-        if (first + k * step < a.rows) ring.start(a, first + k * step, t, k);
-        if constexpr (R::kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
-    }
+    for (int k = 0; k < stages - 1; ++k) start(rows.first + k * rows.step, k);
     float mean = 0.f, rstd = 0.f;
-    if (first < a.rows) mean = a.mean[first], rstd = a.rstd[first];
+    if (rows.first < a.rows) mean = a.mean[rows.first], rstd = a.rstd[rows.first];
     int stage = 0, turn = 0;
-    for (long long row = first; row < a.rows; row += step, turn ^= 1) {
-        float h[kHold ? C : 1][V], d[kHold ? C : 1][V];
+    for (long long row = rows.first; row < a.rows; row += rows.step, turn ^= 1) {
+        float h[kHold ? C : 1][8], d[kHold ? C : 1][8];
         float ds[2] = {}, dh[2] = {};    // sums of d and of d h
         const float now_mean = mean, now_rstd = rstd;
         const int now = stage;
-        Vec<X, V> vx[R::kAsync ? 1 : C];
-        Vec<G, V> vg[R::kAsync ? 1 : C];
-        if constexpr (!R::kAsync) {
+        Vec<X, 8> vx;
+        Vec<G, 8> vg;
+        // h and dy of access c; nothing outside the row
+        auto take = [&](int c, float (&hh)[8], float (&g)[8]) {
+            read_shared(x_at(now, c), vx.w);
+            read_shared(g_at(now, c), vg.w);
 #pragma unroll
-            for (int c = 0; c < C; ++c) vx[c] = ring.x[c], vg[c] = ring.dy[c];
-        } else {
-            wait_all_but<kMaxStages - 2>(stages - 2);
-        }
-        {
-            // the row after the ones on their way takes the place of the one before this (which has been read)
-            const long long ahead = row + (R::kAsync ? stages - 1 : 1) * step;
-            const int to = stage == 0 ? stages - 1 : stage - 1;
-            if (ahead < a.rows) ring.start(a, ahead, t, to);
-            if constexpr (R::kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
-            if (row + step < a.rows) mean = a.mean[row + step], rstd = a.rstd[row + step];
-        }
+            for (int k = 0; k < 8; k += 2) {
+                hh[k] = vx.value(k), hh[k + 1] = vx.value(k + 1);
+                g[k] = vg.value(k), g[k + 1] = vg.value(k + 1);
+                add2(hh[k], hh[k + 1], -now_mean, -now_mean);
+                mul2(hh[k], hh[k + 1], now_rstd, now_rstd);
+            }
+            if (partial(c))
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (outside(c, k)) hh[k] = g[k] = 0.f;
+        };
+        wait_all_but<kMaxStages - 2>(stages - 2);
+        // the row after the ones on their way takes the place of the one before this (which has been read)
+        start(row + (stages - 1) * rows.step, stage == 0 ? stages - 1 : stage - 1);
+        if (row + rows.step < a.rows) mean = a.mean[row + rows.step], rstd = a.rstd[row + rows.step];
         stage = stage + 1 == stages ? 0 : stage + 1;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * tpr + t) * V, at = kHold ? c : 0, from = R::kAsync ? 0 : c;
-            if (col >= a.cols) continue;
-            if constexpr (R::kAsync) ring.take(now, c, vx[0], vg[0]);
-            if constexpr (!kHold) weight_at(c, w[0]);
-            if constexpr (V == 1) {
-                const float g = vg[from].value(0);
-                h[at][0] = (vx[from].value(0) - now_mean) * now_rstd;
-                d[at][0] = g * w[at][0];
-                dw[c][0] = fmaf(g, h[at][0], dw[c][0]);
-                db[c][0] += g;
-                ds[0] += d[at][0];
-                dh[0] = fmaf(d[at][0], h[at][0], dh[0]);
-            } else {
+            const int at = kHold ? c : 0;
+            if (column(c) >= a.cols) continue;
+            if constexpr (!kHold) weight_at(c);
+            float g[8];
+            take(c, h[at], g);
 #pragma unroll
-                for (int k = 0; k < V; k += 2) {
-                    const float g = vg[from].value(k), g1 = vg[from].value(k + 1);
-                    h[at][k] = vx[from].value(k), h[at][k + 1] = vx[from].value(k + 1);
-                    d[at][k] = g, d[at][k + 1] = g1;
-                    add2(h[at][k], h[at][k + 1], -now_mean, -now_mean);
-                    mul2(h[at][k], h[at][k + 1], now_rstd, now_rstd);
-                    mul2(d[at][k], d[at][k + 1], w[at][k], w[at][k + 1]);
-                    fma2(dw[c][k], dw[c][k + 1], g, g1, h[at][k], h[at][k + 1]);
-                    add2(db[c][k], db[c][k + 1], g, g1);
-                    add2(ds[0], ds[1], d[at][k], d[at][k + 1]);
-                    fma2(dh[0], dh[1], d[at][k], d[at][k + 1], h[at][k], h[at][k + 1]);
-                }
+            for (int k = 0; k < 8; k += 2) {
+                d[at][k] = g[k], d[at][k + 1] = g[k + 1];
+                mul2(d[at][k], d[at][k + 1], w[at][k], w[at][k + 1]);
+                fma2(dw[c][k], dw[c][k + 1], g[k], g[k + 1], h[at][k], h[at][k + 1]);
+                add2(db[c][k], db[c][k + 1], g[k], g[k + 1]);
+                add2(ds[0], ds[1], d[at][k], d[at][k + 1]);
+                fma2(dh[0], dh[1], d[at][k], d[at][k + 1], h[at][k], h[at][k + 1]);
             }
         }
-        float s[2] = {ds[0] + ds[1], dh[0] + dh[1]};
         if (!a.y) continue;
+        float s[2] = {ds[0] + ds[1], dh[0] + dh[1]};
         group_sum(s, group, tpr, t >> 5, room[turn] + warp0);
         const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int col = (c * tpr + t) * V, at = kHold ? c : 0;
-            if (col >= a.cols) continue;
-            float o[V];
+            const int at = kHold ? c : 0;
+            if (column(c) >= a.cols) continue;
+            float o[8];
             if constexpr (!kHold) {
-                ring.take(now, c, vx[0], vg[0]);
-                weight_at(c, w[0]);
+                weight_at(c);
+                take(c, h[0], d[0]);
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    h[0][k] = (vx[0].value(k) - now_mean) * now_rstd;
-                    d[0][k] = vg[0].value(k) * w[0][k];
-                }
+                for (int k = 0; k < 8; k += 2) mul2(d[0][k], d[0][k + 1], w[0][k], w[0][k + 1]);
             }
-            if constexpr (V == 1) {
-                o[0] = now_rstd * fmaf(h[at][0], -c2, d[at][0] - c1);
-            } else {
 #pragma unroll
-                for (int k = 0; k < V; k += 2) {
-                    o[k] = d[at][k], o[k + 1] = d[at][k + 1];
-                    add2(o[k], o[k + 1], -c1, -c1);
-                    fma2(o[k], o[k + 1], h[at][k], h[at][k + 1], -c2, -c2);
-                    mul2(o[k], o[k + 1], now_rstd, now_rstd);
-                }
+            for (int k = 0; k < 8; k += 2) {
+                o[k] = d[at][k], o[k + 1] = d[at][k + 1];
+                add2(o[k], o[k + 1], -c1, -c1);
+                fma2(o[k], o[k + 1], h[at][k], h[at][k + 1], -c2, -c2);
+                mul2(o[k], o[k + 1], now_rstd, now_rstd);
             }
-            store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, o);
+            store_columns<kSkew>(a.y, a.y_bf16, row * a.y_ld, column(c), a.cols, o);
         }
     }
     if (!a.part) return;
-    // the groups one after another, so that the order is theirs
-    if constexpr (R::kAsync) wait_all_but<0>(0);
-    __syncthreads();
+    // the groups one after another, so that the order is theirs (their columns may lie at different threads: all of a group's
+    // columns belong to it, so that every sum meets every column once)
+    wait_all_but<0>(0);
     float* const sums = reinterpret_cast<float*>(dynamic);
     float* const part = a.part + 2ll * blockIdx.x * a.cols;
     for (int g = 0; g < groups; ++g) {
         const bool last = g == groups - 1;
-        if (group == g)
+        __syncthreads();
+        if (group != g) continue;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                const int col = (c * tpr + t) * V;
-                if (col >= a.cols) continue;
+        for (int c = 0; c < C; ++c)
 #pragma unroll
-                for (int k = 0; k < V; ++k) {
-                    float p = dw[c][k], q = db[c][k];
-                    if (g > 0) p += sums[col + k], q += sums[a.cols + col + k];
-                    if (last) part[col + k] = p, part[a.cols + col + k] = q;
-                    else sums[col + k] = p, sums[a.cols + col + k] = q;
-                }
+            for (int k = 0; k < 8; ++k) {
+                const int col = column(c) + k;
+                if (static_cast<unsigned>(col) >= static_cast<unsigned>(a.cols)) continue;
+                float p = dw[c][k], q = db[c][k];
+                if (g > 0) p += sums[col], q += sums[a.cols + col];
+                if (last) part[col] = p, part[a.cols + col] = q;
+                else sums[col] = p, sums[a.cols + col] = q;
             }
-        if (!last) __syncthreads();
     }
 }
 
@@ -612,7 +619,7 @@ k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
     const G* const dy = static_cast<const G*>(a.dy) + row * a.dy_ld;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float s[2] = {0.f, 0.f};
-    for (int col = threadIdx.x * V; col < a.cols; col += 1024 * V) {
+    for (int col = threadIdx.x * V; col < a.cols; col += blockDim.x * V) {
         Vec<X, V> vx;
         Vec<G, V> vg;
         vx.load(x + col);
@@ -630,7 +637,7 @@ k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
         s[0] += p;
         s[1] += q;
     }
-    group_sum(s, 0, 1024, threadIdx.x >> 5, room);
+    group_sum(s, 0, blockDim.x, threadIdx.x >> 5, room);
     if (threadIdx.x == 0) out[row] = make_float2(s[0] * a.inv_cols, s[1] * a.inv_cols);
 }
 
@@ -763,55 +770,66 @@ came_status validate_ln(const came_layernorm* l, bool backward)
     return CAME_OK;
 }
 
-// Elements per access: 8 where every row of every tensor starts at a multiple of 8 elements (and 16 bytes, or 32), then 2, then 1.
-int access_of(const came_layernorm& l, bool backward)
+// How the rows of all tensors can be accessed: eight elements at a time, aligned, where they begin at the same places.
+struct Access {
+    bool wide;                           // every row begins at a multiple of eight elements, and has such a length
+    int  period;                         // else: rows until the places repeat, 1 to 8; 0: not at the same places
+};
+
+Access access_of(const came_layernorm& l, bool backward)
 {
-    for (int v : {8, 2}) {
-        bool ok = l.cols % v == 0 && l.x_ld % v == 0 && l.y_ld % v == 0;
-        auto fits = [&](const void* p, int32_t dt) { ok = ok && aligned_to(p, v * dtype_bytes(dt)); };
-        fits(l.x, l.x_dtype);
-        fits(backward ? l.dy : l.y, l.y_dtype);
-        fits(l.weight, l.weight_dtype);
-        if (!backward) fits(l.bias, l.weight_dtype);
-        if (backward && l.dx) {
-            ok = ok && l.dx_ld % v == 0;
-            fits(l.dx, l.dx_dtype);
-        }
-        if (ok) return v;
-    }
-    return 1;
+    Access a = {true, 0};
+    bool same = true;                    // all tensors begin aligned, and their strides agree modulo 8
+    auto rows = [&](const void* p, int64_t ld, int32_t dt) {
+        same = same && aligned_to(p, 8 * dtype_bytes(dt)) && ld % 8 == l.x_ld % 8;
+    };
+    rows(l.x, l.x_ld, l.x_dtype);
+    rows(backward ? l.dy : l.y, l.y_ld, l.y_dtype);
+    if (backward && l.dx) rows(l.dx, l.dx_ld, l.dx_dtype);
+    a.wide = same && l.cols % 8 == 0 && l.x_ld % 8 == 0 && aligned_to(l.weight, 8 * dtype_bytes(l.weight_dtype)) &&
+             (backward || aligned_to(l.bias, 8 * dtype_bytes(l.weight_dtype)));
+    if (same)
+        for (a.period = 1; a.period * l.x_ld % 8; a.period *= 2) {}
+    return a;
 }
 
 // Threads per row, in whole warps, where each holds `held` elements.
 int threads_per_row(long long cols, int held) { return static_cast<int>((cols + 32 * held - 1) / (32 * held)) * 32; }
 
-struct BackwardPlan { int v, held, tpr, threads, stages, blocks, column_blocks; size_t smem, means, part, bytes; };
+// Blocks of `groups` groups that take `at_once` rows each time: no more than have rows, and groups for every place.
+int blocks_for(long long rows, int groups, int at_once, int period)
+{
+    const long long want = std::min<long long>((rows + at_once * groups - 1) / (at_once * groups), kSMs);
+    return static_cast<int>(std::max<long long>({1, want, (period + groups - 1) / groups}));
+}
+
+struct BackwardPlan { int held, tpr, threads, stages, blocks, column_blocks; Access access; size_t smem, means, part, bytes; };
 
 BackwardPlan plan_backward(const came_layernorm& l)
 {
     BackwardPlan p = {};
-    p.v = access_of(l, true);
-    const size_t xb = dtype_bytes(l.x_dtype), gb = dtype_bytes(l.y_dtype);
-    const bool async = p.v * std::min(xb, gb) >= 4, sums = l.dweight || l.dbias;
-    // elements of a row per thread (0: the row does not fit a block)
-    if (!async) p.held = l.cols <= 8 * kBlockThreads ? 8 : 0;
-    else if (l.cols <= 8 * 32) p.held = 8;
-    else if (l.cols <= 16 * kBlockThreads) p.held = 16;
-    else if (p.v == 8 && l.cols <= 32 * kBlockThreads) p.held = 32;
+    p.access = access_of(l, true);
+    const size_t pair = dtype_bytes(l.x_dtype) + dtype_bytes(l.y_dtype);
+    const bool sums = l.dweight || l.dbias;
+    const int64_t span = l.cols + (p.access.wide ? 0 : 7);       // columns, and the place of the first
+    // elements of a row per thread (0: the row does not fit a block, or its tensors' rows begin at different places)
+    if (!p.access.period) p.held = 0;
+    else if (span <= 8 * 32) p.held = 8;
+    else if (span <= 16 * kBlockThreads) p.held = 16;
+    else if (span <= 32 * kBlockThreads) p.held = 32;
     if (p.held) {
-        p.tpr = threads_per_row(l.cols, p.held);
+        p.tpr = threads_per_row(span, p.held);
         const int groups = std::max(1, kBlockThreads / p.tpr);
         p.threads = groups * p.tpr;
-        const size_t stage = async ? p.held * (xb + gb) * p.threads : 0;
-        const size_t weights = p.held == 32 ? sizeof(float) * 32 * p.threads : 0;
-        p.stages = async ? static_cast<int>(std::max<size_t>(2, std::min<size_t>(kMaxStages, (kRingBytes - weights) / stage))) : 2;
+        const size_t stage = p.held * pair * p.threads, weights = p.held == 32 ? sizeof(float) * 32 * p.threads : 0;
+        p.stages = static_cast<int>(std::max<size_t>(2, std::min<size_t>(kMaxStages, (kRingBytes - weights) / stage)));
         p.smem = std::max(weights + stage * p.stages, groups > 1 && sums ? sizeof(float) * 2 * l.cols : 0);
         if (p.smem > kRingBytes) p.held = 0;
-        const long long want = (l.rows + groups - 1) / groups;
-        p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, kSMs)));
+        p.blocks = blocks_for(l.rows, groups, 1, p.access.period);
     }
     if (!p.held) {
-        p.column_blocks = static_cast<int>((l.cols + 32 * p.v - 1) / (32 * p.v));
+        const int v = p.access.wide ? 8 : 1;
+        p.column_blocks = static_cast<int>((l.cols + 32 * v - 1) / (32 * v));
         const long long want = (l.rows + 7) / 8;
         p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, std::max(1, kSMs * 8 / p.column_blocks))));
     }
@@ -823,31 +841,25 @@ BackwardPlan plan_backward(const came_layernorm& l)
     return p;
 }
 
-template <typename X, int V, int E>
+template <typename X, int E, bool kSkew>
 cudaError_t launch_forward_rows(LnArgs a, int32_t device, cudaStream_t stream)
 {
     static std::atomic<uint64_t> done{0};
-    auto* const kernel = k_ln_forward_rows<X, V, E / V>;
+    auto* const kernel = k_ln_forward_rows<X, E / 8, kSkew>;
     const cudaError_t e = allow_smem(kernel, kRingBytes, device, done);
     if (e != cudaSuccess) return e;
-    a.tpr = threads_per_row(a.cols, E);
+    a.tpr = threads_per_row(a.cols + (kSkew ? 7 : 0), E);
     const int groups = std::max(1, kBlockThreads / a.tpr), threads = groups * a.tpr;
     const int stage = 2 * E * static_cast<int>(sizeof(X)) * threads;         // (64 KB at most)
     a.stages = std::min(kMaxStages, kRingBytes / stage);
-    const long long want = (a.rows + 2 * groups - 1) / (2 * groups);
-    kernel<<<static_cast<unsigned>(std::min<long long>(want, kSMs)), threads, static_cast<size_t>(stage) * a.stages, stream>>>(a);
+    kernel<<<blocks_for(a.rows, groups, 2, a.period), threads, static_cast<size_t>(stage) * a.stages, stream>>>(a);
     return cudaGetLastError();
 }
 
 template <typename X, int V>
-cudaError_t launch_forward(LnArgs a, int32_t device, cudaStream_t stream)
+cudaError_t launch_forward_once(LnArgs a, cudaStream_t stream)
 {
-    constexpr int kMost = V == 8 ? 32 : 16;      // elements that a thread may hold
-    // (fp32 rows in wide accesses: a block per few rows is faster from 257 columns on, 612 against 735 us at 128k x 4096: fewer
-    // instructions for a byte, so that occupancy hides the latency)
-    if constexpr (V * sizeof(X) >= 4)
-        if (a.cols <= 16 * kBlockThreads && static_cast<long long>(a.rows) * a.cols >= kManyElements && (V * sizeof(X) < 32 || a.cols <= 8 * 32))
-            return a.cols <= 8 * 32 ? launch_forward_rows<X, V, 8>(a, device, stream) : launch_forward_rows<X, V, 16>(a, device, stream);
+    constexpr int kMost = V == 8 ? 32 : 8;       // elements that a thread may hold
     if (a.cols > 1024 * kMost) {
         k_ln_forward_long<X, V><<<a.rows, 1024, 0, stream>>>(a);
         return cudaGetLastError();
@@ -864,46 +876,56 @@ cudaError_t launch_forward(LnArgs a, int32_t device, cudaStream_t stream)
 }
 
 template <typename X>
-cudaError_t launch_forward_v(const LnArgs& a, int v, int32_t device, cudaStream_t stream)
+cudaError_t launch_forward(LnArgs a, const Access& access, int32_t device, cudaStream_t stream)
 {
-    if (v == 8) return launch_forward<X, 8>(a, device, stream);
-    if (v == 2) return launch_forward<X, 2>(a, device, stream);
-    return launch_forward<X, 1>(a, device, stream);
+    a.period = std::max(1, access.period);
+    const long long span = a.cols + (access.wide ? 0 : 7);
+    // Many rows, and a block holds them.  (Wide fp32 rows of more than 256 columns: a block per few rows is faster, 612 against
+    // 735 us at 128k x 4096: fewer instructions for a byte, so that occupancy hides the latency.)
+    if (access.period && span <= 16 * kBlockThreads && static_cast<long long>(a.rows) * a.cols >= kManyElements &&
+        !(access.wide && sizeof(X) == 4 && a.cols > 8 * 32)) {
+        if (access.wide) return span <= 8 * 32 ? launch_forward_rows<X, 8, false>(a, device, stream) : launch_forward_rows<X, 16, false>(a, device, stream);
+        return span <= 8 * 32 ? launch_forward_rows<X, 8, true>(a, device, stream) : launch_forward_rows<X, 16, true>(a, device, stream);
+    }
+    return access.wide ? launch_forward_once<X, 8>(a, stream) : launch_forward_once<X, 1>(a, stream);
 }
 
-template <typename X, typename G, int V, int E>
+template <typename X, typename G, int E, bool kSkew>
 cudaError_t launch_held(LnArgs a, const BackwardPlan& p, int32_t device, cudaStream_t stream)
 {
     static std::atomic<uint64_t> done{0};
-    auto* const kernel = k_ln_backward<X, G, V, E / V, E != 32>;
+    auto* const kernel = k_ln_backward<X, G, E / 8, E != 32, kSkew>;
     const cudaError_t e = allow_smem(kernel, kRingBytes, device, done);
     if (e != cudaSuccess) return e;
     a.tpr = p.tpr;
     a.stages = p.stages;
+    a.period = p.access.period;
     kernel<<<p.blocks, p.threads, p.smem, stream>>>(a);
     return cudaGetLastError();
 }
 
 template <typename X, typename G, int V>
-cudaError_t launch_backward(const LnArgs& a, const BackwardPlan& p, float2* means, int32_t device, cudaStream_t stream)
+cudaError_t launch_by_columns(const LnArgs& a, const BackwardPlan& p, float2* means, cudaStream_t stream)
 {
-    constexpr bool kAsync = Ring<X, G, V, 1>::kAsync;
-    if (p.held == 8) return launch_held<X, G, V, 8>(a, p, device, stream);
-    if constexpr (kAsync)
-        if (p.held == 16) return launch_held<X, G, V, 16>(a, p, device, stream);
-    if constexpr (V == 8)
-        if (p.held == 32) return launch_held<X, G, V, 32>(a, p, device, stream);
-    if (a.y) k_ln_backward_rows<X, G, V><<<a.rows, 1024, 0, stream>>>(a, means);
+    const int threads = std::min(1024, threads_per_row(a.cols, V));
+    if (a.y) k_ln_backward_rows<X, G, V><<<a.rows, threads, 0, stream>>>(a, means);
     k_ln_backward_columns<X, G, V><<<dim3(p.column_blocks, p.blocks), 256, 0, stream>>>(a, means);
     return cudaGetLastError();
 }
 
 template <typename X, typename G>
-cudaError_t launch_backward_v(const LnArgs& a, const BackwardPlan& p, float2* means, int32_t device, cudaStream_t stream)
+cudaError_t launch_backward(const LnArgs& a, const BackwardPlan& p, float2* means, int32_t device, cudaStream_t stream)
 {
-    if (p.v == 8) return launch_backward<X, G, 8>(a, p, means, device, stream);
-    if (p.v == 2) return launch_backward<X, G, 2>(a, p, means, device, stream);
-    return launch_backward<X, G, 1>(a, p, means, device, stream);
+    if (p.access.wide) {
+        if (p.held == 8) return launch_held<X, G, 8, false>(a, p, device, stream);
+        if (p.held == 16) return launch_held<X, G, 16, false>(a, p, device, stream);
+        if (p.held == 32) return launch_held<X, G, 32, false>(a, p, device, stream);
+        return launch_by_columns<X, G, 8>(a, p, means, stream);
+    }
+    if (p.held == 8) return launch_held<X, G, 8, true>(a, p, device, stream);
+    if (p.held == 16) return launch_held<X, G, 16, true>(a, p, device, stream);
+    if (p.held == 32) return launch_held<X, G, 32, true>(a, p, device, stream);
+    return launch_by_columns<X, G, 1>(a, p, means, stream);
 }
 
 LnArgs args_of(const came_layernorm& l, bool backward)
@@ -939,10 +961,10 @@ came_status came_layernorm_forward(const came_layernorm* l, int32_t device, void
     if ((s = require_current_device(device)) != CAME_OK) return s;
     if (l->rows == 0) return CAME_OK;
     const LnArgs a = args_of(*l, false);
-    const int v = access_of(*l, false);
+    const Access access = access_of(*l, false);
     const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = l->x_dtype == CAME_BF16 ? launch_forward_v<__nv_bfloat16>(a, v, device, stream)
-                                                  : launch_forward_v<float>(a, v, device, stream);
+    const cudaError_t e = l->x_dtype == CAME_BF16 ? launch_forward<__nv_bfloat16>(a, access, device, stream)
+                                                  : launch_forward<float>(a, access, device, stream);
     return e == cudaSuccess ? CAME_OK : report_cuda(e, "kernel launch");
 }
 
@@ -973,11 +995,11 @@ came_status came_layernorm_backward(const came_layernorm* l, void* workspace, in
     cudaError_t e = cudaSuccess;
     if (l->rows && (a.y || sums)) {
         if (l->x_dtype == CAME_BF16)
-            e = l->y_dtype == CAME_BF16 ? launch_backward_v<__nv_bfloat16, __nv_bfloat16>(a, p, means, device, stream)
-                                        : launch_backward_v<__nv_bfloat16, float>(a, p, means, device, stream);
+            e = l->y_dtype == CAME_BF16 ? launch_backward<__nv_bfloat16, __nv_bfloat16>(a, p, means, device, stream)
+                                        : launch_backward<__nv_bfloat16, float>(a, p, means, device, stream);
         else
-            e = l->y_dtype == CAME_BF16 ? launch_backward_v<float, __nv_bfloat16>(a, p, means, device, stream)
-                                        : launch_backward_v<float, float>(a, p, means, device, stream);
+            e = l->y_dtype == CAME_BF16 ? launch_backward<float, __nv_bfloat16>(a, p, means, device, stream)
+                                        : launch_backward<float, float>(a, p, means, device, stream);
     }
     if (e == cudaSuccess && sums && (l->rows || !(l->flags & CAME_LAYERNORM_ACCUMULATE))) {
         LnFinish f{a.part, l->dweight, l->dbias, l->rows ? p.blocks : 0, a.cols, a.w_bf16, (l->flags & CAME_LAYERNORM_ACCUMULATE) ? 1 : 0};

@@ -127,35 +127,65 @@ __device__ __forceinline__ void add_value(float& sum, const Vec<__nv_bfloat16, 8
     asm("add.rn.f32.bf16 %0, %1, %0;" : "+f"(sum) : "h"(h));
 }
 
-// Eight columns of a row, of which `left` are there; V elements per access.
-template <typename T, int V>
-__device__ __forceinline__ void load_row(Vec<T, 8>& to, const T* p, long long left)
-{
-    if constexpr (V == 8) {
-        if (left >= 8) to.load(p);
-    } else {
+// 256 columns of a row that starts anywhere, loaded in words of 4 bytes, side by side for the warp, and handed to the lanes
+// (eight columns each) through shared memory.  A word that reaches over an end of the row is loaded element by element; what
+// lies outside becomes zero.
+template <typename T>
+struct Words {
+    static constexpr int E = 4 / static_cast<int>(sizeof(T));            // elements of a word
+    static constexpr int W = 8 / E;                                      // words of a lane
+    static constexpr int kRoom = 32 * W + 4;                             // words of a row in shared memory
+    uint32_t w[W + (E > 1)];                                             // (bf16: one more for the row, lane 0's)
+
+    // 1 where the columns begin in the middle of a word
+    static __device__ __forceinline__ int skew(const T* p) { return E > 1 ? static_cast<int>(reinterpret_cast<uintptr_t>(p) >> 1 & 1) : 0; }
+    // `p`: the first column; the row has `before` columns in front of it and `left` from it on
+    __device__ __forceinline__ void load(const T* p, long long before, long long left)
+    {
+        const int lane = threadIdx.x & 31, s = skew(p);
 #pragma unroll
-        for (int k = 0; k < 8; k += V) {
-            Vec<T, V> v;
-#pragma unroll
-            for (int j = 0; j < Vec<T, V>::W; ++j) v.w[j] = 0u;
-            if (k < left) v.load(p + k);
-            if constexpr (V * sizeof(T) >= 4) {
-#pragma unroll
-                for (int j = 0; j < Vec<T, V>::W; ++j) to.w[k * sizeof(T) / 4 + j] = v.w[j];
-            } else {
-                if (k & 1) to.w[k >> 1] |= v.w[0] << 16;
-                else to.w[k >> 1] = v.w[0];
+        for (int k = 0; k < W + (E > 1); ++k) {
+            w[k] = 0u;
+            const int e = (lane + 32 * k) * E - s;
+            if (k == W && lane) continue;
+            if (e + before >= 0 && e + E <= left) {
+                asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[k]) : "l"(p + e));
+            } else if constexpr (E > 1) {
+                Vec<T, 1> v;
+                if (e + before >= 0 && e < left) v.load(p + e), w[k] = v.w[0];
+                else if (e + 1 + before >= 0 && e + 1 < left) v.load(p + e + 1), w[k] = v.w[0] << 16;
             }
         }
     }
-}
+    __device__ __forceinline__ void hand_over(uint32_t* room) const
+    {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int k = 0; k < W; ++k) room[lane + 32 * k] = w[k];
+        if constexpr (E > 1)
+            if (lane == 0) room[32 * W] = w[W];
+    }
+    static __device__ __forceinline__ void take(Vec<T, 8>& to, const uint32_t* room, int skew)
+    {
+        const uint32_t* const mine = room + W * (threadIdx.x & 31);
+#pragma unroll
+        for (int k = 0; k < W; k += 4) {
+            const uint4 x = *reinterpret_cast<const uint4*>(mine + k);
+            to.w[k] = x.x, to.w[k + 1] = x.y, to.w[k + 2] = x.z, to.w[k + 3] = x.w;
+        }
+        if constexpr (E > 1) {
+            const uint32_t behind = mine[W];
+#pragma unroll
+            for (int k = 0; k < W; ++k) to.w[k] = __funnelshift_r(to.w[k], k + 1 < W ? to.w[k + 1] : behind, 16 * skew);
+        }
+    }
+};
 
 // One warp: tile_rows rows (a multiple of 8) and 256 columns of a head, `batches` of the batch.  In a group of eight rows a lane's eight
 // columns meet fifteen diagonals; eight of these are complete for the lane when the group is done and go to the warp's line in
 // shared memory, the others are the next group's upper ones.  Lanes and groups that meet the same diagonal follow one
 // another in the warp's order, so the sums' order is fixed.
-template <typename T, int V, int M>
+template <typename T, bool kAligned, int M>
 __global__ void __launch_bounds__(kWarps * 32)
 k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ Buckets<M> buckets)
 {
@@ -170,13 +200,15 @@ k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ B
     const int h = blockIdx.y;
     if (unit >= units) return;
     float* const line = reinterpret_cast<float*>(dynamic) + warp * length;       // line[x]: the diagonal column - row = x - tr
+    // (rows that are not aligned: four rows on their way to the lanes)
+    uint32_t* const room = reinterpret_cast<uint32_t*>(dynamic) + kWarps * length + warp * 4 * Words<T>::kRoom;
     for (int x = lane; x < length; x += 32) line[x] = 0.f;
     __syncwarp();
     const long long tile = unit / a.batch_groups;
     const long long i0 = tile / a.column_tiles * tr, j0 = tile % a.column_tiles * kTileColumns;
     const long long n0 = unit % a.batch_groups * a.batches, n1 = min(a.batch, n0 + a.batches);
     const int rows = static_cast<int>(min(static_cast<long long>(tr), a.q - i0));
-    const long long left = a.k - j0 - 8 * lane;
+    const long long column = j0 + 8 * lane;
     auto flush = [&](const float* sums, int base) {      // eight diagonals of every lane, side by side
         float4* const to = reinterpret_cast<float4*>(line + base + 8 * lane);
         float4 x = to[0], y = to[1];
@@ -186,24 +218,47 @@ k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ B
         __syncwarp();
     };
     for (long long n = n0; n < n1; ++n) {
-        const T* p = static_cast<const T*>(a.data) + n * a.batch_stride + h * a.head_stride + i0 * a.q_stride + j0 + 8 * lane;
+        const T* row = static_cast<const T*>(a.data) + n * a.batch_stride + h * a.head_stride + i0 * a.q_stride;
         float sums[15];                  // sums[d + 7]: the diagonal d = column - row within the group
 #pragma unroll
         for (int d = 0; d < 15; ++d) sums[d] = 0.f;
         int base = tr;
         for (int r = 0; r < rows; r += 8, base -= 8) {
-            Vec<T, 8> v[8];
+            if constexpr (kAligned) {
+                Vec<T, 8> v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
+                for (int u = 0; u < 8; ++u) {
 #pragma unroll
-                for (int j = 0; j < Vec<T, 8>::W; ++j) v[u].w[j] = 0u;
-                if (r + u < rows && left > 0) load_row<T, V>(v[u], p + u * a.q_stride, left);
+                    for (int j = 0; j < Vec<T, 8>::W; ++j) v[u].w[j] = 0u;
+                    if (r + u < rows && column < a.k) v[u].load(row + u * a.q_stride + column);
+                }
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) add_value(sums[k - u + 7], v[u], k);
+            } else {
+#pragma unroll
+                for (int half = 0; half < 8; half += 4) {
+                    Words<T> v[4];
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const bool there = r + half + u < rows;
+                        v[u].load(row + (half + u) * a.q_stride + j0, there ? j0 : 0, there ? a.k - j0 : 0);
+                    }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) v[u].hand_over(room + u * Words<T>::kRoom);
+                    __syncwarp();
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        Vec<T, 8> x;
+                        Words<T>::take(x, room + u * Words<T>::kRoom, Words<T>::skew(row + (half + u) * a.q_stride + j0));
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) add_value(sums[k - (half + u) + 7], x, k);
+                    }
+                    __syncwarp();
+                }
             }
-            p += 8 * a.q_stride;
-#pragma unroll
-            for (int u = 0; u < 8; ++u)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) add_value(sums[k - u + 7], v[u], k);
+            row += 8 * a.q_stride;
             flush(sums + 7, base);
 #pragma unroll
             for (int d = 14; d >= 8; --d) sums[d] = sums[d - 8];
@@ -212,35 +267,42 @@ k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ B
         }
         flush(sums + 7, base);           // (sums[7] is zero: its place belongs to the group before)
     }
-    // Buckets, in the order of their diagonals: -(n - 1) .. 0 before the query, 1 .. n - 1 behind it.
+    // Buckets are intervals of diagonals: a lane adds a short one up, the warp a long one.
     const long long origin = j0 - i0 - offset_of(a) - tr;        // line[x] has key - query - offset = origin + x
+    constexpr long long kNone = 4 * kFar;
     float* const part = a.part + (h * units + unit) * a.buckets;
-    for (int b = lane; b < a.buckets; b += 32) part[b] = 0.f;
-    __syncwarp();
-    auto order = [&](long long relative) {
-        const int b = bucket_of(start, buckets.n, distance_of(relative, buckets.both));
-        return relative > 0 && buckets.both ? b : -b;
-    };
-    const int first = order(origin), last = order(origin + length - 1);
-    for (int o = first; o <= last; ++o) {
-        const int m = o < 0 ? -o : o;
-        const bool end = m == buckets.n - 1;
-        long long lo, hi;                // the bucket's interval of relative positions
-        if (o > 0) {
-            lo = start[m];
-            hi = end ? 2 * kFar + length : start[m + 1];
-        } else {
-            lo = end ? -2 * kFar - length : 1 - static_cast<long long>(start[m + 1]);
-            hi = 1 - static_cast<long long>(start[m]);
-            if (o == 0) hi = buckets.both ? 1 : 2 * kFar + length;
+    for (int b0 = 0; b0 < a.buckets; b0 += 32) {
+        const int b = b0 + lane;
+        int x0 = 0, x1 = 0;
+        if (b < a.buckets) {
+            const bool behind = b >= buckets.n;          // (only with buckets.both)
+            const int m = behind ? b - buckets.n : b;
+            const long long from = start[m], to = m == buckets.n - 1 ? kNone : start[m + 1];     // its distances [from, to)
+            long long lo, hi;
+            if (behind) {
+                lo = max(1ll, from);
+                hi = to;
+            } else {
+                lo = 1 - to;
+                hi = m == 0 && !buckets.both ? kNone : 1 - from;
+            }
+            x0 = static_cast<int>(max(0ll, min(static_cast<long long>(length), lo - origin)));
+            x1 = static_cast<int>(max(0ll, min(static_cast<long long>(length), hi - origin)));
         }
-        const int x0 = static_cast<int>(max(0ll, min(static_cast<long long>(length), lo - origin)));
-        const int x1 = static_cast<int>(max(0ll, min(static_cast<long long>(length), hi - origin)));
-        float s = 0.f;
-        for (int x = x0 + lane; x < x1; x += 32) s += line[x];
+        const bool large = x1 - x0 > 32;
+        float mine = 0.f;
+        if (!large)
+            for (int x = x0; x < x1; ++x) mine += line[x];
+        for (unsigned todo = __ballot_sync(0xffffffffu, large); todo; todo &= todo - 1) {
+            const int owner = __ffs(todo) - 1;
+            const int y0 = __shfl_sync(0xffffffffu, x0, owner), y1 = __shfl_sync(0xffffffffu, x1, owner);
+            float s = 0.f;
+            for (int x = y0 + lane; x < y1; x += 32) s += line[x];
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-        if (lane == 0) part[o > 0 ? buckets.n + m : m] = s;
+            for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+            if (lane == owner) mine = s;
+        }
+        if (b < a.buckets) part[b] = mine;
     }
 }
 
@@ -334,19 +396,16 @@ came_status validate_posbias(const came_posbias* p, bool backward)
     return CAME_OK;
 }
 
-struct BackwardPlan { int tile_rows, row_tiles, column_tiles, batches, batch_groups, v; long long units, bytes; };
+struct BackwardPlan { int tile_rows, row_tiles, column_tiles, batches, batch_groups; bool aligned; long long units, bytes; };
 
 // Rows of a tile, and batches for a warp: as large as leaves every SM about 32 warps, so that a diagonal's sums stay in
 // registers and shared memory for long.
 BackwardPlan plan_backward(const came_posbias& p)
 {
     BackwardPlan b = {};
-    b.v = 1;
-    for (int v : {8, 2}) {
-        const bool fits = p.k_len % v == 0 && (p.q_len <= 1 || p.q_stride % v == 0) && (p.heads == 1 || p.head_stride % v == 0) &&
-                          (p.batch <= 1 || p.batch_stride % v == 0) && aligned_to(p.data, v * dtype_bytes(p.data_dtype));
-        if (fits) { b.v = v; break; }
-    }
+    // 8 elements of every row and tile in one access
+    b.aligned = p.k_len % 8 == 0 && (p.q_len <= 1 || p.q_stride % 8 == 0) && (p.heads == 1 || p.head_stride % 8 == 0) &&
+                (p.batch <= 1 || p.batch_stride % 8 == 0) && aligned_to(p.data, 8 * dtype_bytes(p.data_dtype));
     const long long want = kSMs * 32;
     const long long columns = std::max<int64_t>(1, (p.k_len + kTileColumns - 1) / kTileColumns);
     b.tile_rows = 128;
@@ -414,10 +473,10 @@ cudaError_t launch_backward(const BiasArgs& a, const came_posbias& d, const Back
     Buckets<M> b;
     fill_buckets(d, b);
     const dim3 grid(static_cast<unsigned>((p.units + kWarps - 1) / kWarps), a.heads);
-    const size_t smem = sizeof(float) * kWarps * (p.tile_rows + kTileColumns);   // (12 KB at most)
-    if (p.v == 8) k_posbias_backward<T, 8, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
-    else if (p.v == 2) k_posbias_backward<T, 2, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
-    else k_posbias_backward<T, 1, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
+    // (45 KB at most)
+    const size_t smem = sizeof(float) * kWarps * (p.tile_rows + kTileColumns + (p.aligned ? 0 : 4 * Words<T>::kRoom));
+    if (p.aligned) k_posbias_backward<T, true, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
+    else k_posbias_backward<T, false, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
     return cudaGetLastError();
 }
 

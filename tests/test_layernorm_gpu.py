@@ -341,3 +341,46 @@ def test_many_rows_in_both_directions(env, rows, cols, extra, offset, dtype, out
     for got, terms in ((dw, g * h), (db, g)):
         tol = (rows / 148 + 70) * U * terms.abs().sum(0) + HALF[wdt] * terms.sum(0).abs() * (1 + HALF[wdt]) + 1e-40
         assert bool(((got.double() - terms.sum(0)).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("cols", [1001, 1002, 1004, 771, 100, 5003, 9001])
+@pytest.mark.parametrize("dtype,mixed", [("f32", False), ("bf16", False), ("bf16", True)])
+def test_contiguous_rows_of_odd_lengths(env, cols, dtype, mixed):
+    """Rows that begin at other places relative to an aligned address; whatever a tensor's neighbours in memory hold stays out of it."""
+    torch, binding = env
+    rows = 5 + (5 << 20) // cols
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    dt, gdt = _dt(torch, dtype), torch.float32 if mixed else _dt(torch, dtype)
+
+    def between(dt):                     # a tensor between NaN, starting at an aligned address
+        flat = torch.full((64 + rows * cols + 64,), float("nan"), dtype=dt, device="cuda")
+        view = flat[64:64 + rows * cols].view(rows, cols)
+        return flat, view
+    (fx, x), (fy, y), (fg, dy), (fd, dx) = between(dt), between(gdt), between(gdt), between(dt)
+    x.copy_(torch.randn(rows, cols, generator=gen, device="cuda"))
+    x[3], x[4, 0], x[0, -1] = float("inf"), float("nan"), float("inf")       # neighbours of rows 2, 3, 5 and 1
+    dy.copy_(torch.randn(rows, cols, generator=gen, device="cuda"))
+    w, b = torch.randn(cols, generator=gen, device="cuda"), torch.randn(cols, generator=gen, device="cuda")
+    _, mean, rstd = binding.layer_norm_forward(x, w, b, out=y)
+    good = torch.ones(rows, dtype=torch.bool, device="cuda")
+    good[[0, 3, 4]] = False
+    assert bool(y[good].isfinite().all()) and bool(y[~good].isnan().any(1).all())
+    _check_forward(torch, x[good], w, b, 1e-5, y[good], mean[good], rstd[good], "f32" if gdt == torch.float32 else "bf16")
+    binding.layer_norm_backward(dy, x, mean, rstd, w, grad_x=dx)
+    assert bool(dx[good].isfinite().all())
+    x[~good] = 1.0
+    _, mean, rstd = binding.layer_norm_forward(x, w, b, out=y)
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    binding.layer_norm_backward(dy, x, mean, rstd, w, grad_x=dx, grad_weight=dw, grad_bias=db)
+    for flat in (fx, fy, fg, fd):
+        assert bool(flat[:64].isnan().all()) and bool(flat[-64:].isnan().all())
+    g, r = dy.double(), rstd.double()[:, None]
+    h = (x.double() - mean.double()[:, None]) * r
+    d = g * w.double()
+    c1, c2 = d.mean(1, keepdim=True), (d * h).mean(1, keepdim=True)
+    want = r * (d - c1 - h * c2)
+    tol = r * (6 * U * (d.abs() + c1.abs() + (h * c2).abs()) + _chain(cols) * (d.abs().mean(1, keepdim=True) + h.abs() * (d * h).abs().mean(1, keepdim=True)))
+    tol = (tol + HALF[dtype] * want.abs()) * (1 + HALF[dtype]) + 1e-40
+    assert bool(((dx.double() - want).abs() <= tol).all())
+    for got, terms in ((dw, g * h), (db, g)):
+        assert bool(((got.double() - terms.sum(0)).abs() <= (rows / 148 + 70) * U * terms.abs().sum(0) + 1e-40).all())
