@@ -4,8 +4,8 @@
 //   dtable[b, h] = sum over (n, i, j) with that bucket of dout[n, h, i, j]
 //
 // Everything depends on j - i alone.  Forward: a block writes a tile of one head from a line of the tile's
-// diagonals in shared memory.  Backward: a warp adds up the diagonals of its tile in registers, going down the rows, and
-// the buckets, which are intervals of diagonals, at the end.
+// diagonals in shared memory.  Backward: a warp follows diagonals, whose sums stay in registers, and adds up the buckets,
+// which are intervals of diagonals, at the end.
 #include "came_vec.cuh"
 
 #include <algorithm>
@@ -17,7 +17,6 @@ using namespace came_ops;
 
 constexpr int kMostBuckets = 1024;
 constexpr int kSMs = 148;
-constexpr int kTileColumns = 256;        // backward: columns of a warp's tile, eight per lane
 constexpr int kWarps = 8;
 constexpr long long kFar = 1ll << 40;
 
@@ -38,8 +37,8 @@ struct BiasArgs {
     long long      q, k, batch, table_ld, batch_stride, head_stride, q_stride;
     int            heads, buckets, table_bf16;
     int            tile_rows, tile_vectors;          // forward
-    int            row_tiles, column_tiles, batches; // backward: tiles of a head, batches per warp
-    int            batch_groups;
+    long long      tiles;                // backward: tiles of diagonals, parts of a tile's rows, batches for a warp
+    int            chunks, batches, batch_groups;
     float*         part;                 // backward: [heads][units][buckets]
 };
 
@@ -127,148 +126,77 @@ __device__ __forceinline__ void add_value(float& sum, const Vec<__nv_bfloat16, 8
     asm("add.rn.f32.bf16 %0, %1, %0;" : "+f"(sum) : "h"(h));
 }
 
-// 256 columns of a row that starts anywhere, loaded in words of 4 bytes, side by side for the warp, and handed to the lanes
-// (eight columns each) through shared memory.  A word that reaches over an end of the row is loaded element by element; what
-// lies outside becomes zero.
-template <typename T>
-struct Words {
-    static constexpr int E = 4 / static_cast<int>(sizeof(T));            // elements of a word
-    static constexpr int W = 8 / E;                                      // words of a lane
-    static constexpr int kRoom = 32 * W + 4;                             // words of a row in shared memory
-    uint32_t w[W + (E > 1)];                                             // (bf16: one more for the row, lane 0's)
-
-    // 1 where the columns begin in the middle of a word
-    static __device__ __forceinline__ int skew(const T* p) { return E > 1 ? static_cast<int>(reinterpret_cast<uintptr_t>(p) >> 1 & 1) : 0; }
-    // `p`: the first column; the row has `before` columns in front of it and `left` from it on
-    __device__ __forceinline__ void load(const T* p, long long before, long long left)
-    {
-        const int lane = threadIdx.x & 31, s = skew(p);
-#pragma unroll
-        for (int k = 0; k < W + (E > 1); ++k) {
-            w[k] = 0u;
-            const int e = (lane + 32 * k) * E - s;
-            if (k == W && lane) continue;
-            if (e + before >= 0 && e + E <= left) {
-                asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[k]) : "l"(p + e));
-            } else if constexpr (E > 1) {
-                Vec<T, 1> v;
-                if (e + before >= 0 && e < left) v.load(p + e), w[k] = v.w[0];
-                else if (e + 1 + before >= 0 && e + 1 < left) v.load(p + e + 1), w[k] = v.w[0] << 16;
-            }
-        }
-    }
-    __device__ __forceinline__ void hand_over(uint32_t* room) const
-    {
-        const int lane = threadIdx.x & 31;
-#pragma unroll
-        for (int k = 0; k < W; ++k) room[lane + 32 * k] = w[k];
-        if constexpr (E > 1)
-            if (lane == 0) room[32 * W] = w[W];
-    }
-    static __device__ __forceinline__ void take(Vec<T, 8>& to, const uint32_t* room, int skew)
-    {
-        const uint32_t* const mine = room + W * (threadIdx.x & 31);
-#pragma unroll
-        for (int k = 0; k < W; k += 4) {
-            const uint4 x = *reinterpret_cast<const uint4*>(mine + k);
-            to.w[k] = x.x, to.w[k + 1] = x.y, to.w[k + 2] = x.z, to.w[k + 3] = x.w;
-        }
-        if constexpr (E > 1) {
-            const uint32_t behind = mine[W];
-#pragma unroll
-            for (int k = 0; k < W; ++k) to.w[k] = __funnelshift_r(to.w[k], k + 1 < W ? to.w[k + 1] : behind, 16 * skew);
-        }
-    }
-};
-
-// One warp: tile_rows rows (a multiple of 8) and 256 columns of a head, `batches` of the batch.  In a group of eight rows a lane's eight
-// columns meet fifteen diagonals; eight of these are complete for the lane when the group is done and go to the warp's line in
-// shared memory, the others are the next group's upper ones.  Lanes and groups that meet the same diagonal follow one
-// another in the warp's order, so the sums' order is fixed.
-template <typename T, bool kAligned, int M>
-__global__ void __launch_bounds__(kWarps * 32)
+// Rows of a head that are eight apart begin at the same place relative to an aligned address, whatever their stride is.  A warp takes
+// such rows, first + 8 m, and goes down them while its lanes go right, an aligned access of eight elements for a row: the
+// differences column - row of a lane's elements stay what they are, so that eight sums in registers are all it needs.  An
+// access v of a row covers the columns 8 v - skew to 8 v - skew + 7; lane l has the accesses with v - m = block + l.
+// The accesses that reach over an end of the row, one or two for a lane, are made afterwards, element by element.
+template <typename T, int M>
+__global__ void __launch_bounds__(kWarps * 32, sizeof(T) == 2 ? 4 : 2)
 k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ Buckets<M> buckets)
 {
-    extern __shared__ __align__(16) char dynamic[];
+    constexpr int length = 256;
+    __shared__ float lines[kWarps][length];
     __shared__ int start[M];
     release_dependents();
     for (int m = threadIdx.x; m < buckets.n; m += kWarps * 32) start[m] = buckets.start[m];
     __syncthreads();
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tr = a.tile_rows, length = tr + kTileColumns;
-    const long long units = static_cast<long long>(a.row_tiles) * a.column_tiles * a.batch_groups;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long units = 8ll * a.tiles * a.chunks * a.batch_groups;
     const long long unit = static_cast<long long>(blockIdx.x) * kWarps + warp;
     const int h = blockIdx.y;
     if (unit >= units) return;
-    float* const line = reinterpret_cast<float*>(dynamic) + warp * length;       // line[x]: the diagonal column - row = x - tr
-    // (rows that are not aligned: four rows on their way to the lanes)
-    uint32_t* const room = reinterpret_cast<uint32_t*>(dynamic) + kWarps * length + warp * 4 * Words<T>::kRoom;
-    for (int x = lane; x < length; x += 32) line[x] = 0.f;
-    __syncwarp();
-    const long long tile = unit / a.batch_groups;
-    const long long i0 = tile / a.column_tiles * tr, j0 = tile % a.column_tiles * kTileColumns;
+    const long long chunk = unit / a.batch_groups % a.chunks, tile = unit / a.batch_groups / a.chunks % a.tiles;
+    const int first = static_cast<int>(unit / a.batch_groups / a.chunks / a.tiles);
     const long long n0 = unit % a.batch_groups * a.batches, n1 = min(a.batch, n0 + a.batches);
-    const int rows = static_cast<int>(min(static_cast<long long>(tr), a.q - i0));
-    const long long column = j0 + 8 * lane;
-    auto flush = [&](const float* sums, int base) {      // eight diagonals of every lane, side by side
-        float4* const to = reinterpret_cast<float4*>(line + base + 8 * lane);
-        float4 x = to[0], y = to[1];
-        x.x += sums[0], x.y += sums[1], x.z += sums[2], x.w += sums[3];
-        y.x += sums[4], y.y += sums[5], y.z += sums[6], y.w += sums[7];
-        to[0] = x, to[1] = y;
-        __syncwarp();
-    };
+    const T* const head = static_cast<const T*>(a.data) + h * a.head_stride + first * a.q_stride;
+    // (the unit's batches begin at the same place)
+    const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(head + n0 * a.batch_stride) / sizeof(T) & 7);
+    const long long rows = (a.q - first + 7) >> 3, vectors = (a.k + skew + 7) >> 3;
+    const long long block = 32 * tile - (((a.q + 7) >> 3) - 1);
+    const long long low = max(0ll, -(block + 31)), high = min(rows, vectors - block);      // rows that meet the tile
+    const long long m0 = low + chunk * a.tile_rows, m1 = min(high, m0 + a.tile_rows);
+    const long long mine = block + lane;
+    float sums[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sums[k] = 0.f;
+    // rows for which this lane's access lies within the row
+    const long long whole0 = max(m0, (skew ? 1ll : 0ll) - mine), whole1 = min(m1, ((a.k + skew) >> 3) - mine);
     for (long long n = n0; n < n1; ++n) {
-        const T* row = static_cast<const T*>(a.data) + n * a.batch_stride + h * a.head_stride + i0 * a.q_stride;
-        float sums[15];                  // sums[d + 7]: the diagonal d = column - row within the group
+        const T* const here = head + n * a.batch_stride + 8 * mine - skew;       // row m's access: here + m step
+        const long long step = 8 * a.q_stride + 8;
+        const T* p = here + m0 * step;
+        for (long long m = m0; m < m1; m += 8, p += 8 * step) {
+            Vec<T, 8> v[8];
 #pragma unroll
-        for (int d = 0; d < 15; ++d) sums[d] = 0.f;
-        int base = tr;
-        for (int r = 0; r < rows; r += 8, base -= 8) {
-            if constexpr (kAligned) {
-                Vec<T, 8> v[8];
+            for (int u = 0; u < 8; ++u) {
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-#pragma unroll
-                    for (int j = 0; j < Vec<T, 8>::W; ++j) v[u].w[j] = 0u;
-                    if (r + u < rows && column < a.k) v[u].load(row + u * a.q_stride + column);
-                }
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) add_value(sums[k - u + 7], v[u], k);
-            } else {
-#pragma unroll
-                for (int half = 0; half < 8; half += 4) {
-                    Words<T> v[4];
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const bool there = r + half + u < rows;
-                        v[u].load(row + (half + u) * a.q_stride + j0, there ? j0 : 0, there ? a.k - j0 : 0);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) v[u].hand_over(room + u * Words<T>::kRoom);
-                    __syncwarp();
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        Vec<T, 8> x;
-                        Words<T>::take(x, room + u * Words<T>::kRoom, Words<T>::skew(row + (half + u) * a.q_stride + j0));
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) add_value(sums[k - (half + u) + 7], x, k);
-                    }
-                    __syncwarp();
-                }
+                for (int j = 0; j < Vec<T, 8>::W; ++j) v[u].w[j] = 0u;
+                if (m + u >= whole0 && m + u < whole1) v[u].load(p + u * step);
             }
-            row += 8 * a.q_stride;
-            flush(sums + 7, base);
 #pragma unroll
-            for (int d = 14; d >= 8; --d) sums[d] = sums[d - 8];
+            for (int u = 0; u < 8; ++u)
 #pragma unroll
-            for (int d = 0; d < 8; ++d) sums[d] = 0.f;
+                for (int k = 0; k < 8; ++k) add_value(sums[k], v[u], k);
         }
-        flush(sums + 7, base);           // (sums[7] is zero: its place belongs to the group before)
+        // the row's first access, where it begins in front of the row, and its last, where it ends behind it
+#pragma unroll 1
+        for (int side = 0; side < 2; ++side) {
+            const long long vector = side ? vectors - 1 : 0, m = vector - mine;
+            const bool part = side ? (a.k + skew) % 8 != 0 && (vector > 0 || !skew) : skew != 0;
+            if (!part || m < m0 || m >= m1) continue;
+            const long long column = 8 * vector - skew;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (column + k >= 0 && column + k < a.k) sums[k] += to_float(here[m * step + k]);
+        }
     }
+    float* const line = lines[warp];     // line[x]: the x-th of the tile's diagonals
+#pragma unroll
+    for (int k = 0; k < 8; ++k) line[8 * lane + k] = sums[k];
+    __syncwarp();
     // Buckets are intervals of diagonals: a lane adds a short one up, the warp a long one.
-    const long long origin = j0 - i0 - offset_of(a) - tr;        // line[x] has key - query - offset = origin + x
+    const long long origin = 8 * block - skew - first - offset_of(a);    // line[x] has key - query - offset = origin + x
     constexpr long long kNone = 4 * kFar;
     float* const part = a.part + (h * units + unit) * a.buckets;
     for (int b0 = 0; b0 < a.buckets; b0 += 32) {
@@ -396,28 +324,26 @@ came_status validate_posbias(const came_posbias* p, bool backward)
     return CAME_OK;
 }
 
-struct BackwardPlan { int tile_rows, row_tiles, column_tiles, batches, batch_groups; bool aligned; long long units, bytes; };
+struct BackwardPlan { int tile_rows, chunks, batches, batch_groups; long long tiles, units, bytes; };
 
-// Rows of a tile, and batches for a warp: as large as leaves every SM about 32 warps, so that a diagonal's sums stay in
-// registers and shared memory for long.
+// Rows that a warp goes down, and batches for a warp: as many as leave every SM about 32 warps.
 BackwardPlan plan_backward(const came_posbias& p)
 {
     BackwardPlan b = {};
-    // 8 elements of every row and tile in one access
-    b.aligned = p.k_len % 8 == 0 && (p.q_len <= 1 || p.q_stride % 8 == 0) && (p.heads == 1 || p.head_stride % 8 == 0) &&
-                (p.batch <= 1 || p.batch_stride % 8 == 0) && aligned_to(p.data, 8 * dtype_bytes(p.data_dtype));
-    const long long want = kSMs * 32;
-    const long long columns = std::max<int64_t>(1, (p.k_len + kTileColumns - 1) / kTileColumns);
+    const long long rows = std::max<long long>(1, (p.q_len + 7) / 8), vectors = std::max<long long>(1, (p.k_len + 14) / 8);
+    const long long batch = std::max<int64_t>(1, p.batch), want = kSMs * 32;
+    b.tiles = (rows - 1 + vectors + 31) / 32;
+    const long long tall = std::min(rows, vectors + 31);         // rows that meet a tile, at most
+    const long long all = 8 * b.tiles * p.heads;
     b.tile_rows = 128;
-    auto tiles = [&] { return columns * std::max<int64_t>(1, (p.q_len + b.tile_rows - 1) / b.tile_rows) * p.heads; };
-    while (b.tile_rows > 16 && tiles() * std::max<int64_t>(1, p.batch) < want) b.tile_rows /= 2;
-    b.column_tiles = static_cast<int>(columns);
-    b.row_tiles = static_cast<int>(std::max<int64_t>(1, (p.q_len + b.tile_rows - 1) / b.tile_rows));
-    const long long batch = std::max<int64_t>(1, p.batch);
-    const long long groups = std::min(batch, std::max(1ll, want / tiles()));
+    auto chunks = [&] { return (tall + b.tile_rows - 1) / b.tile_rows; };
+    while (b.tile_rows > 16 && all * chunks() * batch < want) b.tile_rows /= 2;
+    b.chunks = static_cast<int>(chunks());
+    // (a warp's batches begin at one place)
+    const long long groups = batch > 1 && p.batch_stride % 8 ? batch : std::min(batch, std::max(1ll, want / (all * b.chunks)));
     b.batches = static_cast<int>((batch + groups - 1) / groups);
     b.batch_groups = static_cast<int>((batch + b.batches - 1) / b.batches);
-    b.units = static_cast<long long>(b.row_tiles) * b.column_tiles * b.batch_groups;
+    b.units = 8 * b.tiles * b.chunks * b.batch_groups;
     b.bytes = b.units * p.heads * p.buckets * 4;
     return b;
 }
@@ -473,10 +399,7 @@ cudaError_t launch_backward(const BiasArgs& a, const came_posbias& d, const Back
     Buckets<M> b;
     fill_buckets(d, b);
     const dim3 grid(static_cast<unsigned>((p.units + kWarps - 1) / kWarps), a.heads);
-    // (45 KB at most)
-    const size_t smem = sizeof(float) * kWarps * (p.tile_rows + kTileColumns + (p.aligned ? 0 : 4 * Words<T>::kRoom));
-    if (p.aligned) k_posbias_backward<T, true, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
-    else k_posbias_backward<T, false, M><<<grid, kWarps * 32, smem, stream>>>(a, b);
+    k_posbias_backward<T, M><<<grid, kWarps * 32, 0, stream>>>(a, b);
     return cudaGetLastError();
 }
 
@@ -536,8 +459,8 @@ came_status came_posbias_backward(const came_posbias* p, void* workspace, int64_
     BiasArgs a = args_of(*p);
     a.part = static_cast<float*>(workspace);
     a.tile_rows = plan.tile_rows;
-    a.row_tiles = plan.row_tiles;
-    a.column_tiles = plan.column_tiles;
+    a.tiles = plan.tiles;
+    a.chunks = plan.chunks;
     a.batches = plan.batches;
     a.batch_groups = plan.batch_groups;
     cudaError_t e = cudaSuccess;
