@@ -105,6 +105,9 @@ __device__ __forceinline__ void store_columns(void* p, int is_bf16, long long ro
     store_as<8>(p, is_bf16, row + column, x);
 }
 
+// Backward: places for an eighth of a row's sums in shared memory (an odd number, for the banks).
+__host__ __device__ __forceinline__ int sums_width(int cols) { return ((cols + 7) >> 3) | 1; }
+
 __device__ __forceinline__ void group_barrier(int group, int tpr)
 {
     asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(tpr) : "memory");
@@ -451,7 +454,7 @@ __global__ void __launch_bounds__(kBlockThreads, 1)
 k_ln_backward(const __grid_constant__ LnArgs a)
 {
     constexpr int kX = 8 * static_cast<int>(sizeof(X)), kG = 8 * static_cast<int>(sizeof(G)), kStage = C * (kX + kG);
-    extern __shared__ __align__(16) char dynamic[];      // the ring; at the end the groups' sums: [2][cols]
+    extern __shared__ __align__(16) char dynamic[];      // the ring; at the end the groups' sums
     __shared__ float room[2][kBlockThreads / 32][2];
     release_dependents();
     const int tpr = a.tpr, groups = blockDim.x / tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
@@ -585,26 +588,37 @@ k_ln_backward(const __grid_constant__ LnArgs a)
         }
     }
     if (!a.part) return;
-    // the groups one after another, so that the order is theirs (their columns may lie at different threads: all of a group's
-    // columns belong to it, so that every sum meets every column once)
-    wait_all_but<0>(0);
-    float* const sums = reinterpret_cast<float*>(dynamic);
     float* const part = a.part + 2ll * blockIdx.x * a.cols;
-    for (int g = 0; g < groups; ++g) {
-        const bool last = g == groups - 1;
-        __syncthreads();
-        if (group != g) continue;
+    if (groups == 1) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int col = column(c) + k;
-                if (static_cast<unsigned>(col) >= static_cast<unsigned>(a.cols)) continue;
-                float p = dw[c][k], q = db[c][k];
-                if (g > 0) p += sums[col], q += sums[a.cols + col];
-                if (last) part[col] = p, part[a.cols + col] = q;
-                else sums[col] = p, sums[a.cols + col] = q;
-            }
+            for (int k = 0; k < 8; ++k)
+                if (!outside(c, k)) part[column(c) + k] = dw[c][k], part[a.cols + column(c) + k] = db[c][k];
+        return;
+    }
+    // Every group's sums side by side in shared memory, then added in the groups' order.  Column j is at (j mod 8) wide + j / 8: one
+    // of a thread's eight columns at a time, the threads' lie side by side.
+    wait_all_but<0>(0);
+    __syncthreads();
+    float* const sums = reinterpret_cast<float*>(dynamic);
+    const int wide = sums_width(a.cols), each = 8 * wide;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (outside(c, k)) continue;
+            const int col = column(c) + k, at = 2 * group * each + (col & 7) * wide + (col >> 3);
+            sums[at] = dw[c][k];
+            sums[at + each] = db[c][k];
+        }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.cols; i += blockDim.x) {
+        const int which = i >= a.cols, col = i - which * a.cols;
+        const float* const from = sums + which * each + (col & 7) * wide + (col >> 3);
+        float s = 0.f;
+        for (int g = 0; g < groups; ++g) s += from[2 * g * each];
+        part[i] = s;
     }
 }
 
@@ -822,10 +836,12 @@ BackwardPlan plan_backward(const came_layernorm& l)
         const int groups = std::max(1, kBlockThreads / p.tpr);
         p.threads = groups * p.tpr;
         const size_t stage = p.held * pair * p.threads, weights = p.held == 32 ? sizeof(float) * 32 * p.threads : 0;
-        p.stages = static_cast<int>(std::max<size_t>(2, std::min<size_t>(kMaxStages, (kRingBytes - weights) / stage)));
-        p.smem = std::max(weights + stage * p.stages, groups > 1 && sums ? sizeof(float) * 2 * l.cols : 0);
-        if (p.smem > kRingBytes) p.held = 0;
         p.blocks = blocks_for(l.rows, groups, 1, p.access.period);
+        // (no more places than a group has rows, and one)
+        const long long turns = l.rows / std::max(1, p.blocks * groups / p.access.period * p.access.period) + 2;
+        p.stages = static_cast<int>(std::max<long long>(2, std::min<long long>({kMaxStages, static_cast<long long>((kRingBytes - weights) / stage), turns})));
+        p.smem = std::max(weights + stage * p.stages, groups > 1 && sums ? sizeof(float) * 16 * groups * sums_width(static_cast<int>(l.cols)) : 0);
+        if (p.smem > kRingBytes) p.held = 0;
     }
     if (!p.held) {
         const int v = p.access.wide ? 8 : 1;
