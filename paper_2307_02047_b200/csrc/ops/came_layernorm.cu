@@ -193,22 +193,25 @@ __device__ __forceinline__ void wait_all_but(int n)      // N at most: the young
 
 // ---- forward ------------------------------------------------------------------------------------
 
-// C accesses of V elements per thread: the row's column (c tpr + thread) V.
-template <typename X, int V, int C>
+// R rows of a group at once, C accesses of V elements per thread: the row's column (c tpr + thread) V.
+template <typename X, int V, int C, int R>
 __global__ void __launch_bounds__(1024)
 k_ln_forward(const __grid_constant__ LnArgs a)
 {
     __shared__ float room[2][32][2];     // 32 warps at most, of all groups together; one set for each sum
     const int tpr = a.tpr, group = threadIdx.x / tpr, t = threadIdx.x - group * tpr;
-    const int row = blockIdx.x * (blockDim.x / tpr) + group;
+    const int row = (blockIdx.x * (blockDim.x / tpr) + group) * R;
     if (row >= a.rows) return;           // (the whole group)
     const int warp0 = group * (tpr >> 5);
-    const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
-    Vec<X, V> raw[C];
+    Vec<X, V> raw[R][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int col = (c * tpr + t) * V;
-        if (col < a.cols) raw[c].load(x + col);
+    for (int r = 0; r < R; ++r) {
+        const X* const x = static_cast<const X*>(a.x) + min(row + r, a.rows - 1) * a.x_ld;       // (a row that is not there: the last once more)
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = (c * tpr + t) * V;
+            if (col < a.cols) raw[r][c].load(x + col);
+        }
     }
     // (few elements per thread: the parameters are on their way while the sums are formed)
     constexpr bool kEarly = C * V <= 8;
@@ -221,47 +224,75 @@ k_ln_forward(const __grid_constant__ LnArgs a)
             if (a.b && col < a.cols) load_param<V>(a.b, a.w_bf16, col, b[c]);
         }
     }
-    float sum = 0.f;
+    float sums[2] = {0.f, 0.f}, squares[2] = {0.f, 0.f};
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        if ((c * tpr + t) * V < a.cols)
+    for (int r = 0; r < R; ++r) {
+        float even = 0.f, odd = 0.f;
 #pragma unroll
-            for (int k = 0; k < V; ++k) sum += raw[c].value(k);
-    const float mean = group_sum(sum, group, tpr, t >> 5, room[0] + warp0) * a.inv_cols;
-    float sq = 0.f;
+        for (int c = 0; c < C; ++c) {
+            if ((c * tpr + t) * V >= a.cols) continue;
+            if constexpr (V == 1) even += raw[r][c].value(0);
+            else
 #pragma unroll
-    for (int c = 0; c < C; ++c)
-        if ((c * tpr + t) * V < a.cols)
+                for (int k = 0; k < V; k += 2) add2(even, odd, raw[r][c].value(k), raw[r][c].value(k + 1));
+        }
+        sums[r] = even + odd;
+    }
+    group_sum(sums, group, tpr, t >> 5, room[0] + warp0);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float d = raw[c].value(k) - mean;
-                sq = fmaf(d, d, sq);
+    for (int r = 0; r < R; ++r) {
+        const float mean = sums[r] *= a.inv_cols;
+        float even = 0.f, odd = 0.f;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            if ((c * tpr + t) * V >= a.cols) continue;
+            if constexpr (V == 1) {
+                const float d = raw[r][c].value(0) - mean;
+                even = fmaf(d, d, even);
+            } else {
+#pragma unroll
+                for (int k = 0; k < V; k += 2) {
+                    float d = raw[r][c].value(k), e = raw[r][c].value(k + 1);
+                    add2(d, e, -mean, -mean);
+                    fma2(even, odd, d, e, d, e);
+                }
             }
-    sq = group_sum(sq, group, tpr, t >> 5, room[1] + warp0);
-    const float rstd = __frsqrt_rn(fmaf(sq, a.inv_cols, a.eps));
-    if (t == 0 && a.mean) {
-        a.mean[row] = mean;
-        a.rstd[row] = rstd;
+        }
+        squares[r] = even + odd;
+    }
+    group_sum(squares, group, tpr, t >> 5, room[1] + warp0);
+    float rstd[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        rstd[r] = __frsqrt_rn(fmaf(squares[r], a.inv_cols, a.eps));
+        if (t == 0 && a.mean && row + r < a.rows) {
+            a.mean[row + r] = sums[r];
+            a.rstd[row + r] = rstd[r];
+        }
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int col = (c * tpr + t) * V;
         if (col >= a.cols) continue;
         const int at = kEarly ? c : 0;
-        float y[V];
-#pragma unroll
-        for (int k = 0; k < V; ++k) y[k] = (raw[c].value(k) - mean) * rstd;
-        if (a.w) {
-            if constexpr (!kEarly) load_param<V>(a.w, a.w_bf16, col, w[0]);
-#pragma unroll
-            for (int k = 0; k < V; ++k) y[k] = __fmul_rn(y[k], w[at][k]);
+        if constexpr (!kEarly) {
+            if (a.w) load_param<V>(a.w, a.w_bf16, col, w[0]);
+            if (a.b) load_param<V>(a.b, a.w_bf16, col, b[0]);
         }
-        if (a.b) {
-            if constexpr (!kEarly) load_param<V>(a.b, a.w_bf16, col, b[0]);
 #pragma unroll
-            for (int k = 0; k < V; ++k) y[k] = __fadd_rn(y[k], b[at][k]);
+        for (int r = 0; r < R; ++r) {
+            if (row + r >= a.rows) continue;
+            float y[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) y[k] = __fmul_rn(__fadd_rn(raw[r][c].value(k), -sums[r]), rstd[r]);
+            if (a.w)
+#pragma unroll
+                for (int k = 0; k < V; ++k) y[k] = __fmul_rn(y[k], w[at][k]);
+            if (a.b)
+#pragma unroll
+                for (int k = 0; k < V; ++k) y[k] = __fadd_rn(y[k], b[at][k]);
+            store_as<V>(a.y, a.y_bf16, (row + r) * a.y_ld + col, y);
         }
-        store_as<V>(a.y, a.y_bf16, row * a.y_ld + col, y);
     }
 }
 
@@ -827,8 +858,12 @@ BackwardPlan plan_backward(const came_layernorm& l)
     const bool sums = l.dweight || l.dbias;
     const int64_t span = l.cols + (p.access.wide ? 0 : 7);       // columns, and the place of the first
     // elements of a row per thread (0: the row does not fit a block, or its tensors' rows begin at different places)
+    // 32 for bf16: the sums and barriers of a row are half as much for each element (128k x 4096: 526 us, 547 with 16; 512 columns 83
+    // and 75, 60000 x 1001 113 and 94); fp32 leaves too few places in the ring for it (65536 x 5120: 1068 and 663).
+    auto busy = [&](int held) { const int tpr = threads_per_row(span, held); return kBlockThreads / tpr * tpr >= kBlockThreads * 7 / 8; };
     if (!p.access.period) p.held = 0;
     else if (span <= 8 * 32) p.held = 8;
+    else if (pair <= 4 && span <= 32 * kBlockThreads && (p.access.wide ? l.cols > 512 : !busy(16) && busy(32))) p.held = 32;
     else if (span <= 16 * kBlockThreads) p.held = 16;
     else if (span <= 32 * kBlockThreads) p.held = 32;
     if (p.held) {
@@ -872,22 +907,29 @@ cudaError_t launch_forward_rows(LnArgs a, int32_t device, cudaStream_t stream)
     return cudaGetLastError();
 }
 
-template <typename X, int V>
-cudaError_t launch_forward_once(LnArgs a, cudaStream_t stream)
+template <typename X, int V, int C, int R>
+cudaError_t launch_forward_once(LnArgs a, int threads, cudaStream_t stream)
 {
-    constexpr int kMost = V == 8 ? 32 : 8;       // elements that a thread may hold
-    if (a.cols > 1024 * kMost) {
-        k_ln_forward_long<X, V><<<a.rows, 1024, 0, stream>>>(a);
-        return cudaGetLastError();
-    }
+    a.tpr = threads_per_row(a.cols, V * C);
+    const int groups = std::max(1, threads / a.tpr);
+    const long long at_once = static_cast<long long>(groups) * R;
+    k_ln_forward<X, V, C, R><<<static_cast<unsigned>((a.rows + at_once - 1) / at_once), groups * a.tpr, 0, stream>>>(a);
+    return cudaGetLastError();
+}
+
+template <typename X, int V>
+cudaError_t launch_forward_v(const LnArgs& a, cudaStream_t stream)
+{
     // Few rows: as many threads for each as there are accesses.  More rows: more elements for a thread.
-    const bool few = a.rows <= 2 * kSMs && a.cols <= 8 * 1024;
-    const int each = few ? 8 : kMost;
-    a.tpr = threads_per_row(a.cols, each);
-    const int groups = few ? 1 : std::max(1, 256 / a.tpr), threads = groups * a.tpr;
-    const unsigned blocks = static_cast<unsigned>((a.rows + groups - 1) / groups);
-    if (a.cols <= a.tpr * 8) k_ln_forward<X, V, 8 / V><<<blocks, threads, 0, stream>>>(a);
-    else k_ln_forward<X, V, kMost / V><<<blocks, threads, 0, stream>>>(a);
+    if (a.rows <= 2 * kSMs && a.cols <= 8 * 1024) return launch_forward_once<X, V, 8 / V, 1>(a, 0, stream);
+    if (a.cols <= (V == 8 ? 8 * 32 : 8 * 1024)) return launch_forward_once<X, V, 8 / V, 1>(a, 256, stream);
+    if constexpr (V == 8) {
+        // (two rows share the parameters and the barriers; rows beyond 8192 columns leave too few warps for that: 32768 rows of
+        // 16384 bf16 528 us, 605 in twos)
+        if (a.cols <= 16 * 512) return launch_forward_once<X, 8, 2, 2>(a, 256, stream);
+        if (a.cols <= 32 * 1024) return launch_forward_once<X, 8, 4, 1>(a, 256, stream);
+    }
+    k_ln_forward_long<X, V><<<a.rows, 1024, 0, stream>>>(a);
     return cudaGetLastError();
 }
 
@@ -896,14 +938,17 @@ cudaError_t launch_forward(LnArgs a, const Access& access, int32_t device, cudaS
 {
     a.period = std::max(1, access.period);
     const long long span = a.cols + (access.wide ? 0 : 7);
-    // Many rows, and a block holds them.  (Wide fp32 rows of more than 256 columns: a block per few rows is faster, 612 against
-    // 735 us at 128k x 4096: fewer instructions for a byte, so that occupancy hides the latency.)
-    if (access.period && span <= 16 * kBlockThreads && static_cast<long long>(a.rows) * a.cols >= kManyElements &&
-        !(access.wide && sizeof(X) == 4 && a.cols > 8 * 32)) {
-        if (access.wide) return span <= 8 * 32 ? launch_forward_rows<X, 8, false>(a, device, stream) : launch_forward_rows<X, 16, false>(a, device, stream);
-        return span <= 8 * 32 ? launch_forward_rows<X, 8, true>(a, device, stream) : launch_forward_rows<X, 16, true>(a, device, stream);
+    // Many rows, and a block holds them.  Not wide fp32 rows of more than 256 columns (a block per few rows is faster, 612 against
+    // 735 us at 128k x 4096: fewer instructions for a byte, so that occupancy hides the latency), nor wide ones that leave a
+    // block few threads (65536 x 5120 bf16: 316 against 377).
+    const bool many = static_cast<long long>(a.rows) * a.cols >= kManyElements, narrow = span <= 8 * 32;
+    const int tpr = threads_per_row(span, 16);
+    if (access.period && span <= 16 * kBlockThreads && many &&
+        (!access.wide || narrow || (sizeof(X) == 2 && kBlockThreads / tpr * tpr >= kBlockThreads * 7 / 8))) {
+        if (access.wide) return narrow ? launch_forward_rows<X, 8, false>(a, device, stream) : launch_forward_rows<X, 16, false>(a, device, stream);
+        return narrow ? launch_forward_rows<X, 8, true>(a, device, stream) : launch_forward_rows<X, 16, true>(a, device, stream);
     }
-    return access.wide ? launch_forward_once<X, 8>(a, stream) : launch_forward_once<X, 1>(a, stream);
+    return access.wide ? launch_forward_v<X, 8>(a, stream) : launch_forward_v<X, 1>(a, stream);
 }
 
 template <typename X, typename G, int E, bool kSkew>
