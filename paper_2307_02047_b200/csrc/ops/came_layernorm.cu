@@ -4,9 +4,14 @@
 //   dx = rstd (d - mean(d) - h mean(d h)),  d = dy w,  h = (x - mean) rstd
 //   dw = sum over rows of dy h,  db = sum over rows of dy
 //
-// A group of 32 to 1024 threads takes a row: it is read once and stays in registers, as stored, while its sums are
+// A group of 32 to 1024 threads takes a row: it is read once and stays in registers or shared memory while its sums are
 // formed.  In the backward pass a group goes from row to row and keeps, for its columns, the sums over its
 // rows in registers; blocks write those to the workspace, and a second, short grid adds them.
+//
+// fp32 is bound by the bytes (128k x 4096: forward 615 us, 7.0 TB/s; backward 935 us, 6.9 TB/s).  bf16 has half the bytes
+// for the same arithmetic: forward 402 us (5.3 TB/s, 0.82 of the measured copy rate), backward 547 us (5.9 TB/s), 584 under
+// a load that lowers the clock: about 17 and 22 instructions for an element, 60 % of what can be issued, which is
+// what arithmetic on pairs and two sums per exchange of a warp have left.
 #include "came_vec.cuh"
 
 #include <algorithm>
@@ -39,6 +44,20 @@ struct LnArgs {
     int         period;                  // rows until one begins at the same place relative to an aligned address
     int         w_bf16, y_bf16;
 };
+
+// Two fp32 in one 64-bit register: additions, products and multiply-adds of both at a time, half the instructions, each rounded
+// as ever.
+struct Two {
+    unsigned long long v;
+    __device__ __forceinline__ Two() {}
+    __device__ __forceinline__ Two(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+    __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+    __device__ __forceinline__ float sum() const { float a, b; get(a, b); return a + b; }
+};
+__device__ __forceinline__ Two operator+(Two a, Two b) { Two c; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(c.v) : "l"(a.v), "l"(b.v)); return c; }
+__device__ __forceinline__ Two operator*(Two a, Two b) { Two c; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(c.v) : "l"(a.v), "l"(b.v)); return c; }
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) { Two d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d.v) : "l"(a.v), "l"(b.v), "l"(c.v)); return d; }
+__device__ __forceinline__ Two both(float a) { return Two(a, a); }
 
 template <int V>
 __device__ __forceinline__ void load_param(const void* p, int is_bf16, int at, float (&out)[V])
@@ -88,6 +107,18 @@ __device__ __forceinline__ void load_columns(const void* p, int is_bf16, int col
     }
 }
 
+// Zero in the place of the columns that the row does not have.
+__device__ __forceinline__ void drop_outside(Two (&x)[4], int column, int cols)
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float a, b;
+        x[k].get(a, b);
+        x[k] = Two(static_cast<unsigned>(column + 2 * k) < static_cast<unsigned>(cols) ? a : 0.f,
+                   static_cast<unsigned>(column + 2 * k + 1) < static_cast<unsigned>(cols) ? b : 0.f);
+    }
+}
+
 template <bool kSkew>
 __device__ __forceinline__ void store_columns(void* p, int is_bf16, long long row, int column, int cols, const float (&x)[8])
 {
@@ -111,22 +142,6 @@ __host__ __device__ __forceinline__ int sums_width(int cols) { return ((cols + 7
 __device__ __forceinline__ void group_barrier(int group, int tpr)
 {
     asm volatile("bar.sync %0, %1;" :: "r"(group + 1), "r"(tpr) : "memory");
-}
-
-// Two additions, products or multiply-adds at a time: half the instructions, each rounded as ever.
-__device__ __forceinline__ void add2(float& a, float& b, float x, float y)
-{
-    asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; add.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
-}
-__device__ __forceinline__ void mul2(float& a, float& b, float x, float y)
-{
-    asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mul.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(a), "+f"(b) : "f"(x), "f"(y));
-}
-// (a, b) += (x, y) * (u, v)
-__device__ __forceinline__ void fma2(float& a, float& b, float x, float y, float u, float v)
-{
-    asm("{ .reg .b64 p, q, r; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mov.b64 r, {%4, %5}; fma.rn.f32x2 p, q, r, p; mov.b64 {%0, %1}, p; }"
-        : "+f"(a), "+f"(b) : "f"(x), "f"(y), "f"(u), "f"(v));
 }
 
 // The two sums v over a group's threads, the same in all of them.  The halves of a warp take one sum each after the first
@@ -227,38 +242,37 @@ k_ln_forward(const __grid_constant__ LnArgs a)
     float sums[2] = {0.f, 0.f}, squares[2] = {0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        float even = 0.f, odd = 0.f;
+        Two sum(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if ((c * tpr + t) * V >= a.cols) continue;
-            if constexpr (V == 1) even += raw[r][c].value(0);
+            if constexpr (V == 1) sum = sum + Two(raw[r][c].value(0), 0.f);
             else
 #pragma unroll
-                for (int k = 0; k < V; k += 2) add2(even, odd, raw[r][c].value(k), raw[r][c].value(k + 1));
+                for (int k = 0; k < V; k += 2) sum = sum + Two(raw[r][c].value(k), raw[r][c].value(k + 1));
         }
-        sums[r] = even + odd;
+        sums[r] = sum.sum();
     }
     group_sum(sums, group, tpr, t >> 5, room[0] + warp0);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const float mean = sums[r] *= a.inv_cols;
-        float even = 0.f, odd = 0.f;
+        Two sum(0.f, 0.f);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if ((c * tpr + t) * V >= a.cols) continue;
             if constexpr (V == 1) {
-                const float d = raw[r][c].value(0) - mean;
-                even = fmaf(d, d, even);
+                const Two d(raw[r][c].value(0) - mean, 0.f);
+                sum = fma(d, d, sum);
             } else {
 #pragma unroll
                 for (int k = 0; k < V; k += 2) {
-                    float d = raw[r][c].value(k), e = raw[r][c].value(k + 1);
-                    add2(d, e, -mean, -mean);
-                    fma2(even, odd, d, e, d, e);
+                    const Two d = Two(raw[r][c].value(k), raw[r][c].value(k + 1)) + both(-mean);
+                    sum = fma(d, d, sum);
                 }
             }
         }
-        squares[r] = even + odd;
+        squares[r] = sum.sum();
     }
     group_sum(squares, group, tpr, t >> 5, room[1] + warp0);
     float rstd[R];
@@ -329,7 +343,6 @@ k_ln_forward_rows(const __grid_constant__ LnArgs a)
     const int skew = kSkew ? rows.skew : 0;
     const long long other = kSkew ? a.period : 1, end = kSkew ? static_cast<long long>(a.rows - 1) * a.x_ld + a.cols : 0;
     auto column = [&](int c) { return (c * tpr + t) * 8 - skew; };
-    auto outside = [&](int c, int k) { return static_cast<unsigned>(column(c) + k) >= static_cast<unsigned>(a.cols); };
     auto partial = [&](int c) { return kSkew && (column(c) < 0 || column(c) + 8 > a.cols); };
     const uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
     auto place = [&](int stage, int r, int c) { return base + (((stage * 2 + r) * C + c) * blockDim.x + threadIdx.x) * kX; };
@@ -345,18 +358,21 @@ k_ln_forward_rows(const __grid_constant__ LnArgs a)
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     for (int k = 0; k < stages - 1; ++k) start(rows.first + k * rows.step, k);
-    float w[C][8], b[C][8];
+    Two w[C][4], b[C][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
+        float one[8], zero[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[c][k] = 1.f, b[c][k] = 0.f;
-        load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, w[c]);
-        load_columns<kSkew>(a.b, a.w_bf16, column(c), a.cols, b[c]);
+        for (int k = 0; k < 8; ++k) one[k] = 1.f, zero[k] = 0.f;
+        load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, one);
+        load_columns<kSkew>(a.b, a.w_bf16, column(c), a.cols, zero);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[c][k] = Two(one[2 * k], one[2 * k + 1]), b[c][k] = Two(zero[2 * k], zero[2 * k + 1]);
     }
     int stage = 0;
     for (long long row = rows.first; row < a.rows; row += rows.step) {
         wait_all_but<kMaxStages - 2>(stages - 2);
-        float x[2][C][8], sums[2][2] = {};
+        Two x[2][C][4], sums[2] = {both(0.f), both(0.f)};
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -365,35 +381,32 @@ k_ln_forward_rows(const __grid_constant__ LnArgs a)
                 if (column(c) >= a.cols) continue;
                 read_shared(place(stage, r, c), v.w);            // (a second row that is not there: whatever the ring holds; not written)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[r][c][k] = v.value(k);
-                if (partial(c))
+                for (int k = 0; k < 4; ++k) x[r][c][k] = Two(v.value(2 * k), v.value(2 * k + 1));
+                if (partial(c)) drop_outside(x[r][c], column(c), a.cols);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[r][c][k] = outside(c, k) ? 0.f : x[r][c][k];
-#pragma unroll
-                for (int k = 0; k < 8; k += 2) add2(sums[r][0], sums[r][1], x[r][c][k], x[r][c][k + 1]);
+                for (int k = 0; k < 4; ++k) sums[r] = sums[r] + x[r][c][k];
             }
-        float s[2] = {sums[0][0] + sums[0][1], sums[1][0] + sums[1][1]};
+        float s[2] = {sums[0].sum(), sums[1].sum()};
         // two rows into the place of the two before these (which have been read)
         start(row + (stages - 1) * rows.step, stage == 0 ? stages - 1 : stage - 1);
         stage = stage + 1 == stages ? 0 : stage + 1;
         group_sum(s, group, tpr, t >> 5, room[0] + warp0);
-        float squares[2][2] = {};
+        Two squares[2] = {both(0.f), both(0.f)};
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             s[r] *= a.inv_cols;
+            const Two minus = both(-s[r]);
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 if (column(c) >= a.cols) continue;
 #pragma unroll
-                for (int k = 0; k < 8; k += 2) add2(x[r][c][k], x[r][c][k + 1], -s[r], -s[r]);
-                if (partial(c))
+                for (int k = 0; k < 4; ++k) x[r][c][k] = x[r][c][k] + minus;
+                if (partial(c)) drop_outside(x[r][c], column(c), a.cols);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) x[r][c][k] = outside(c, k) ? 0.f : x[r][c][k];
-#pragma unroll
-                for (int k = 0; k < 8; k += 2) fma2(squares[r][0], squares[r][1], x[r][c][k], x[r][c][k + 1], x[r][c][k], x[r][c][k + 1]);
+                for (int k = 0; k < 4; ++k) squares[r] = fma(x[r][c][k], x[r][c][k], squares[r]);
             }
         }
-        float q[2] = {squares[0][0] + squares[0][1], squares[1][0] + squares[1][1]};
+        float q[2] = {squares[0].sum(), squares[1].sum()};
         group_sum(q, group, tpr, t >> 5, room[1] + warp0);
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
@@ -409,12 +422,7 @@ k_ln_forward_rows(const __grid_constant__ LnArgs a)
                 if (column(c) >= a.cols) continue;
                 float y[8];
 #pragma unroll
-                for (int k = 0; k < 8; k += 2) {
-                    float p = x[r][c][k], o = x[r][c][k + 1];
-                    y[k] = b[c][k], y[k + 1] = b[c][k + 1];
-                    mul2(p, o, rstd, rstd);
-                    fma2(y[k], y[k + 1], p, o, w[c][k], w[c][k + 1]);
-                }
+                for (int k = 0; k < 4; ++k) fma(x[r][c][k] * both(rstd), w[c][k], b[c][k]).get(y[2 * k], y[2 * k + 1]);
                 store_columns<kSkew>(a.y, a.y_bf16, here * a.y_ld, column(c), a.cols, y);
             }
         }
@@ -496,15 +504,18 @@ k_ln_backward(const __grid_constant__ LnArgs a)
     auto column = [&](int c) { return (c * tpr + t) * 8 - skew; };
     auto outside = [&](int c, int k) { return static_cast<unsigned>(column(c) + k) >= static_cast<unsigned>(a.cols); };
     auto partial = [&](int c) { return kSkew && (column(c) < 0 || column(c) + 8 > a.cols); };
-    float w[kHold ? C : 1][8], dw[C][8], db[C][8];
+    Two w[kHold ? C : 1][4], dw[C][4], db[C][4];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dw[c][k] = db[c][k] = 0.f;
+        for (int k = 0; k < 4; ++k) dw[c][k] = db[c][k] = both(0.f);
         if constexpr (kHold) {
+            float x[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) w[c][k] = 1.f;
-            load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, w[c]);
+            for (int k = 0; k < 8; ++k) x[k] = 1.f;
+            load_columns<kSkew>(a.w, a.w_bf16, column(c), a.cols, x);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[c][k] = Two(x[2 * k], x[2 * k + 1]);
         }
     }
     uint32_t base = static_cast<uint32_t>(__cvta_generic_to_shared(dynamic));
@@ -526,7 +537,7 @@ k_ln_backward(const __grid_constant__ LnArgs a)
         Vec<float, 8> v;
         read_shared(weights + c * blockDim.x * 32, v.w);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[0][k] = v.value(k);
+        for (int k = 0; k < 4; ++k) w[0][k] = Two(v.value(2 * k), v.value(2 * k + 1));
     };
     // (accesses of a warp lie side by side: stage, then access, then thread)
     auto x_at = [&](int stage, int c) { return base + stage * kStage * blockDim.x + (c * blockDim.x + threadIdx.x) * kX; };
@@ -549,27 +560,25 @@ k_ln_backward(const __grid_constant__ LnArgs a)
     if (rows.first < a.rows) mean = a.mean[rows.first], rstd = a.rstd[rows.first];
     int stage = 0, turn = 0;
     for (long long row = rows.first; row < a.rows; row += rows.step, turn ^= 1) {
-        float h[kHold ? C : 1][8], d[kHold ? C : 1][8];
-        float ds[2] = {}, dh[2] = {};    // sums of d and of d h
-        const float now_mean = mean, now_rstd = rstd;
+        Two h[kHold ? C : 1][4], d[kHold ? C : 1][4];
+        Two ds = both(0.f), dh = both(0.f);      // sums of d and of d h
+        const Two minus = both(-mean), now_rstd = both(rstd);
         const int now = stage;
         Vec<X, 8> vx;
         Vec<G, 8> vg;
         // h and dy of access c; nothing outside the row
-        auto take = [&](int c, float (&hh)[8], float (&g)[8]) {
+        auto take = [&](int c, Two (&hh)[4], Two (&g)[4]) {
             read_shared(x_at(now, c), vx.w);
             read_shared(g_at(now, c), vg.w);
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                hh[k] = vx.value(k), hh[k + 1] = vx.value(k + 1);
-                g[k] = vg.value(k), g[k + 1] = vg.value(k + 1);
-                add2(hh[k], hh[k + 1], -now_mean, -now_mean);
-                mul2(hh[k], hh[k + 1], now_rstd, now_rstd);
+            for (int k = 0; k < 4; ++k) {
+                hh[k] = (Two(vx.value(2 * k), vx.value(2 * k + 1)) + minus) * now_rstd;
+                g[k] = Two(vg.value(2 * k), vg.value(2 * k + 1));
             }
-            if (partial(c))
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    if (outside(c, k)) hh[k] = g[k] = 0.f;
+            if (partial(c)) {
+                drop_outside(hh, column(c), a.cols);
+                drop_outside(g, column(c), a.cols);
+            }
         };
         wait_all_but<kMaxStages - 2>(stages - 2);
         // the row after the ones on their way takes the place of the one before this (which has been read)
@@ -581,22 +590,21 @@ k_ln_backward(const __grid_constant__ LnArgs a)
             const int at = kHold ? c : 0;
             if (column(c) >= a.cols) continue;
             if constexpr (!kHold) weight_at(c);
-            float g[8];
+            Two g[4];
             take(c, h[at], g);
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                d[at][k] = g[k], d[at][k + 1] = g[k + 1];
-                mul2(d[at][k], d[at][k + 1], w[at][k], w[at][k + 1]);
-                fma2(dw[c][k], dw[c][k + 1], g[k], g[k + 1], h[at][k], h[at][k + 1]);
-                add2(db[c][k], db[c][k + 1], g[k], g[k + 1]);
-                add2(ds[0], ds[1], d[at][k], d[at][k + 1]);
-                fma2(dh[0], dh[1], d[at][k], d[at][k + 1], h[at][k], h[at][k + 1]);
+            for (int k = 0; k < 4; ++k) {
+                d[at][k] = g[k] * w[at][k];
+                dw[c][k] = fma(g[k], h[at][k], dw[c][k]);
+                db[c][k] = db[c][k] + g[k];
+                ds = ds + d[at][k];
+                dh = fma(d[at][k], h[at][k], dh);
             }
         }
         if (!a.y) continue;
-        float s[2] = {ds[0] + ds[1], dh[0] + dh[1]};
+        float s[2] = {ds.sum(), dh.sum()};
         group_sum(s, group, tpr, t >> 5, room[turn] + warp0);
-        const float c1 = s[0] * a.inv_cols, c2 = s[1] * a.inv_cols;
+        const Two c1 = both(-s[0] * a.inv_cols), c2 = both(-s[1] * a.inv_cols);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const int at = kHold ? c : 0;
@@ -606,15 +614,10 @@ k_ln_backward(const __grid_constant__ LnArgs a)
                 weight_at(c);
                 take(c, h[0], d[0]);
 #pragma unroll
-                for (int k = 0; k < 8; k += 2) mul2(d[0][k], d[0][k + 1], w[0][k], w[0][k + 1]);
+                for (int k = 0; k < 4; ++k) d[0][k] = d[0][k] * w[0][k];
             }
 #pragma unroll
-            for (int k = 0; k < 8; k += 2) {
-                o[k] = d[at][k], o[k + 1] = d[at][k + 1];
-                add2(o[k], o[k + 1], -c1, -c1);
-                fma2(o[k], o[k + 1], h[at][k], h[at][k + 1], -c2, -c2);
-                mul2(o[k], o[k + 1], now_rstd, now_rstd);
-            }
+            for (int k = 0; k < 4; ++k) (fma(h[at][k], c2, d[at][k] + c1) * now_rstd).get(o[2 * k], o[2 * k + 1]);
             store_columns<kSkew>(a.y, a.y_bf16, row * a.y_ld, column(c), a.cols, o);
         }
     }
@@ -624,8 +627,14 @@ k_ln_backward(const __grid_constant__ LnArgs a)
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (!outside(c, k)) part[column(c) + k] = dw[c][k], part[a.cols + column(c) + k] = db[c][k];
+            for (int k = 0; k < 8; k += 2) {
+                float p[2], q[2];
+                dw[c][k / 2].get(p[0], p[1]);
+                db[c][k / 2].get(q[0], q[1]);
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+                    if (!outside(c, k + j)) part[column(c) + k + j] = p[j], part[a.cols + column(c) + k + j] = q[j];
+            }
         return;
     }
     // Every group's sums side by side in shared memory, then added in the groups' order.  Column j is at (j mod 8) wide + j / 8: one
@@ -637,11 +646,17 @@ k_ln_backward(const __grid_constant__ LnArgs a)
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            if (outside(c, k)) continue;
-            const int col = column(c) + k, at = 2 * group * each + (col & 7) * wide + (col >> 3);
-            sums[at] = dw[c][k];
-            sums[at + each] = db[c][k];
+        for (int k = 0; k < 8; k += 2) {
+            float p[2], q[2];
+            dw[c][k / 2].get(p[0], p[1]);
+            db[c][k / 2].get(q[0], q[1]);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (outside(c, k + j)) continue;
+                const int col = column(c) + k + j, at = 2 * group * each + (col & 7) * wide + (col >> 3);
+                sums[at] = p[j];
+                sums[at + each] = q[j];
+            }
         }
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.cols; i += blockDim.x) {
@@ -858,12 +873,14 @@ BackwardPlan plan_backward(const came_layernorm& l)
     const bool sums = l.dweight || l.dbias;
     const int64_t span = l.cols + (p.access.wide ? 0 : 7);       // columns, and the place of the first
     // elements of a row per thread (0: the row does not fit a block, or its tensors' rows begin at different places)
-    // 32 for bf16: the sums and barriers of a row are half as much for each element (128k x 4096: 526 us, 547 with 16; 512 columns 83
-    // and 75, 60000 x 1001 113 and 94); fp32 leaves too few places in the ring for it (65536 x 5120: 1068 and 663).
+    // 32 for bf16 rows that one warp then holds, without a barrier (131072 x 768: 108 us, 127 with 16; 512 columns 83 and 75), and
+    // where 16 would leave the block few threads (65536 x 5120: 384 and 480).  Else 16: what 32 reads again costs more than its fewer
+    // barriers save (128k x 4096 under load: 584 us, 605 with 32).  fp32 leaves too few places in the ring for 32 (65536 x 5120:
+    // 1068 us, 663 with 16).
     auto busy = [&](int held) { const int tpr = threads_per_row(span, held); return kBlockThreads / tpr * tpr >= kBlockThreads * 7 / 8; };
     if (!p.access.period) p.held = 0;
     else if (span <= 8 * 32) p.held = 8;
-    else if (pair <= 4 && span <= 32 * kBlockThreads && (p.access.wide ? l.cols > 512 : !busy(16) && busy(32))) p.held = 32;
+    else if (pair <= 4 && span <= 32 * kBlockThreads && ((p.access.wide && l.cols > 512 && l.cols <= 1024) || (!busy(16) && busy(32)))) p.held = 32;
     else if (span <= 16 * kBlockThreads) p.held = 16;
     else if (span <= 32 * kBlockThreads) p.held = 32;
     if (p.held) {
