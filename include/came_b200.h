@@ -5,7 +5,9 @@
  * Confidence-guided Adaptive Memory Efficient Optimization", Algorithm 2) over a
  * list of parameter tensors resident on one GPU, and the operators of a training
  * step that stand next to it: the global gradient norm with clipping, the embedding
- * lookup and its gradient (further below, each with its formulas).
+ * lookup and its gradient, AdamW with states in 32 or 8 bits, layer norm and its
+ * backward pass, a learned relative position bias and its gradient (further below,
+ * each with its formulas).
  *
  * For a matrix parameter theta (n rows x m columns, row-major) with gradient g,
  * one step computes, in the notation of Algorithm 2 (all matrix squares,
@@ -583,7 +585,7 @@ typedef struct {
     const int64_t* device_offset;   /* DEVICE int64 [1], 8-byte aligned: the offset is read there by the
                                  kernels (for captured decoding); NULL: `offset`                  */
     int64_t        offset;    /* in [-2^40, 2^40] (what device_offset holds is clamped to that)   */
-    int64_t        q_len, k_len;    /* 0 .. 2^30                                                  */
+    int64_t        q_len, k_len;    /* 0 .. 2^30; forward: q_len up to 2^22 - 64                  */
     int64_t        batch;     /* backward: 0 .. 2^20                                              */
     int64_t        table_ld;  /* elements from bucket to bucket, heads .. 2^29                    */
     int64_t        batch_stride, head_stride, q_stride;   /* backward: >= 0, elements             */

@@ -917,8 +917,8 @@ class AdamWOptimizer:
         for name, x in given.items():
             if x is not None and len(x) != n:
                 raise CameError(CAME_ERR_SHAPE, f"{name} must be as many as params")
-        if (m is None) != (v is None):
-            raise CameError(CAME_ERR_NULL, "m and v belong together")
+        if (m is None) != (v is None) or (m is None and (m_scale is not None or v_scale is not None)):
+            raise CameError(CAME_ERR_NULL, "m and v belong together, and scales to them")
         first = self.params[0]
         _cuda_tensor(first, "params[0]")
         self.device, self.seed, self.step_count = first.device, seed, step_count
@@ -1221,7 +1221,10 @@ def _layer_norm_function():
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out_dtype=None):
     """``layer_norm_forward``'s y as part of autograd's graph (once differentiable): gradients of ``x``, ``weight`` and
-    ``bias``, each in its own type.  When nothing requires grad, or grad mode is off, y alone is computed."""
+    ``bias``, each in its own type.  When nothing requires grad, or grad mode is off, y alone is computed.
+
+    (Of autograd in general: before a backward pass is captured into a CUDA graph, eager graphs of the same leaves
+    have to be gone; torch ends the process otherwise.)"""
     if _torch().is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad)):
         return _layer_norm_function().apply(x, weight, bias, eps, out_dtype)
     return layer_norm_forward(x, weight, bias, eps, out_dtype=out_dtype, stats=False)

@@ -279,6 +279,27 @@ def test_another_stream_and_device_order(env):
     assert torch.equal(m, g)
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_than_two_to_the_31_elements(env, bits):
+    """The last elements are those of a small tensor whose blocks have the same numbers (the random bits go by them)."""
+    torch, binding = env
+    n, tail = (1 << 31) + 300, 300
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[-tail:] = torch.randn(tail, device="cuda").bfloat16()
+    opt = binding.AdamWOptimizer([p], [g], state_bits=bits, seed=4)
+    opt.step(lr=1e-2)
+    assert not p[:-tail].any()
+    m, v = ref.step(np.zeros(tail, np.float32), g[-tail:].float().cpu().numpy(), np.zeros(tail, np.float32), np.zeros(tail, np.float32), dict(HP, weight_decay=0.0), 1)[1:3]
+    if bits == 32:
+        assert np.array_equal(opt.m[0][-tail:].cpu().numpy(), m) and np.array_equal(opt.v[0][-tail:].cpu().numpy(), v)
+    else:                                # (2^31 is a multiple of 256: the tail begins a block)
+        r = ref.random_bits(tail, (1 << 31) // 256, 4, 1)
+        codes, scales = ref.encode(m, r & np.uint64(0xFFFF), ref.E4M3, 7, True)
+        assert np.array_equal(opt.m[0].view(torch.uint8)[-tail:].cpu().numpy(), codes) and np.array_equal(opt.m_scale[0].view(torch.uint8)[-2:].cpu().numpy(), scales)
+    want, _, _, tol = ref.step(np.zeros(tail, np.float32), g[-tail:].float().cpu().numpy(), np.zeros(tail, np.float32), np.zeros(tail, np.float32), dict(HP, weight_decay=0.0), 1)
+    assert (np.abs(p[-tail:].cpu().numpy() - want) <= tol).all()
+
+
 def test_refusals(env):
     torch, binding = env
     E = binding.CameError
@@ -288,7 +309,7 @@ def test_refusals(env):
             (lambda: new([], []), 2), (lambda: new([p], [g, g]), 2), (lambda: new([p.cpu()], [g]), 7), (lambda: new([p], [g.cpu()]), 7),
             (lambda: new([p.half()], [g]), 3), (lambda: new([p], [g.half()]), 3), (lambda: new([p], [g[:63]]), 2), (lambda: new([p], [p]), 12),
             (lambda: new([p[::2]], [g[:32]]), 11), (lambda: new([p], [g], state_bits=4), 3), (lambda: new([p], [g], state_bits=[8, 8]), 2),
-            (lambda: new([p], [g], m=[torch.zeros_like(p)]), 1), (lambda: new([p], [g], flags=[2]), 11), (lambda: new([p], [g], seed=-1), 5),
+            (lambda: new([p], [g], m=[torch.zeros_like(p)]), 1), (lambda: new([p], [g], state_bits=8, m_scale=[p]), 1), (lambda: new([p], [g], flags=[2]), 11), (lambda: new([p], [g], seed=-1), 5),
             (lambda: new([p, p[10:20]], [g, g[:10]]), 12), (lambda: new([p], [g], bf16_copy=[g]), 3),
             (lambda: new([p], [g], state_bits=8, m=[torch.zeros(64, device="cuda").to(torch.float8_e4m3fn)],
                          v=[torch.zeros(64, device="cuda").to(torch.float8_e5m2)]), 1)):
