@@ -524,9 +524,9 @@ came_status came_adamw_destroy(came_adamw_ctx* ctx);
  *             the terms in brackets with CAME_LAYERNORM_ACCUMULATE
  * Everything is computed in fp32 and rounded once to the stored type, to nearest even.  The variance is that of
  * the differences from the mean.  Sums are added in an order that depends on the sizes alone: results are
- * bit-reproducible.  Rows may have any stride >= cols and any element-aligned address (strides, lengths and
- * addresses that are multiples of 8 elements, 16 bytes at least, are faster); weight, bias and their gradients are
- * contiguous.  What is written shares memory with nothing else (CAME_ERR_OVERLAP; the ranges from a buffer's
+ * bit-reproducible.  Rows may have any stride >= cols and any element-aligned address (tensors of rows that
+ * begin at a multiple of 8 elements, and whose strides agree modulo 8, are faster); weight, bias and their gradients
+ * are contiguous.  What is written shares memory with nothing else (CAME_ERR_OVERLAP; the ranges from a buffer's
  * first to its last element count). */
 enum { CAME_LAYERNORM_ACCUMULATE = 1u << 0 };   /* backward: add to dweight and dbias */
 

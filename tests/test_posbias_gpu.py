@@ -1,9 +1,9 @@
 """The relative position bias bit for bit, and its gradient against the formula in 64 bits.
 
-A sum of N terms is formed in fp32: at most 8 terms in a register, then at most tile_rows / 8 = 16 times the batches of a warp
-in shared memory, at most (128 + 256) / 32 = 12 in a lane and 5 levels across it, units / 32 + 37 at the end.  For the sizes here (below 16
-batches for a warp and 4096 units) a term passes fewer than 8 + 16 * 16 + 17 + 128 + 37 < 512 additions: the error is below 512 u of the
-sum of magnitudes (u = 2^-24), plus half a step of the stored type."""
+A sum of N terms is formed in fp32: a diagonal's in one register, a term for each eighth row of a part of at most 128 such rows and for
+each batch of a warp, then at most 8 diagonals of a lane one after another and 5 levels across the warp (a short interval: 32 diagonals),
+units / 32 + 32 at the end.  For the sizes here (at most 3 batches, 1024 units) a term passes at most 3 * 128 + 32 + 64 additions,
+and no more than 512: the error is below 512 u of the sum of magnitudes (u = 2^-24), plus half a step of the stored type."""
 import pytest
 
 from tests.test_posbias_cpu import bucket
