@@ -7,8 +7,8 @@
 // where states have 8 bits.  Nothing crosses from one such block to the next, so there is one pass, one
 // launch for each type of state and gradient in the list, and no order that could change a result.
 //
-// Bound by the bytes: 355 M elements with fp32 states and gradients move 9.9 GB; 256 M with 8-bit states, bf16
-// gradients and bf16 copies 4.1 GB in 626 us (6.5 TB/s, the measured copy rate).  The 8-bit form computes about 70
+// Bound by the bytes: 355 M elements with fp32 states and gradients move 9.9 GB in 1450 us (6.8 TB/s); 256 M with 8-bit
+// states, bf16 gradients and bf16 copies 4.1 GB in 626 us (6.5 TB/s, the measured copy rate).  The 8-bit form computes about 70
 // instructions for an element, three quarters of what the SMs can issue in that time, a third of them for the random bits
 // and the rounding; one hash serves both states.
 #include "came_vec.cuh"

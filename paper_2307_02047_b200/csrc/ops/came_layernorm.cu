@@ -22,8 +22,8 @@ namespace {
 using namespace came_ops;
 
 constexpr int kSMs = 148;
-constexpr int kBlockThreads = 512;       // backward: threads of a block at most
-constexpr int kRingBytes = 200 << 10;    // backward: shared memory for rows on their way
+constexpr int kBlockThreads = 512;       // threads of a block whose groups go from row to row, at most
+constexpr int kRingBytes = 200 << 10;    // its shared memory for rows on their way
 constexpr int kMaxStages = 6;
 constexpr long long kManyElements = 4ll << 20;      // forward: from here on groups go from row to row
 
@@ -899,7 +899,9 @@ BackwardPlan plan_backward(const came_layernorm& l)
         const int v = p.access.wide ? 8 : 1;
         p.column_blocks = static_cast<int>((l.cols + 32 * v - 1) / (32 * v));
         const long long want = (l.rows + 7) / 8;
-        p.blocks = static_cast<int>(std::max(1ll, std::min<long long>(want, std::max(1, kSMs * 8 / p.column_blocks))));
+        // (and at most 512 rows one after another for a warp)
+        const long long blocks = std::max<long long>({1, kSMs * 8 / p.column_blocks, (l.rows + 4095) / 4096});
+        p.blocks = static_cast<int>(std::max(1ll, std::min({want, blocks, 65535ll})));
     }
     size_t at = 0;
     auto take = [&](size_t b) { const size_t here = at; at += (b + 255) / 256 * 256; return here; };

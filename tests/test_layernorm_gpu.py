@@ -384,3 +384,16 @@ def test_contiguous_rows_of_odd_lengths(env, cols, dtype, mixed):
     assert bool(((dx.double() - want).abs() <= tol).all())
     for got, terms in ((dw, g * h), (db, g)):
         assert bool(((got.double() - terms.sum(0)).abs() <= (rows / 148 + 70) * U * terms.abs().sum(0) + 1e-40).all())
+
+
+def test_sums_over_many_long_rows(env):
+    """Rows beyond a block, 9000 of them and all of one sign: a warp adds 512 at most one after another."""
+    torch, binding = env
+    rows, cols = 9000, 20000
+    x = torch.randn(rows, cols, device="cuda").bfloat16()
+    dy = torch.rand(rows, cols, device="cuda").bfloat16()
+    _, mean, rstd = binding.layer_norm_forward(x)
+    db = torch.empty(cols, device="cuda")
+    binding.layer_norm_backward(dy, x, mean, rstd, grad_bias=db, need_x=False)
+    want = sum(part.double().sum(0) for part in dy.split(1000))
+    assert bool(((db.double() - want).abs() <= (512 + 40) * U * want).all())
