@@ -132,12 +132,13 @@ __device__ __forceinline__ unsigned encode8(const float (&x)[8], const unsigned 
     }
     const int e = max(static_cast<int>(top >> 23) - F::kTop, 0);
     // One factor scales and lowers the exponent: 2^(127 - e - kLow), also where it is subnormal.  Of blocks whose values are
-    // so large that it would vanish, a part of it is taken first (what that loses is far below every code).
+    // so large that it would vanish, 2^-96 is taken first, which leaves at least 2^-144 (e4m3, e = 247) for the largest fp32.  What
+    // that loses are values below 2^-30 in a block whose codes' last random bit is worth 2^5 or more.
     int power = 254 - e - F::kLow;
     float first = 1.f;
     if (power < -22) {
-        first = 0x1p-64f;
-        power += 64;
+        first = 0x1p-96f;
+        power += 96;
     }
     const float factor = power_of_two(power);
     uint32_t c[8];                                       // codes in the upper byte

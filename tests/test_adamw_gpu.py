@@ -326,3 +326,19 @@ def test_refusals(env):
             opt.step(**kw)
         assert e.value.status == status, (kw, e.value)
     assert opt.step_count == 0 and not p.any()
+
+
+@pytest.mark.parametrize("gdt", ["f32", "bf16"])
+def test_blocks_of_large_values(env, gdt):
+    """Blocks of m up to 1e38 and of v up to 9e35 (larger gradients' squares overflow), whose scales lie at the end of their range."""
+    sizes = [1e17, 1e18, 5e18, 1e19, 1.7e19, 1e20, 1e29, 1e30, 1e31, 1e33, 1e36, 3e38]
+    pair = Pair(env, [256 * len(sizes) + 300], [0], gdt, 8)
+    for _ in range(3):
+        pair.new_gradients()
+        for i, size in enumerate(sizes + [1e30]):        # (and a short block)
+            part = pair.g[0][256 * i:256 * (i + 1)] if i < len(sizes) else pair.g[0][-40:]
+            x = size * pair.rng.uniform(0.25, 1.0, part.numel()) * pair.rng.choice([-1.0, 1.0], part.numel())
+            part.copy_(pair.torch.from_numpy(x.astype(np.float32)))
+        pair.check_step()
+        # a code of at least half of the block's largest is there: nothing has vanished
+        assert all(int((pair.bytes_of(pair.m[0])[256 * i:256 * (i + 1)] & 127).max()) >= 0x70 for i in range(len(sizes)))
