@@ -149,7 +149,7 @@ __device__ __forceinline__ unsigned encode8(const float (&x)[8], const unsigned 
         if constexpr (F::kSigned) {
             c[k] = ((s << (24 - F::kDrop)) & 0x7f000000u) | (__float_as_uint(x[k]) & 0x80ffffffu);
         } else {
-            s = max(s, min(__float_as_uint(x[k]), 1u << F::kDrop));      // not zero: not stored as zero
+            if (x[k] > 0.f) s = max(s, 1u << F::kDrop);          // not zero (subnormal values neither): not stored as zero
             c[k] = s << (24 - F::kDrop);
         }
     }

@@ -342,3 +342,16 @@ def test_blocks_of_large_values(env, gdt):
         pair.check_step()
         # a code of at least half of the block's largest is there: nothing has vanished
         assert all(int((pair.bytes_of(pair.m[0])[256 * i:256 * (i + 1)] & 127).max()) >= 0x70 for i in range(len(sizes)))
+
+
+@pytest.mark.parametrize("gdt", ["f32", "bf16"])
+def test_subnormal_second_moments_beside_larger_ones(env, gdt):
+    """A v above zero is stored as something above zero, also where it is a subnormal number (here 2e-41 to 4e-40)."""
+    pair = Pair(env, [1024, 300], [0, 0], gdt, 8)
+    for _ in range(3):
+        pair.new_gradients()
+        for g in pair.g:
+            x = pair.rng.uniform(1.5e-19, 6e-19, g[3::7].numel()) * pair.rng.choice([-1.0, 1.0], g[3::7].numel())
+            g[3::7] = pair.torch.from_numpy(x.astype(np.float32)).to(device=g.device, dtype=g.dtype)
+        pair.check_step()
+        assert all((pair.bytes_of(v)[3::7] > 0).all() for v in pair.v)
