@@ -444,8 +444,9 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
  *   m = fl(fl(beta1 m) + fl((1-beta1) g))         v = fl(fl(beta2 v) + fl((1-beta2) fl(g g)))
  *   p = p - (lr wd p + lr m / (1-beta1^t) / (sqrt(v / (1-beta2^t)) + eps))
  * beta, 1-beta are rounded to fp32 once (1-beta formed in double).  The update uses m and v as they are
- * here, whatever they are stored in; the root and the quotient are approximations good to 2^-22 each.
- * A root, or a sum of root and eps, below 2^-126 counts as zero: with eps = 0 that divides by zero.
+ * here, whatever they are stored in; eps is taken as fp32.  The root and the quotient are approximations good to 2^-22 each; a v
+ * below 2^-126 may count as zero where that changes the sum of root and eps by less than 2^-24 of it.  A sum below 2^-126 (v is
+ * zero, and eps zero or nearly so) counts as zero and divides by zero; one above 2^126 counts as infinite.
  *
  * States of 8 bits (state_bits = 8): every 256 consecutive elements of a tensor (the last block may be
  * shorter) share one byte e_m and one byte e_v, and

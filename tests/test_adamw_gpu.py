@@ -355,3 +355,17 @@ def test_subnormal_second_moments_beside_larger_ones(env, gdt):
             g[3::7] = pair.torch.from_numpy(x.astype(np.float32)).to(device=g.device, dtype=g.dtype)
         pair.check_step()
         assert all((pair.bytes_of(v)[3::7] > 0).all() for v in pair.v)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-20, 1e-15, 5.7e-11, 5.8e-11])
+def test_small_gradients_with_a_smaller_eps(env, bits, eps):
+    """Gradients of 1e-20 to 1e-17: their second moments are subnormal numbers in the first steps, and count, with eps on both sides
+    of the border from which on they are left out."""
+    pair = Pair(env, [1024, 77], [0, 0], "f32", bits)
+    for _ in range(3):
+        for g in pair.g:
+            x = 10.0 ** pair.rng.uniform(-20, -17, g.numel()) * pair.rng.choice([-1.0, 1.0], g.numel())
+            g.copy_(pair.torch.from_numpy(x.astype(np.float32)))
+        pair.check_step(dict(HP, eps=eps))
+        assert all(bool(p.isfinite().all()) for p in pair.p)
