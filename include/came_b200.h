@@ -572,7 +572,8 @@ came_status came_layernorm_backward(const came_layernorm* l, void* workspace, in
  *   bucket = d                                                              for d < E
  *            min(n - 1, E + floor((n - E) log(d / E) / log(max_distance / E)))     else
  * where a d at a border belongs above it (the borders are found once per call and compared in
- * whole numbers).  Sums are formed in fp32, in an order that depends on the sizes alone:
+ * whole numbers).  Sums are formed in fp32 by at most 512 additions of a diagonal's terms one after another, 32 of a bucket's
+ * diagonals and 16 of such sums, from there on in fp64, and rounded once, in an order that depends on the sizes alone:
  * results are bit-reproducible.  What is written shares memory with nothing that is read (CAME_ERR_OVERLAP). */
 enum {
     CAME_POSBIAS_BIDIRECTIONAL = 1u << 0,

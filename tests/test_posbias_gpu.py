@@ -185,3 +185,17 @@ def test_refusals(env):
         with pytest.raises(binding.CameError) as e:
             bad()
         assert e.value.status == status, e.value
+
+
+@pytest.mark.parametrize("dt,heads,q,k,batch,expanded", [("f32", 64, 64, 64, 65536, True), ("f32", 64, 512, 520, 300, True), ("f32", 12, 333, 517, 257, True),
+                                                         ("f32", 1, 100, 90, 40000, True), ("f32", 1, 99, 91, 40001, False), ("bf16", 2, 63, 200, 3000, False)])
+def test_large_batches_of_one_sign(env, dt, heads, q, k, batch, expanded):
+    """Sums of equal numbers, whose roundings all go one way: at most 512 additions in a row for a lane's diagonal, 32 for the diagonals
+    of a bucket, 16 for the warps' sums, then 64 bits, and the rounding at the end: 561 u of the sum."""
+    torch, binding = env
+    one = torch.full((1, heads, q, k), 0.1, device="cuda").to(_dt(torch, dt))
+    dout = one.expand(batch, -1, -1, -1) if expanded else one.repeat(batch, 1, 1, 1)
+    grad = binding.position_bias_backward(dout, torch.empty(32, heads, device="cuda"))
+    count = torch.bincount(_buckets(torch, q, k, 0, 32, 128, True).view(-1), minlength=32).double()
+    want = (count * batch * float(one[0, 0, 0, 0]))[:, None].expand(-1, heads)
+    assert bool(((grad.double() - want).abs() <= 561 * U * want).all()), float(((grad.double() - want).abs() / want.clamp(min=1e-9)).max()) / U
