@@ -39,7 +39,7 @@ struct BiasArgs {
     int            heads, buckets, table_bf16;
     int            tile_rows, tile_vectors;          // forward
     long long      tiles;                // backward: tiles of diagonals, parts of a tile's rows, batches for a warp
-    int            chunks, batches, batch_groups;
+    int            chunks, batches, batch_groups, period;
     float*         part;                 // backward: [heads][units][buckets]
 };
 
@@ -151,9 +151,10 @@ k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ B
     // (the warps of a block: the eight places, neighbouring rows)
     const int first = static_cast<int>(unit % 8);
     const long long group = unit / 8, chunk = group / a.batch_groups % a.chunks, tile = group / a.batch_groups / a.chunks;
-    const long long n0 = group % a.batch_groups * a.batches, n1 = min(a.batch, n0 + a.batches);
+    const int part_of_batch = static_cast<int>(group % a.batch_groups), place = part_of_batch % a.period;
+    const long long n0 = place + static_cast<long long>(part_of_batch - place) * a.batches, n1 = min(a.batch, n0 + static_cast<long long>(a.period) * a.batches);
     const T* const head = static_cast<const T*>(a.data) + h * a.head_stride + first * a.q_stride;
-    // (the unit's batches begin at the same place)
+    // (the unit's batches, n0, n0 + period, ..., begin at the same place)
     const int skew = static_cast<int>(reinterpret_cast<uintptr_t>(head + n0 * a.batch_stride) / sizeof(T) & 7);
     const long long rows = (a.q - first + 7) >> 3, vectors = (a.k + skew + 7) >> 3;
     const long long block = 32 * tile - (((a.q + 7) >> 3) - 1);
@@ -170,7 +171,7 @@ k_posbias_backward(const __grid_constant__ BiasArgs a, const __grid_constant__ B
     for (int k = 0; k < 8; ++k) sums[k] = 0.f;
     // rows for which this lane's access lies within the row
     const long long whole0 = max(m0, (skew ? 1ll : 0ll) - mine), whole1 = min(m1, ((a.k + skew) >> 3) - mine);
-    for (long long n = n0; n < n1; ++n) {
+    for (long long n = n0; n < n1; n += a.period) {
         const T* const here = head + n * a.batch_stride + 8 * mine - skew;       // row m's access: here + m step
         const long long step = 8 * a.q_stride + 8;
         const T* p = here + m0 * step;
@@ -341,7 +342,7 @@ came_status validate_posbias(const came_posbias* p, bool backward)
     return CAME_OK;
 }
 
-struct BackwardPlan { int tile_rows, chunks, batches, batch_groups; long long tiles, units, bytes; };
+struct BackwardPlan { int tile_rows, chunks, batches, batch_groups, period; long long tiles, units, bytes; };
 
 // Rows that a warp goes down, and batches for a warp: as many as leave every SM about 32 warps.
 BackwardPlan plan_backward(const came_posbias& p)
@@ -356,12 +357,15 @@ BackwardPlan plan_backward(const came_posbias& p)
     auto chunks = [&] { return (tall + b.tile_rows - 1) / b.tile_rows; };
     while (b.tile_rows > 16 && all * chunks() * batch < want) b.tile_rows /= 2;
     b.chunks = static_cast<int>(chunks());
-    // (a warp's batches begin at one place)
-    const long long groups = batch > 1 && p.batch_stride % 8 ? batch : std::min(batch, std::max(1ll, want / (all * b.chunks)));
+    // A warp's batches begin at one place: every period-th one.
+    b.period = 1;
+    while (b.period < batch && b.period * p.batch_stride % 8) b.period *= 2;
+    b.period = static_cast<int>(std::min<long long>(b.period, batch));
+    const long long count = (batch + b.period - 1) / b.period, turns = std::min(count, std::max(1ll, want / (all * b.chunks) / b.period));
     // (and as few that a lane adds kMostAdditions terms of a diagonal at most one after another)
     const long long most = std::max(1ll, kMostAdditions / std::min<long long>(b.tile_rows, tall));
-    b.batches = static_cast<int>(std::min(most, (batch + groups - 1) / groups));
-    b.batch_groups = static_cast<int>((batch + b.batches - 1) / b.batches);
+    b.batches = static_cast<int>(std::min(most, (count + turns - 1) / turns));
+    b.batch_groups = static_cast<int>((count + b.batches - 1) / b.batches * b.period);
     b.units = 8 * b.tiles * b.chunks * b.batch_groups;
     b.bytes = b.units * p.heads * p.buckets * 4;
     return b;
@@ -482,6 +486,7 @@ came_status came_posbias_backward(const came_posbias* p, void* workspace, int64_
     a.chunks = plan.chunks;
     a.batches = plan.batches;
     a.batch_groups = plan.batch_groups;
+    a.period = plan.period;
     cudaError_t e = cudaSuccess;
     const bool small = p->data_dtype == CAME_BF16;
     if (!empty && few_buckets(*p))

@@ -84,3 +84,12 @@ def test_without_gpu_reports_device_error():
             with pytest.raises(binding.CameError) as e:
                 call(_p(**over))
             assert e.value.status == 7
+
+
+@pytest.mark.parametrize("heads,q,k", [(1, 1, 1), (64, 1, 5), (4, 65, 63), (2, 301, 303)])
+def test_workspace_of_batches_at_odd_strides(heads, q, k):
+    """Batches begin at one of eight places: eight times the sums at most of batches that all begin at one."""
+    for batch in (1, 5, 100, 1 << 20):
+        sizes = [binding.came_posbias_workspace(_p(heads=heads, table_ld=heads, q_len=q, k_len=k, q_stride=k, head_stride=q * k, batch=batch, table=1 << 50,
+                                                   batch_stride=stride)) for stride in (-(-heads * q * k // 8) * 8, -(-heads * q * k // 8) * 8 + 1)]
+        assert sizes[1] <= 8 * sizes[0]
