@@ -523,8 +523,8 @@ came_status came_adamw_destroy(came_adamw_ctx* ctx);
  *   backward  h = (x - mean) rstd,  d = dy w,  dx = rn(rstd (d - sum d / cols - h sum (d h) / cols))
  *             dweight = rn([dweight +] sum over rows of dy h),  dbias = rn([dbias +] sum over rows of dy)
  *             the terms in brackets with CAME_LAYERNORM_ACCUMULATE
- * Everything is computed in fp32 and rounded once to the stored type, to nearest even; a sum over rows adds up to
- * max(512, rows / 144) terms one after another before it goes on by tree.  The variance is that of
+ * Everything is computed in fp32 and rounded once to the stored type, to nearest even; a sum over a row adds up to
+ * 264 + cols / 2^18 terms one after another, one over rows max(512, rows / 144), before it goes on by tree.  The variance is that of
  * the differences from the mean.  Sums are added in an order that depends on the sizes alone: results are
  * bit-reproducible.  Rows may have any stride >= cols and any element-aligned address (tensors of rows that
  * begin at a multiple of 8 elements, and whose strides agree modulo 8, are faster); weight, bias and their gradients

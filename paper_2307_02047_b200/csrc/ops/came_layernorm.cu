@@ -25,6 +25,7 @@ constexpr int kSMs = 148;
 constexpr int kBlockThreads = 512;       // threads of a block whose groups go from row to row, at most
 constexpr int kRingBytes = 200 << 10;    // its shared memory for rows on their way
 constexpr int kMaxStages = 6;
+constexpr int kRun = 256;                // rows longer than a block: additions of a thread one after another
 constexpr long long kManyElements = 4ll << 20;      // forward: from here on groups go from row to row
 
 struct LnArgs {
@@ -429,8 +430,9 @@ k_ln_forward_rows(const __grid_constant__ LnArgs a)
     }
 }
 
-// Rows that do not fit a block's registers: three passes over a row.
-template <typename X, int V>
+// Rows that do not fit a block's registers: three passes over a row.  kRuns: a thread has more than kRun columns to add (the
+// loops in two levels cost shorter rows 4 to 8 %).
+template <typename X, int V, bool kRuns>
 __global__ void __launch_bounds__(1024)
 k_ln_forward_long(const __grid_constant__ LnArgs a)
 {
@@ -438,25 +440,35 @@ k_ln_forward_long(const __grid_constant__ LnArgs a)
     const int row = blockIdx.x, t = threadIdx.x;
     const X* const x = static_cast<const X*>(a.x) + row * a.x_ld;
     float sum = 0.f, sq = 0.f;
-    for (int col = t * V; col < a.cols; col += 1024 * V) {
-        Vec<X, V> v;
-        v.load(x + col);
-        float s = 0.f;
+    for (int c0 = 0; c0 < (kRuns ? a.cols : 1); c0 += kRun * 1024 * V) {
+        const int c1 = kRuns ? min(a.cols, c0 + kRun * 1024 * V) : a.cols;
+        float run = 0.f;
+        for (int col = c0 + t * V; col < c1; col += 1024 * V) {
+            Vec<X, V> v;
+            v.load(x + col);
+            float s = 0.f;
 #pragma unroll
-        for (int k = 0; k < V; ++k) s += v.value(k);
-        sum += s;
+            for (int k = 0; k < V; ++k) s += v.value(k);
+            run += s;
+        }
+        sum += run;
     }
     const float mean = group_sum(sum, 0, 1024, t >> 5, room[0]) * a.inv_cols;
-    for (int col = t * V; col < a.cols; col += 1024 * V) {
-        Vec<X, V> v;
-        v.load(x + col);
-        float s = 0.f;
+    for (int c0 = 0; c0 < (kRuns ? a.cols : 1); c0 += kRun * 1024 * V) {
+        const int c1 = kRuns ? min(a.cols, c0 + kRun * 1024 * V) : a.cols;
+        float run = 0.f;
+        for (int col = c0 + t * V; col < c1; col += 1024 * V) {
+            Vec<X, V> v;
+            v.load(x + col);
+            float s = 0.f;
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float d = v.value(k) - mean;
-            s = fmaf(d, d, s);
+            for (int k = 0; k < V; ++k) {
+                const float d = v.value(k) - mean;
+                s = fmaf(d, d, s);
+            }
+            run += s;
         }
-        sq += s;
+        sq += run;
     }
     sq = group_sum(sq, 0, 1024, t >> 5, room[1]);
     const float rstd = __frsqrt_rn(fmaf(sq, a.inv_cols, a.eps));
@@ -679,23 +691,29 @@ k_ln_backward_rows(const __grid_constant__ LnArgs a, float2* out)
     const G* const dy = static_cast<const G*>(a.dy) + row * a.dy_ld;
     const float mean = a.mean[row], rstd = a.rstd[row];
     float s[2] = {0.f, 0.f};
-    for (int col = threadIdx.x * V; col < a.cols; col += blockDim.x * V) {
-        Vec<X, V> vx;
-        Vec<G, V> vg;
-        vx.load(x + col);
-        vg.load(dy + col);
-        float w[V], p = 0.f, q = 0.f;
+    for (int c0 = 0; c0 < a.cols; c0 += kRun * blockDim.x * V) {
+        const int c1 = min(a.cols, c0 + kRun * static_cast<int>(blockDim.x) * V);
+        float run[2] = {0.f, 0.f};
+        for (int col = c0 + threadIdx.x * V; col < c1; col += blockDim.x * V) {
+            Vec<X, V> vx;
+            Vec<G, V> vg;
+            vx.load(x + col);
+            vg.load(dy + col);
+            float w[V], p = 0.f, q = 0.f;
 #pragma unroll
-        for (int k = 0; k < V; ++k) w[k] = 1.f;
-        if (a.w) load_param<V>(a.w, a.w_bf16, col, w);
+            for (int k = 0; k < V; ++k) w[k] = 1.f;
+            if (a.w) load_param<V>(a.w, a.w_bf16, col, w);
 #pragma unroll
-        for (int k = 0; k < V; ++k) {
-            const float d = vg.value(k) * w[k];
-            p += d;
-            q = fmaf(d, (vx.value(k) - mean) * rstd, q);
+            for (int k = 0; k < V; ++k) {
+                const float d = vg.value(k) * w[k];
+                p += d;
+                q = fmaf(d, (vx.value(k) - mean) * rstd, q);
+            }
+            run[0] += p;
+            run[1] += q;
         }
-        s[0] += p;
-        s[1] += q;
+        s[0] += run[0];
+        s[1] += run[1];
     }
     group_sum(s, 0, blockDim.x, threadIdx.x >> 5, room);
     if (threadIdx.x == 0) out[row] = make_float2(s[0] * a.inv_cols, s[1] * a.inv_cols);
@@ -948,7 +966,8 @@ cudaError_t launch_forward_v(const LnArgs& a, cudaStream_t stream)
         if (a.cols <= 16 * 512) return launch_forward_once<X, 8, 2, 2>(a, 256, stream);
         if (a.cols <= 32 * 1024) return launch_forward_once<X, 8, 4, 1>(a, 256, stream);
     }
-    k_ln_forward_long<X, V><<<a.rows, 1024, 0, stream>>>(a);
+    if (a.cols > kRun * 1024 * V) k_ln_forward_long<X, V, true><<<a.rows, 1024, 0, stream>>>(a);
+    else k_ln_forward_long<X, V, false><<<a.rows, 1024, 0, stream>>>(a);
     return cudaGetLastError();
 }
 

@@ -397,3 +397,23 @@ def test_sums_over_many_long_rows(env):
     binding.layer_norm_backward(dy, x, mean, rstd, grad_bias=db, need_x=False)
     want = sum(part.double().sum(0) for part in dy.split(1000))
     assert bool(((db.double() - want).abs() <= (512 + 40) * U * want).all())
+
+
+def test_sums_over_a_very_long_row(env):
+    """2^27 - 1 equal numbers, whose roundings all go one way: a thread adds 256 in a row, then at most 512 such sums, and 10 levels
+    across the block; the mean's own factor and product are two more."""
+    torch, binding = env
+    x = torch.full((1, (1 << 27) - 1), 0.1, device="cuda")
+    value = float(x[0, 0])
+    e = (256 + 512 + 12) * U * value
+    y, mean, rstd = binding.layer_norm_forward(x)
+    assert abs(float(mean) - value) <= e
+    assert float(y.abs().max()) <= 2 * e * 1e-5 ** -0.5                  # the mean's error, and the differences' rounding
+    # the variance: squares of 0.1 (every second element has the other sign: the mean is 0.1 / n)
+    x[0, 1::2] = -value
+    _, _, rstd = binding.layer_norm_forward(x)
+    want = (value ** 2 + 1e-5) ** -0.5
+    assert abs(float(rstd) - want) <= want * ((256 + 512 + 16) * U / 2 + 3 * U)
+    # d is the same everywhere, and its mean is taken off: nothing is left but the mean's error
+    dx = binding.layer_norm_backward(torch.full_like(x, value), x, torch.zeros(1, device="cuda"), torch.ones(1, device="cuda"))
+    assert float(dx.abs().max()) <= 2 * e
