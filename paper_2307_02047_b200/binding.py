@@ -534,6 +534,21 @@ def _torch():
     return _torch_module
 
 
+_forward_ad = None
+
+
+def _refuse_tangents(*tensors) -> None:
+    """Forward-mode differentiation has no formulas here, and a result without a tangent would count as constant."""
+    global _forward_ad
+    if _forward_ad is None:
+        _forward_ad = _torch().autograd.forward_ad
+    if _forward_ad._current_level < 0:       # (looked at first: unpacking takes a microsecond for each tensor)
+        return
+    for t in tensors:
+        if t is not None and _forward_ad.unpack_dual(t).tangent is not None:
+            raise CameError(CAME_ERR_UNSUPPORTED, "a tensor carries a tangent: no forward-mode differentiation here")
+
+
 def _call_on(index, call, *args) -> None:
     """``call(*args, index, stream)`` with device ``index`` current; ``stream``: its current stream's
     address (asked for directly: a Stream object costs more than a launch)."""
@@ -764,6 +779,7 @@ def embed_forward(table, ids, scale: float = 1.0, out=None, out_dtype=None):
     When autograd records and the table requires grad, the result carries the graph: the table's
     gradient is ``embed_backward``'s, a whole matrix of its type (once differentiable).  ``out``
     must be None then; ``embed_backward`` itself adds to a buffer of the caller's."""
+    _refuse_tangents(table)
     if table.requires_grad and _torch().is_grad_enabled():
         if out is not None:
             raise CameError(CAME_ERR_UNSUPPORTED, "a table that requires grad takes no out: detach it, or disable grad mode")
@@ -793,6 +809,7 @@ def embed_backward(grad_out, ids, grad, scale: float = 1.0, padding_row: Optiona
     ``grad_out``: fp32 or bf16, shape ``(*ids.shape, cols)``; ``grad``: fp32 or bf16 matrix, every
     row of it written unless ``accumulate``; tokens of ``padding_row`` add nothing.  Returns
     ``grad``.  Bit-reproducible: a row's tokens are added in an order fixed by the ids."""
+    _refuse_tangents(grad_out)
     rows, cols, grad_ld, grad_code, index = _embed_table(grad, "grad")
     id_code = _embed_ids(ids, index)
     ld, code = _embed_data(grad_out, "grad_out", ids, cols, index)
@@ -1106,6 +1123,7 @@ def layer_norm_forward(x, weight=None, bias=None, eps: float = 1e-5, out=None, o
     shape, made here (of type ``out_dtype``, x's when that is None too) when it is None.  ``mean`` and ``rstd`` are fp32,
     one for each row, in the shape of x without its last dimension; with ``stats`` false they are not written and
     ``y`` alone is returned (inference).  No autograd: see ``layer_norm``."""
+    _refuse_tangents(x, weight, bias)
     torch = _torch()
     if _lib is None:
         load()
@@ -1149,6 +1167,7 @@ def layer_norm_backward(grad_out, x, mean, rstd, weight=None, grad_x=None, grad_
     them.  ``grad_weight``, ``grad_bias``: buffers of a row's length, in the weight's type (without a weight: fp32 or bf16,
     both the same), which receive the sums over all rows, or to which these are added with ``accumulate``; None: not
     wanted.  Returns ``grad_x``.  Bit-reproducible."""
+    _refuse_tangents(grad_out, x, mean, rstd, weight)
     torch = _torch()
     if _lib is None:
         load()
@@ -1226,6 +1245,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, out_dtype=None):
     (Of autograd in general: before a backward pass is captured into a CUDA graph, eager graphs of the same leaves
     have to be gone; torch ends the process otherwise.)"""
     if _torch().is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or (bias is not None and bias.requires_grad)):
+        _refuse_tangents(x, weight, bias)
         return _layer_norm_function().apply(x, weight, bias, eps, out_dtype)
     return layer_norm_forward(x, weight, bias, eps, out_dtype=out_dtype, stats=False)
 
@@ -1298,6 +1318,7 @@ def position_bias_forward(table, q_len: int, k_len: int, offset=0, bidirectional
 
     When autograd records and the table requires grad, the result carries the graph: the table's gradient is
     ``position_bias_backward``'s, in its type (once differentiable).  ``out`` must be None then."""
+    _refuse_tangents(table)
     if _lib is None:
         load()
     if table.requires_grad and _torch().is_grad_enabled():
@@ -1336,6 +1357,7 @@ def position_bias_backward(grad_out, grad, offset=0, bidirectional: bool = True,
     ``grad_out``: fp32 or bf16, ``(heads, q_len, k_len)`` or ``(batch, heads, q_len, k_len)`` (a bias that was added to a
     batch of scores), with any strides but a contiguous last dimension; ``grad``: fp32 or bf16 ``(buckets, heads)``.
     Returns ``grad``.  Bit-reproducible."""
+    _refuse_tangents(grad_out)
     if _lib is None:
         load()
     buckets, heads, ld, code, index = _embed_table(grad, "grad")
