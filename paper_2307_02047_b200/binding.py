@@ -11,6 +11,7 @@ that fails, or a call returns an error status, a ``CameError`` is raised.
 from __future__ import annotations
 
 import ctypes
+import operator
 import struct
 from typing import List, Optional, Sequence
 
@@ -1271,6 +1272,8 @@ def _posbias_backward_call(p, workspace, size, index, stream):
 def _offset_of(offset, index):
     """(address of an offset on the device, offset on the host)."""
     if isinstance(offset, int):
+        if not -1 << 40 <= offset <= 1 << 40:
+            raise CameError(CAME_ERR_SHAPE, "offset must lie in [-2^40, 2^40]")
         return 0, offset
     torch = _torch()
     if not isinstance(offset, torch.Tensor) or offset.dtype != torch.int64 or offset.numel() != 1:
@@ -1278,6 +1281,16 @@ def _offset_of(offset, index):
     if offset.get_device() != index:
         raise CameError(CAME_ERR_DEVICE, "offset must be on the table's GPU")
     return offset.data_ptr(), 0
+
+
+def _check_distance(max_distance) -> None:
+    """What the packed descriptor can hold (the library looks at the rest)."""
+    try:
+        fits = 0 <= operator.index(max_distance) <= 1 << 29
+    except TypeError:
+        fits = False
+    if not fits:
+        raise CameError(CAME_ERR_HPARAM, "max_distance must be a whole number, up to 2^29")
 
 
 def _position_bias_function():
@@ -1327,9 +1340,10 @@ def position_bias_forward(table, q_len: int, k_len: int, offset=0, bidirectional
         return _position_bias_function().apply(table, q_len, k_len, offset, bidirectional, max_distance, out_dtype)
     buckets, heads, ld, code, index = _embed_table(table, "table")
     offset_at, offset = _offset_of(offset, index)
+    _check_distance(max_distance)
     if out is None:
-        if q_len < 0 or k_len < 0:
-            raise CameError(CAME_ERR_SHAPE, "q_len and k_len must be at least 0")
+        if not (0 <= q_len <= 1 << 30 and 0 <= k_len <= 1 << 30) or heads * q_len * k_len > 1 << 40:
+            raise CameError(CAME_ERR_SHAPE, "q_len and k_len must lie in [0, 2^30], all elements together 2^40")
         out = table.new_empty((heads, q_len, k_len), dtype=out_dtype)
     else:
         if out_dtype is not None and out.dtype != out_dtype:
@@ -1362,6 +1376,7 @@ def position_bias_backward(grad_out, grad, offset=0, bidirectional: bool = True,
         load()
     buckets, heads, ld, code, index = _embed_table(grad, "grad")
     offset_at, offset = _offset_of(offset, index)
+    _check_distance(max_distance)
     if grad_out.get_device() != index:
         raise CameError(CAME_ERR_DEVICE, "grad_out must be on the table's GPU")
     data_code = _DTYPE_CODES.get(grad_out.dtype)

@@ -4,6 +4,7 @@ A sum of N terms is formed in fp32: a diagonal's in one register, a term for eac
 each batch of a warp, then at most 8 diagonals of a lane one after another and 5 levels across the warp (a short interval: 32 diagonals),
 units / 32 + 32 at the end.  For the sizes here (at most 3 batches, 1024 units) a term passes at most 3 * 128 + 32 + 64 additions,
 and no more than 512: the error is below 512 u of the sum of magnitudes (u = 2^-24), plus half a step of the stored type."""
+import numpy as np
 import pytest
 
 from tests.test_posbias_cpu import bucket
@@ -199,3 +200,19 @@ def test_large_batches_of_one_sign(env, dt, heads, q, k, batch, expanded):
     count = torch.bincount(_buckets(torch, q, k, 0, 32, 128, True).view(-1), minlength=32).double()
     want = (count * batch * float(one[0, 0, 0, 0]))[:, None].expand(-1, heads)
     assert bool(((grad.double() - want).abs() <= 561 * U * want).all()), float(((grad.double() - want).abs() / want.clamp(min=1e-9)).max()) / U
+
+
+def test_numbers_beyond_the_descriptor_are_refused(env):
+    """Offsets beyond 64 bits, distances beyond 32 and lengths beyond the limits: as the library refuses smaller ones, before anything is allocated."""
+    torch, binding = env
+    t, d = torch.randn(32, 4, device="cuda"), torch.randn(4, 5, 6, device="cuda")
+    f, g = binding.position_bias_forward, binding.position_bias_backward
+    for bad, status in (
+            (lambda: f(t, 3, 3, offset=1 << 64), 2), (lambda: f(t, 3, 3, offset=-(1 << 40) - 1), 2), (lambda: f(t, 3, 3, max_distance=1 << 33), 5),
+            (lambda: f(t, 3, 3, max_distance=-(1 << 40)), 5), (lambda: f(t, 3, 3, max_distance=128.0), 5), (lambda: f(t, 1 << 40, 1), 2), (lambda: f(t, 1, 1 << 70), 2),
+            (lambda: g(d, t, offset=1 << 64), 2), (lambda: g(d, t, offset=(1 << 40) + 1), 2), (lambda: g(d, t, max_distance=1 << 33), 5),
+            (lambda: f(t.clone().requires_grad_(), 3, 3, offset=1 << 64), 2), (lambda: f(t.clone().requires_grad_(), 3, 3, max_distance=1 << 33), 5)):
+        with pytest.raises(binding.CameError) as e:
+            bad()
+        assert e.value.status == status, e.value
+    assert torch.equal(f(t, 2, 3, offset=1 << 40), f(t, 2, 3, offset=1 << 20)) and torch.equal(f(t, 2, 3, max_distance=np.int64(99)), f(t, 2, 3, max_distance=99))
