@@ -464,7 +464,8 @@ came_status came_embed_backward(const came_embed* e, void* workspace, int64_t wo
  *   k = 0;  k = mix((k ^ w) + 0x3C6EF373) for w = low, high word of seed, low, high word of t
  *   b = number of the block, counted through the whole list of tensors (each has ceil(numel / 256))
  *   r = mix(mix(k + b * 0x9E3779B9) + (element in the block) * 0x9E3779B9)
- * m takes the low 16 bits of r, v the high ones.
+ * m takes the low 16 bits of r, v the high ones.  (An |m| above 1.875 2^127, a v above 1.75 2^127, may be stored as 2^128, which
+ * the next step reads as infinite.)
  *
  * Buffers may have any length (0 included) and any element-aligned address (rows of 256 elements that start
  * 32-byte aligned are faster); they are contiguous and, but for gradients, share no memory
@@ -525,10 +526,10 @@ came_status came_adamw_destroy(came_adamw_ctx* ctx);
  *             the terms in brackets with CAME_LAYERNORM_ACCUMULATE
  * Everything is computed in fp32 and rounded once to the stored type, to nearest even; a sum over a row adds up to
  * 264 + cols / 2^18 terms one after another, one over rows max(512, rows / 144), before it goes on by tree.  The variance is that of
- * the differences from the mean.  Sums are added in an order that depends on the sizes alone: results are
- * bit-reproducible.  Rows may have any stride >= cols and any element-aligned address (tensors of rows that
- * begin at a multiple of 8 elements, and whose strides agree modulo 8, are faster); weight, bias and their gradients
- * are contiguous.  What is written shares memory with nothing else (CAME_ERR_OVERLAP; the ranges from a buffer's
+ * the differences from the mean.  Sums are added in an order that depends on the sizes, the strides and the
+ * pointers' alignment alone: the same call gives the same bits.  Rows may have any stride >= cols and any
+ * element-aligned address (tensors of rows that begin at a multiple of 8 elements, and whose strides agree modulo 8,
+ * are faster); weight, bias and their gradients are contiguous.  What is written shares memory with nothing else (CAME_ERR_OVERLAP; the ranges from a buffer's
  * first to its last element count). */
 enum { CAME_LAYERNORM_ACCUMULATE = 1u << 0 };   /* backward: add to dweight and dbias */
 
@@ -573,8 +574,9 @@ came_status came_layernorm_backward(const came_layernorm* l, void* workspace, in
  *            min(n - 1, E + floor((n - E) log(d / E) / log(max_distance / E)))     else
  * where a d at a border belongs above it (the borders are found once per call and compared in
  * whole numbers).  Sums are formed in fp32 by at most 512 additions of a diagonal's terms one after another, 32 of a bucket's
- * diagonals and 16 of such sums, from there on in fp64, and rounded once, in an order that depends on the sizes alone:
- * results are bit-reproducible.  What is written shares memory with nothing that is read (CAME_ERR_OVERLAP). */
+ * diagonals and 16 of such sums, from there on in fp64, and rounded once, in an order that depends on the sizes, the strides and the
+ * pointer's alignment alone: the same call gives the same bits.  What is written shares memory with nothing that is
+ * read (CAME_ERR_OVERLAP). */
 enum {
     CAME_POSBIAS_BIDIRECTIONAL = 1u << 0,
     CAME_POSBIAS_ACCUMULATE    = 1u << 1     /* backward: add to dtable */

@@ -7,8 +7,8 @@
 // where states have 8 bits.  Nothing crosses from one such block to the next, so there is one pass, one
 // launch for each type of state and gradient in the list, and no order that could change a result.
 //
-// Bound by the bytes: 355 M elements with fp32 states and gradients move 9.9 GB in 1450 us (6.8 TB/s); 256 M with 8-bit
-// states, bf16 gradients and bf16 copies 4.1 GB in 626 us (6.5 TB/s, the measured copy rate).  The 8-bit form computes about 70
+// Bound by the bytes: 355 M elements with fp32 states and gradients move 9.9 GB in 1450 us (6.8 TB/s); 2^28 with 8-bit
+// states, bf16 gradients and bf16 copies 4.3 GB in 655 us (6.6 TB/s, the measured copy rate).  The 8-bit form computes about 70
 // instructions for an element, three quarters of what the SMs can issue in that time, a third of them for the random bits
 // and the rounding; one hash serves both states.
 #include "came_vec.cuh"
@@ -302,8 +302,8 @@ __device__ __forceinline__ void adamw_block(const AdamwTensor& d, const G* grad,
     }
 }
 
-// 8 bits: registers for three blocks per SM (256 M elements: 583 us, against 645 with two and 649 with four, whose
-// registers do not hold the block that is on its way).
+// 8 bits: registers for three blocks per SM (2^28 elements with bf16 gradients and copies: 655 us, against 742 with two and 682
+// with four, whose registers do not hold the block that is on its way; fp32 gradients, no copies: 636, 712 and 797).
 template <int BITS, typename G, bool kFull>
 __global__ void __launch_bounds__(kWarps * 32, BITS == 8 ? 3 : 1)
 k_adamw(const AdamwTensor* __restrict__ table, const void* const* __restrict__ grads, const AdamwTile* __restrict__ tiles,
@@ -353,8 +353,8 @@ k_adamw(const AdamwTensor* __restrict__ table, const void* const* __restrict__ g
         adamw_block<BITS, G, kFull, decltype(is_wide)::value>(d, grad, now, b, left, f, key, e);
         if (lane == j) scales = e;
     };
-    // 8 bits: the next block is on its way while this one is computed (256 M elements: 642 us, 738 without); fp32 states
-    // compute so little that it only costs registers (64 M: 276 and 273 us).
+    // 8 bits: the next block is on its way while this one is computed (2^28 elements with bf16 gradients and copies: 655 us, 750
+    // without); fp32 states compute so little that it only costs registers (64 M: 276 and 273 us).
     constexpr bool kAhead = BITS == 8;
     if (kAhead && b < wide) ahead.load(d, grad, b);
     for (; b < wide; b += kWarps) {

@@ -344,7 +344,8 @@ came_status validate_posbias(const came_posbias* p, bool backward)
 
 struct BackwardPlan { int tile_rows, chunks, batches, batch_groups, period; long long tiles, units, bytes; };
 
-// Rows that a warp goes down, and batches for a warp: as many as leave every SM about 32 warps.
+// Rows that a warp goes down, and batches for a warp: as many as make 32 warps for each SM, of which the kernels' registers let 24
+// (fp32: 16) run at a time (9 x 8 x 1023 x 1025 fp32: 72 us, 77 with 24 or 48 warps; 64 x 12 x 512 x 512 bf16: 108, 101 and 105).
 BackwardPlan plan_backward(const came_posbias& p)
 {
     BackwardPlan b = {};
